@@ -523,6 +523,108 @@ int ct_test_watchdog(int n_events, const int32_t *runs, const double *done_at_s,
  * use: tile_of_block[b] for b < tiles. */
 int ct_test_xcd_band(int tiles, int32_t *tile_of_block);
 
+/* ---- operators of a sequence block ----
+ *
+ * The operators of a recurrent sequence block as it is served: projections
+ * with their epilogue, the short causal convolution along the tokens and the
+ * selective scan. Each call enqueues its kernels on the caller's HIP stream (a
+ * hipStream_t; NULL = the null stream) and returns without waiting. It
+ * allocates nothing, holds nothing from one call to the next and records only
+ * kernels, so it may be captured into a HIP graph. Calls may overlap on any
+ * streams and threads as long as they share no workspace and no output.
+ * Scratch memory, where an operator needs any, is the caller's: the
+ * *_workspace function gives its size in bytes (0: none; it then may be NULL),
+ * its contents need no preparation, and its address is a multiple of 16. All
+ * need ct_init. Results do not depend on timing: the same inputs give the same
+ * bits. Pointers are to device memory and aligned to their element; rows are
+ * contiguous, and lie ld* elements apart. Rows and pointers at multiples of 16
+ * bytes are read faster. A product's rows are at most 4 MiB apart (x, w) and
+ * its sums are in fp32. */
+
+#define CT_ACT_NONE  0
+#define CT_ACT_RELU  1
+#define CT_ACT_RELU6 2
+#define CT_ACT_SILU  3  /* v / (1 + exp(-v))             */
+#define CT_ACT_GELU  4  /* v / 2 (1 + erf(v / sqrt(2)))  */
+
+#define CT_RES_NONE    0
+#define CT_RES_ADD     1  /* y = act(v) + r */
+#define CT_RES_ADD_ACT 2  /* y = act(v + r) */
+
+/* y[i,j] = act(v[i,j]) with v = x w^T + bias, and the residual r as `res` says:
+ * x is m x k, w n x k (an output's weights are a row), r and y are m x n. m, n
+ * and k may be 0 (k = 0: v = bias). NaN goes through every activation. */
+typedef struct ct_linear_op {
+    int32_t m, n, k;
+    int32_t dtype;      /* CT_DT_*: x and w               */
+    int32_t out_dtype;  /* CT_DT_*: r and y; bias is fp32 */
+    int32_t act;        /* CT_ACT_*                       */
+    int32_t res;        /* CT_RES_*                       */
+    int32_t reserved;   /* 0                              */
+    int64_t ldx, ldw, ldr, ldy;
+} ct_linear_op;
+
+int ct_linear_workspace(const ct_linear_op *op, int64_t *bytes);
+/* bias may be NULL; res is read only where op->res asks for it, and may be y
+ * itself (with ldr = ldy). */
+int ct_linear_run(const ct_linear_op *op, const void *x, const void *w, const float *bias, const void *res,
+                  void *y, void *ws, int64_t ws_bytes, void *stream);
+
+/* Sequences packed one after another along the token rows. With offsets (device
+ * memory, count + 1 ascending values of 0..tokens) sequence i is the rows
+ * offsets[i] .. offsets[i+1]-1, possibly none; rows of no sequence are neither
+ * read nor written. Without, the rows are `count` sequences of equal length
+ * (tokens is a multiple of count). slots (device memory, count values): the row
+ * of sequence i in the state arrays, without: i. A sequence whose slot is not
+ * one of 0..num_slots-1 (-1, say) starts from zeros and leaves no state; no two
+ * sequences share another. Offsets and slots are read by the kernels and never
+ * checked on the host: bad ones give wrong results but no access out of bounds. */
+typedef struct ct_sequences {
+    int32_t tokens, count, num_slots;
+    int32_t max_len;  /* upper bound of the lengths, for the choice of a kernel; 0: unknown */
+    const int32_t *offsets, *slots;
+} ct_sequences;
+
+/* Causal depthwise convolution along the tokens of each sequence:
+ *   y[t,c] = act(bias[c] + sum_{j < width} w[c,j] x[t - width + 1 + j, c]),
+ * x and y tokens x channels in `dtype`, w (channels x width) and bias fp32. Rows
+ * before a sequence's start come from state_in (slots x (width-1) x channels in
+ * `dtype`, oldest first), or are 0 without it; state_out (optional, may be
+ * state_in itself) takes the last width-1 rows of state and sequence together.
+ * act: CT_ACT_NONE or CT_ACT_SILU; width 2..8. */
+typedef struct ct_causal_conv_op {
+    int32_t channels, width;
+    int32_t dtype, act;
+    int64_t ldx, ldy;
+} ct_causal_conv_op;
+
+int ct_causal_conv_run(const ct_causal_conv_op *op, const ct_sequences *seqs, const void *x, const float *w,
+                       const float *bias, const void *state_in, void *state_out, void *y, void *stream);
+
+/* Selective state space scan of each sequence, for channel d with state h of
+ * `states` values and group g = d / (channels / groups):
+ *   dt_t = delta[t,d] + dt_bias[d], through softplus if asked for;
+ *   h_t[n] = exp(dt_t a[d,n]) h_{t-1}[n] + dt_t u[t,d] b[t,g,n];
+ *   y[t,d] = (sum_n c[t,g,n] h_t[n] + d_skip[d] u[t,d]) * z / (1 + exp(-z)), z = z[t,d].
+ * u, delta, z, y (tokens x channels) and b, c (tokens x groups x states) in
+ * `dtype`; a (channels x states), dt_bias, d_skip (channels) and the states
+ * (slots x channels x states) fp32. dt_bias, d_skip, z, state_in (zeros) and
+ * state_out may be NULL; state_out may be state_in itself. states 1..256;
+ * groups divides channels. */
+typedef struct ct_scan_op {
+    int32_t channels, states, groups;
+    int32_t dtype;
+    int32_t softplus;  /* 0 or 1 */
+    int32_t reserved;  /* 0      */
+    int64_t ldu, lddelta, ldb, ldc, ldz, ldy;
+} ct_scan_op;
+
+int ct_scan_workspace(const ct_scan_op *op, const ct_sequences *seqs, int64_t *bytes);
+int ct_scan_run(const ct_scan_op *op, const ct_sequences *seqs, const void *u, const void *delta,
+                const float *dt_bias, const float *a, const void *b, const void *c, const float *d_skip,
+                const void *z, const float *state_in, float *state_out, void *y, void *ws, int64_t ws_bytes,
+                void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -22,6 +22,9 @@ CT_OK, CT_E_ARG, CT_E_HIP, CT_E_NOINIT, CT_E_OOM, CT_E_NODEV = 0, -1, -2, -3, -4
 CT_E_TIMEOUT, CT_E_CLIENT, CT_E_STOPPED = -6, -7, -8
 S_OK, S_INVALID, S_LAUNCH, S_TIMEOUT, S_WRONG_ANSWER = 0, 1, 2, 3, 4
 STATUS_NAMES = {0: "ok", 1: "invalid", 2: "launch_error", 3: "timeout", 4: "wrong_answer"}
+DT_F32, DT_BF16 = 0, 1
+ACT_NONE, ACT_RELU, ACT_RELU6, ACT_SILU, ACT_GELU = 0, 1, 2, 3, 4
+RES_NONE, RES_ADD, RES_ADD_ACT = 0, 1, 2
 MASK_WORDS = 8
 MAX_KNOBS = 15
 
@@ -84,6 +87,26 @@ class ct_search_result(ctypes.Structure):
                 ("winner_lat_us", c_f32), ("pad_", c_f32), ("propose_s", c_f64), ("measure_s", c_f64)]
 
 
+class ct_linear_op(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("m", "n", "k", "dtype", "out_dtype", "act", "res", "reserved")] + \
+               [(n, c_i64) for n in ("ldx", "ldw", "ldr", "ldy")]
+
+
+class ct_sequences(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("tokens", "count", "num_slots", "max_len")] + \
+               [(n, ctypes.c_void_p) for n in ("offsets", "slots")]
+
+
+class ct_causal_conv_op(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("channels", "width", "dtype", "act")] + [(n, c_i64) for n in ("ldx", "ldy")]
+
+
+class ct_scan_op(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("channels", "states", "groups", "dtype", "softplus", "reserved")] + \
+               [(n, c_i64) for n in ("ldu", "lddelta", "ldb", "ldc", "ldz", "ldy")]
+
+
+_VP = ctypes.c_void_p
 _SIGS = {
     "ct_init": (c_i32, [c_i32]),
     "ct_num_cus": (c_i32, []),
@@ -135,6 +158,11 @@ _SIGS = {
     "ct_probe_empty": (c_i32, [P(c_u32), c_i32, c_i32, P(ct_measure_opts), P(c_f32)]),
     "ct_probe_copy": (c_i32, [P(c_u32), c_i32, ctypes.c_void_p, ctypes.c_void_p, c_i64, P(ct_measure_opts),
                               P(c_f32)]),
+    "ct_linear_workspace": (c_i32, [P(ct_linear_op), P(c_i64)]),
+    "ct_linear_run": (c_i32, [P(ct_linear_op)] + [_VP] * 6 + [c_i64, _VP]),
+    "ct_causal_conv_run": (c_i32, [P(ct_causal_conv_op), P(ct_sequences)] + [_VP] * 7),
+    "ct_scan_workspace": (c_i32, [P(ct_scan_op), P(ct_sequences), P(c_i64)]),
+    "ct_scan_run": (c_i32, [P(ct_scan_op), P(ct_sequences)] + [_VP] * 12 + [c_i64, _VP]),
 }
 
 _lock = threading.Lock()
@@ -544,6 +572,74 @@ def ct_probe_copy(cu_mask, src, dst, nbytes: int, opts: ct_measure_opts) -> floa
     _check(lib().ct_probe_copy(m, MASK_WORDS if m is not None else 0, _ptr(src), _ptr(dst), nbytes,
                                ctypes.byref(opts), ctypes.byref(g)))
     return g.value
+
+
+# ---------------------------------------------------------------- operators of a sequence block
+def make_linear(m, n, k, dtype, out_dtype, act=ACT_NONE, res=RES_NONE, ldx=0, ldw=0, ldr=0, ldy=0) -> ct_linear_op:
+    """y[m, n] = act(x w^T + bias) with a residual; a pitch of 0 is that of a contiguous array."""
+    return ct_linear_op(int(m), int(n), int(k), int(dtype), int(out_dtype), int(act), int(res), 0,
+                        int(ldx) or k, int(ldw) or k, int(ldr) or n, int(ldy) or n)
+
+
+def make_sequences(tokens, count, num_slots=0, max_len=0, offsets=None, slots=None) -> ct_sequences:
+    """Packed sequences; offsets and slots are int32 device tensors (or addresses), which the
+    returned object keeps alive."""
+    s = ct_sequences(int(tokens), int(count), int(num_slots), int(max_len), _ptr(offsets), _ptr(slots))
+    s.held = (offsets, slots)
+    return s
+
+
+def make_causal_conv(channels, width, dtype, act=ACT_NONE, ldx=0, ldy=0) -> ct_causal_conv_op:
+    return ct_causal_conv_op(int(channels), int(width), int(dtype), int(act), int(ldx) or channels,
+                             int(ldy) or channels)
+
+
+def make_scan(channels, states, groups, dtype, softplus=True, ldu=0, lddelta=0, ldb=0, ldc=0, ldz=0,
+              ldy=0) -> ct_scan_op:
+    gn = groups * states
+    return ct_scan_op(int(channels), int(states), int(groups), int(dtype), int(softplus), 0, int(ldu) or channels,
+                      int(lddelta) or channels, int(ldb) or gn, int(ldc) or gn, int(ldz) or channels,
+                      int(ldy) or channels)
+
+
+def ct_linear_workspace(op: ct_linear_op) -> int:
+    """Bytes of scratch memory that ct_linear_run needs for op."""
+    n = c_i64()
+    _check(lib().ct_linear_workspace(ctypes.byref(op), ctypes.byref(n)))
+    return n.value
+
+
+def _ws(ws, nbytes):
+    """(address, bytes) of a workspace tensor, or of an address with its size."""
+    if ws is None or isinstance(ws, int):
+        return ws, nbytes
+    return ws.data_ptr(), ws.numel() * ws.element_size()
+
+
+def ct_linear_run(op: ct_linear_op, x, w, bias, res, y, ws=None, stream: int = 0, ws_bytes: int = 0) -> None:
+    """Enqueued on `stream` (a raw HIP stream handle, 0 = the null stream); returns without waiting."""
+    ws, nbytes = _ws(ws, ws_bytes)
+    _check(lib().ct_linear_run(op, _ptr(x), _ptr(w), _ptr(bias), _ptr(res), _ptr(y), ws, nbytes, stream or None))
+
+
+def ct_causal_conv_run(op: ct_causal_conv_op, seqs: ct_sequences, x, w, bias, state_in, state_out, y,
+                       stream: int = 0) -> None:
+    _check(lib().ct_causal_conv_run(op, seqs, _ptr(x), _ptr(w), _ptr(bias), _ptr(state_in), _ptr(state_out), _ptr(y),
+                                    stream or None))
+
+
+def ct_scan_workspace(op: ct_scan_op, seqs: ct_sequences) -> int:
+    """Bytes of scratch memory that ct_scan_run needs for op and seqs."""
+    n = c_i64()
+    _check(lib().ct_scan_workspace(ctypes.byref(op), ctypes.byref(seqs), ctypes.byref(n)))
+    return n.value
+
+
+def ct_scan_run(op: ct_scan_op, seqs: ct_sequences, u, delta, dt_bias, a, b, c, d_skip, z, state_in, state_out, y,
+                ws=None, stream: int = 0, ws_bytes: int = 0) -> None:
+    ws, nbytes = _ws(ws, ws_bytes)
+    _check(lib().ct_scan_run(op, seqs, _ptr(u), _ptr(delta), _ptr(dt_bias), _ptr(a), _ptr(b), _ptr(c), _ptr(d_skip),
+                             _ptr(z), _ptr(state_in), _ptr(state_out), _ptr(y), ws, nbytes, stream or None))
 
 
 def header_functions(header_path: Optional[str] = None) -> List[str]:

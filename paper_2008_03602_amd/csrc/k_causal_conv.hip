@@ -1,0 +1,183 @@
+// Causal depthwise convolution along the tokens of packed sequences, its history in slots.
+//   y[t,c] = act(bias[c] + sum_{j<W} w[c,j] x[t-W+1+j, c])
+//
+// A wave computes a tile of U consecutive tokens of one sequence for 64 lanes of VEC
+// channels. All U + W - 1 rows that the tile reads are in flight before the first product,
+// and each output is W multiply-adds in fp32 in the order of j. The W - 1 rows before the
+// tile are read again by it (from the caches: they were read by the tile before).
+// The tile that starts a sequence alone reads its history, and alone writes the new one,
+// after that: in place needs no more than the order of a lane's own accesses.
+#include <hip/hip_runtime.h>
+
+#include "k_seq.h"
+
+namespace ct {
+
+struct ConvArgs {
+  SeqView s;
+  const void* x;
+  const float *w, *bias;
+  const void* state_in;
+  void *state_out, *y;
+  int64_t ldx, ldy;
+  int channels, act, per;
+  int64_t tiles;
+  FastDiv dblocks;  // waves across the channels
+};
+
+// VEC elements at p: one 16-byte access, or a single element.
+template <typename T, int VEC>
+struct Pack {
+  static constexpr int WORDS = VEC == 1 ? 1 : VEC * (int)sizeof(T) / 4;
+  unsigned q[WORDS];
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (VEC == 1) {
+      q[0] = sizeof(T) == 4 ? *(const unsigned*)p : *(const unsigned short*)p;
+    } else {
+      const u32x4 v = *(const u32x4*)p;
+      const unsigned a = v.x, b = v.y, c = v.z, d = v.w;
+      q[0] = a; q[1] = b; q[2] = c; q[3] = d;
+    }
+  }
+  __device__ __forceinline__ void store(T* p) const {
+    if constexpr (VEC == 1) {
+      if constexpr (sizeof(T) == 4) *(unsigned*)p = q[0];
+      else *(unsigned short*)p = (unsigned short)q[0];
+    } else {
+      *(u32x4*)p = (u32x4){q[0], q[1], q[2], q[3]};
+    }
+  }
+  __device__ __forceinline__ void zero() {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) q[i] = 0;
+  }
+  __device__ __forceinline__ float get(int i) const {
+    return sizeof(T) == 4 ? unpack<T>(q[i], 0) : unpack<T>(q[i / 2], i % 2);
+  }
+  __device__ __forceinline__ void set(const float* v) {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i)
+      if constexpr (sizeof(T) == 4) q[i] = __builtin_bit_cast(unsigned, v[i]);
+      else q[i] = pack_bf16(v[2 * i < VEC ? 2 * i : 0], v[2 * i + 1 < VEC ? 2 * i + 1 : 0]);
+  }
+};
+
+template <typename T, int W, int VEC, int U>
+__global__ void __launch_bounds__(256) causal_conv_kernel(ConvArgs a) {
+  using P = Pack<T, VEC>;
+  const int64_t g = (int64_t)blockIdx.x * 4 + wave_id();
+  if (g >= a.tiles * a.dblocks.d) return;
+  const int id = fdiv((int)g, a.dblocks), cb = (int)g - id * a.dblocks.d;
+  int t0;
+  const SeqRange r = find_tile(a.s, a.per, U, id, &t0);
+  const bool first = t0 == r.begin;
+  if (r.s < 0 || (t0 >= r.end && !first)) return;
+  const int c = (cb * 64 + (int)(threadIdx.x & 63)) * VEC;
+  if (c >= a.channels) return;
+
+  const T* x = (const T*)a.x + c;
+  P row[U + W - 1];
+  if (first) {
+    const int slot = seq_slot(a.s, r.s);
+    const int64_t at = ((int64_t)slot * (W - 1)) * a.channels + c;
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i)
+      if (slot >= 0 && a.state_in)
+        row[i].load((const T*)a.state_in + at + (int64_t)i * a.channels);
+      else
+        row[i].zero();
+    if (slot >= 0 && a.state_out) {
+      const int len = r.end - r.begin;
+      P next[W - 1];
+#pragma unroll
+      for (int i = 0; i < W - 1; ++i) {
+        if (len + i >= W - 1)
+          next[i].load(x + (int64_t)(r.end - (W - 1) + i) * a.ldx);
+        else  // a sequence shorter than the history: part of the old one stays
+#pragma unroll
+          for (int k = 0; k < W - 1; ++k)
+            if (k == len + i) next[i] = row[k];
+      }
+#pragma unroll
+      for (int i = 0; i < W - 1; ++i) next[i].store((T*)a.state_out + at + (int64_t)i * a.channels);
+    }
+    if (r.end == r.begin) return;
+  } else {
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i) row[i].load(x + (int64_t)(t0 - (W - 1) + i) * a.ldx);
+  }
+#pragma unroll
+  for (int i = 0; i < U; ++i) row[W - 1 + i].load(x + (int64_t)min(t0 + i, r.end - 1) * a.ldx);
+
+  float w[W][VEC], bias[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) {
+    bias[i] = a.bias ? a.bias[c + i] : 0.f;
+#pragma unroll
+    for (int j = 0; j < W; ++j) w[j][i] = a.w[(int64_t)(c + i) * W + j];
+  }
+  T* y = (T*)a.y + c;
+#pragma unroll
+  for (int t = 0; t < U; ++t) {
+    if (t0 + t >= r.end) break;
+    float v[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+      v[i] = bias[i];
+#pragma unroll
+      for (int j = 0; j < W; ++j) v[i] = fmaf(w[j][i], row[t + j].get(i), v[i]);
+      if (a.act == CT_ACT_SILU) v[i] = silu_f32(v[i]);
+    }
+    P out;
+    out.set(v);
+    out.store(y + (int64_t)(t0 + t) * a.ldy);
+  }
+}
+
+template <typename T, int W, int VEC, int U>
+static int conv_launch(ConvArgs a, hipStream_t st) {
+  const SeqTiles n = seq_tiles(a.s, U);
+  a.tiles = n.total;
+  a.per = n.per;
+  a.dblocks = make_fastdiv((a.channels + 64 * VEC - 1) / (64 * VEC));
+  const int64_t blocks = (n.total * a.dblocks.d + 3) / 4;
+  if (n.total * a.dblocks.d > 0x7FFFFFFF) return refuse_size("ct_causal_conv_run");
+  hipLaunchKernelGGL((causal_conv_kernel<T, W, VEC, U>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+  return hipGetLastError() == hipSuccess ? 0 : -1;
+}
+template <typename T, int W>
+static int conv_pick(const ConvArgs& a, bool wide, hipStream_t st) {
+  constexpr int V = 16 / (int)sizeof(T);
+  const bool step = !a.s.offsets && a.s.len <= 1;
+  if (wide) return step ? conv_launch<T, W, V, 1>(a, st) : conv_launch<T, W, V, 16>(a, st);
+  return step ? conv_launch<T, W, 1, 1>(a, st) : conv_launch<T, W, 1, 16>(a, st);
+}
+template <typename T>
+static int conv_pick_width(const ConvArgs& a, int width, bool wide, hipStream_t st) {
+  switch (width) {
+    case 2: return conv_pick<T, 2>(a, wide, st);
+    case 3: return conv_pick<T, 3>(a, wide, st);
+    case 4: return conv_pick<T, 4>(a, wide, st);
+    case 5: return conv_pick<T, 5>(a, wide, st);
+    case 6: return conv_pick<T, 6>(a, wide, st);
+    case 7: return conv_pick<T, 7>(a, wide, st);
+    default: return conv_pick<T, 8>(a, wide, st);
+  }
+}
+
+int launch_causal_conv(const ct_causal_conv_op& op, const SeqView& s, const void* x, const float* w,
+                       const float* bias, const void* state_in, void* state_out, void* y, void* stream) {
+  ConvArgs a = {};
+  a.s = s;
+  a.x = x; a.w = w; a.bias = bias; a.state_in = state_in; a.state_out = state_out; a.y = y;
+  a.ldx = op.ldx; a.ldy = op.ldy; a.channels = op.channels; a.act = op.act;
+  // 16-byte accesses need every row on a 16-byte address, the history's too
+  const int v = 16 / elem_bytes(op.dtype);
+  const bool wide = ((uintptr_t)x | (uintptr_t)y | (uintptr_t)state_in | (uintptr_t)state_out) % 16 == 0 &&
+                    op.ldx % v == 0 && op.ldy % v == 0 && op.channels % v == 0;
+  hipStream_t st = (hipStream_t)stream;
+  return op.dtype == CT_DT_BF16 ? conv_pick_width<bf16_t>(a, op.width, wide, st)
+                                : conv_pick_width<float>(a, op.width, wide, st);
+}
+
+}  // namespace ct

@@ -1,0 +1,126 @@
+// Device helpers of the sequence-block operators.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "k_util.h"
+#include "seq_internal.h"
+
+namespace ct {
+
+typedef __bf16 bf16_t;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Refuses a launch of more waves or blocks than the kernels' 31-bit numbers can name.
+inline int refuse_size(const char* who) {
+  set_error(std::string(who) + ": too large for one launch");
+  return -2;
+}
+
+// ---- 32-bit words of packed elements ----
+// Element i of a 16-bit pair, or the word itself.
+template <typename T>
+__device__ __forceinline__ float unpack(unsigned word, int i) {
+  if constexpr (sizeof(T) == 4)
+    return __builtin_bit_cast(float, word);
+  else  // a bf16 is the upper half of the fp32 with its value
+    return __builtin_bit_cast(float, i ? word & 0xFFFF0000u : word << 16);
+}
+// Two fp32 rounded to nearest even into one word.
+__device__ __forceinline__ unsigned pack_bf16(float lo, float hi) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  bf16x2 p;
+  p.x = (__bf16)lo;
+  p.y = (__bf16)hi;
+  return __builtin_bit_cast(unsigned, p);
+}
+template <typename T>
+__device__ __forceinline__ T from_f32(float v) {
+  return (T)v;
+}
+
+// ---- scalar functions in fp32 ----
+constexpr float kLog2e = 1.4426950408889634f;
+// v_exp_f32: within an ulp, results below 2^-126 flushed to 0.
+__device__ __forceinline__ float exp_f32(float v) { return __builtin_amdgcn_exp2f(v * kLog2e); }
+// v / (1 + exp(-v)) through the approximate reciprocal (an ulp). exp(-v) = inf gives -0
+// for every finite v, as the limit does.
+__device__ __forceinline__ float silu_f32(float v) { return v * __builtin_amdgcn_rcpf(1.f + exp_f32(-v)); }
+// log(1 + exp(v)) = max(v, 0) + log1p(e), e = exp(-|v|). The step sizes of a scan are the
+// small values of this function, where log(1 + e) has lost e's low bits: u = 1 + e is
+// rounded, and log1p(e) = log(u) + (e - (u - 1)) / u to first order in that rounding.
+__device__ __forceinline__ float softplus_f32(float v) {
+  const float e = exp_f32(-fabsf(v)), u = 1.f + e;
+  const float l = __builtin_amdgcn_logf(u) * 0.6931471805599453f;
+  const float top = v < 0.f ? 0.f : v;  // keeps NaN
+  return top + fmaf(e - (u - 1.f), __builtin_amdgcn_rcpf(u), l);
+}
+// Comparisons that keep NaN, unlike fmax.
+__device__ __forceinline__ float activate(float v, int act) {
+  switch (act) {
+    case CT_ACT_RELU: return v < 0.f ? 0.f : v;
+    case CT_ACT_RELU6: return v < 0.f ? 0.f : (v > 6.f ? 6.f : v);
+    case CT_ACT_SILU: return silu_f32(v);
+    case CT_ACT_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
+  }
+  return v;
+}
+
+// ---- sequences ----
+struct SeqRange {
+  int s, begin, end;  // rows begin..end-1 of sequence s
+};
+// The rows of sequence s, kept inside 0..tokens whatever the offsets hold.
+__device__ __forceinline__ SeqRange seq_range(const SeqView& v, int s) {
+  if (!v.offsets) return {s, s * v.len, s * v.len + v.len};
+  const int b = min(max(v.offsets[s], 0), v.tokens), e = min(max(v.offsets[s + 1], b), v.tokens);
+  return {s, b, e};
+}
+// State slot of sequence s, -1 for none.
+__device__ __forceinline__ int seq_slot(const SeqView& v, int s) {
+  const int slot = v.slots ? v.slots[s] : s;
+  return slot >= 0 && slot < v.num_slots ? slot : -1;
+}
+
+// Sequences cut into tiles of `step` rows that start at a sequence's own start. Sequence s
+// owns the tile numbers from begin / step + s on: at least one, so that an empty sequence
+// has a tile too, and never more than begin to end can need. A few numbers at the end of a
+// sequence are unused.
+struct SeqTiles {
+  int64_t total;
+  int per;  // tiles of each sequence where the lengths are equal
+};
+inline SeqTiles seq_tiles(const SeqView& v, int step) {
+  if (v.offsets) return {(int64_t)v.tokens / step + v.count, 0};
+  const int per = v.len > step ? (v.len + step - 1) / step : 1;
+  return {(int64_t)per * v.count, per};
+}
+// The sequence that tile `id` belongs to (s = -1: none) and, in *first, the row that the tile
+// starts at: at or past the end for an unused number. Uniform over the wave, which looks
+// 64 sequences up at a time.
+__device__ __forceinline__ SeqRange find_tile(const SeqView& v, int per, int step, int id, int* first) {
+  if (!v.offsets) {
+    const int s = id / per;
+    const SeqRange r = seq_range(v, s);
+    *first = r.begin + (id - s * per) * step;
+    return r;
+  }
+  const int lane = (int)(threadIdx.x & 63);
+  int lo = 0, n = v.count;
+  while (true) {
+    const int stride = (n + 63) / 64, i = lane * stride;
+    const bool at_or_before =
+        i < n && min(max(v.offsets[lo + min(i, n - 1)], 0), v.tokens) / step + lo + i <= id;
+    const uint64_t below = __ballot(!at_or_before);  // the first lane past the tile
+    const int k = below ? __builtin_ctzll(below) : 64;
+    if (k == 0) return {-1, 0, 0};
+    lo += (k - 1) * stride;
+    n = min(stride, n - (k - 1) * stride);
+    if (n <= 1) break;
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  const SeqRange r = seq_range(v, lo);
+  *first = r.begin + (id - (r.begin / step + lo)) * step;
+  return r;
+}
+
+}  // namespace ct

@@ -112,6 +112,10 @@ static int check_init() {
   return CT_OK;
 }
 
+// For the entry points outside this unit (sequence.cpp).
+int require_init() { return check_init(); }
+int launch_failed(const char* what) { return hip_fail((std::string(what) + " launch").c_str(), hipGetLastError()); }
+
 static int mask_words_needed() { return (g_num_cus + 31) / 32; }
 
 static int make_key(const uint32_t* mask, int words, MaskKey* key) {

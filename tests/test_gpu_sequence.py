@@ -1,0 +1,618 @@
+"""The sequence-block operators against their formulas in 64 bits on the CPU.
+
+Tolerances are error bounds worked out beside each reference, elementwise: u = 2^-24 for
+every fp32 operation on what it adds up, a few units for exp, log and reciprocals, and the
+output's own rounding (2^-8 relative for bf16, 2^-24 for fp32)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2008_03602_amd import _lib as L
+from gpu_util import device_ready, note
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+F, B = torch.float32, torch.bfloat16
+CODE = {F: L.DT_F32, B: L.DT_BF16}
+ROUND = {F: U, B: 2.0 ** -8}
+NAN = float("nan")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _device():
+    device_ready()
+    yield
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+def gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def normal(g, *shape, std=1.0, mean=0.0, dtype=F):
+    return (torch.randn(shape, generator=g) * std + mean).to(dtype)
+
+
+def placed(t, pitch=0, shift=0, fill=NAN):
+    """t on the GPU as rows `pitch` apart, `shift` elements into its storage; what lies between is NaN."""
+    rows, cols = t.shape
+    pitch = pitch or cols
+    flat = torch.full((rows * pitch + shift + 64,), fill, dtype=t.dtype, device="cuda")
+    view = flat[shift:shift + rows * pitch].view(rows, pitch)[:, :cols]
+    view.copy_(t)
+    return view
+
+
+def within(got, ref, bound, what):
+    got = got.detach().cpu().double()
+    assert got.shape == ref.shape, what
+    bad_kind = torch.isnan(got) != torch.isnan(ref)
+    assert not bad_kind.any(), what + ": NaN in the wrong places"
+    fine = ~torch.isnan(ref)
+    if fine.any():
+        err = (got - ref).abs()[fine]
+        worst = (err / (bound[fine] + 1e-38)).max().item()
+        assert worst <= 1.0, "%s: error %.2f times the bound" % (what, worst)
+
+
+# ------------------------------------------------------------------ linear
+def act64(v, act):
+    if act == L.ACT_RELU:
+        return torch.where(v < 0, torch.zeros_like(v), v)
+    if act == L.ACT_RELU6:
+        return torch.where(v < 0, torch.zeros_like(v), torch.where(v > 6, torch.full_like(v, 6.0), v))
+    if act == L.ACT_SILU:
+        return v / (1 + torch.exp(-v))
+    if act == L.ACT_GELU:
+        return 0.5 * v * (1 + torch.erf(v / math.sqrt(2)))
+    return v
+
+
+def check_linear(m, n, k, dtype, out, act=0, res=0, bias=True, seed=0, pitches=(0, 0, 0, 0), shifts=(0, 0, 0, 0),
+                 in_place=False, garbage_ws=True, what=""):
+    g = gen(seed)
+    x, w = normal(g, m, k, dtype=dtype), normal(g, n, k, std=max(k, 1) ** -0.5, dtype=dtype)
+    b = normal(g, n) if bias else None
+    r = normal(g, m, n, dtype=out) if res else None
+    what = what or "linear m%d n%d k%d %s->%s act%d res%d %s %s" % (m, n, k, dtype, out, act, res, pitches, shifts)
+    note(what)
+    xd, wd = placed(x, pitches[0], shifts[0]), placed(w, pitches[1], shifts[1])
+    bd = b.cuda() if bias else None
+    rd = placed(r, pitches[2], shifts[2]) if res else None
+    yd = rd if in_place else placed(torch.full((m, n), NAN, dtype=out), pitches[3], shifts[3], fill=7.0)
+    ld = [p or d for p, d in zip(pitches, (k, k, n, n))]
+    if in_place:
+        ld[3] = ld[2]
+    op = L.make_linear(m, n, k, CODE[dtype], CODE[out], act, res, *ld)
+    ws = torch.full((max(1, L.ct_linear_workspace(op)),), 255, dtype=torch.uint8, device="cuda")
+    L.ct_linear_run(op, xd, wd, bd, rd, yd, ws, stream())
+    torch.cuda.synchronize()
+    x, w = x.double(), w.double()
+    v, mag = x @ w.t(), x.abs() @ w.abs().t()
+    if bias:
+        v, mag = v + b.double(), mag + b.double().abs()
+    if res == L.RES_ADD_ACT:
+        v, mag = v + r.double(), mag + r.double().abs()
+    y = act64(v, act)
+    # the activations' slopes are at most 1.13, their own errors a few units of what goes in
+    bound = 1.13 * (k + 4) * U * mag + 8 * U * v.abs()
+    if res == L.RES_ADD:
+        y = y + r.double()
+        bound = bound + U * y.abs()
+    bound = bound + ROUND[out] * (y.abs() + bound)
+    within(yd, y, bound, what)
+    if not in_place and pitches[3]:
+        flat = yd.as_strided((m, pitches[3] - n), (pitches[3], 1), yd.storage_offset() + n)
+        assert (flat == 7.0).all(), what + ": wrote between the rows"
+
+
+SIZES = [(1, 16, 8), (1, 1, 1), (2, 17, 40), (5, 33, 129), (16, 64, 64), (17, 80, 72), (33, 48, 1000), (64, 64, 512),
+         (65, 129, 96), (100, 200, 300), (128, 256, 64), (257, 255, 136), (300, 520, 2048)]
+
+
+@pytest.mark.parametrize("dtype,out", [(B, B), (B, F), (F, F), (F, B)])
+@pytest.mark.parametrize("m,n,k", SIZES)
+def test_linear_sizes_and_types(m, n, k, dtype, out):
+    check_linear(m, n, k, dtype, out, act=(m + n) % 5, res=k % 3, seed=m * n + k)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("m,n,k", [(3, 24, 50), (24, 1000, 77), (130, 70, 515), (520, 270, 264)])
+@pytest.mark.parametrize("shifts", [(1, 0, 0, 0), (0, 1, 3, 1), (2, 3, 1, 2)])
+def test_linear_strides_and_alignment(m, n, k, dtype, shifts):
+    check_linear(m, n, k, dtype, dtype, act=3, res=1, seed=3, pitches=(k + 7, k + 3, n + 5, n + 1), shifts=shifts)
+    check_linear(m, n, k, dtype, dtype, act=1, res=2, seed=4, pitches=(k // 8 * 8 + 64, k // 8 * 8 + 16, n // 8 * 8 + 8,
+                                                                      n // 8 * 8 + 24), shifts=(8, 16, 8, 24))
+
+
+@pytest.mark.parametrize("act", range(5))
+@pytest.mark.parametrize("res", range(3))
+@pytest.mark.parametrize("bias", [False, True])
+def test_linear_epilogues(act, res, bias):
+    for m, n, k in ((7, 40, 64), (150, 132, 64)):
+        check_linear(m, n, k, B, F, act, res, bias, seed=act)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 320, 8192), (24, 64, 16384), (200, 96, 8192), (256, 256, 12000)])
+def test_linear_long_reductions(m, n, k):
+    check_linear(m, n, k, B, B, L.ACT_SILU, L.RES_ADD, seed=k)
+    check_linear(m, n, k, F, F, L.ACT_NONE, L.RES_ADD_ACT, seed=k + 1)
+
+
+@pytest.mark.parametrize("m,n", [(2049, 1100), (1536, 2560)])
+def test_linear_many_tiles(m, n):
+    check_linear(m, n, 200, B, B, L.ACT_GELU, 0, seed=9)
+    check_linear(m, n, 136, B, F, L.ACT_NONE, L.RES_ADD, bias=False, seed=10)
+
+
+@pytest.mark.parametrize("m,n,k", [(4, 64, 64), (150, 132, 64), (40, 64, 8192)])
+def test_linear_residual_in_place(m, n, k):
+    check_linear(m, n, k, B, B, 0, L.RES_ADD, seed=1, in_place=True)
+    check_linear(m, n, k, F, F, L.ACT_RELU, L.RES_ADD_ACT, seed=2, in_place=True)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+def test_linear_empty_reduction_is_the_epilogue(dtype):
+    for m, n in ((3, 20), (200, 150)):
+        check_linear(m, n, 0, dtype, F, L.ACT_SILU, L.RES_ADD, seed=5, pitches=(8, 8, 0, 0))
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("m,n,k", [(4, 40, 70), (20, 40, 64), (200, 150, 203), (300, 300, 1000)])
+def test_linear_reads_nothing_beyond_rows_and_columns(m, n, k, dtype):
+    # NaN lies between the rows and behind the arrays: any value beyond k would reach an output
+    check_linear(m, n, k, dtype, F, seed=6, pitches=(k + 8 - k % 8 + 8, k + 8 - k % 8 + 24, 0, 0))
+    check_linear(m, n, k, dtype, F, seed=6, pitches=(k + 1, k + 2, 0, 0))
+
+
+def test_linear_nan_and_infinity_stay_in_their_row_and_column():
+    m, n, k = 150, 140, 96
+    g = gen(11)
+    x, w = normal(g, m, k, dtype=B), normal(g, n, k, dtype=B)
+    x[37, 5], w[101, 8] = NAN, float("inf")
+    for act in range(5):
+        op = L.make_linear(m, n, k, L.DT_BF16, L.DT_F32, act)
+        y = torch.empty(m, n, device="cuda")
+        ws = torch.empty(max(1, L.ct_linear_workspace(op)), dtype=torch.uint8, device="cuda")
+        L.ct_linear_run(op, x.cuda(), w.cuda(), None, None, y, ws, stream())
+        ref = act64(x.double() @ w.double().t(), act)
+        got = y.cpu().double()
+        assert torch.isnan(got[37]).all()
+        others = torch.ones(m, n, dtype=torch.bool)
+        others[37] = False
+        others[:, 101] = False
+        assert torch.isfinite(got[others]).all()
+        assert torch.equal(torch.isnan(got), torch.isnan(ref)), act
+        assert torch.equal(torch.isinf(got), torch.isinf(ref)), act
+
+
+# ------------------------------------------------------------------ sequences
+def layout(lens, extra_slots=2, seed=0, unused=(), lead=0, tail=0):
+    """offsets, slots (int32 tensors) and the number of slots; sequences in `unused` have none."""
+    off = lead + np.concatenate([[0], np.cumsum(lens)])
+    n = len(lens) + extra_slots
+    slots = np.random.RandomState(seed).permutation(n)[:len(lens)].astype(np.int32)
+    for k, i in enumerate(unused):
+        slots[i] = (-1, n, 1 << 30, -(1 << 31))[k % 4]
+    return (torch.tensor(off, dtype=torch.int32), torch.from_numpy(slots), n, int(off[-1]) + tail)
+
+
+def conv64(x, w, bias, state, off, slots, act):
+    """y, the new state and the sum of magnitudes, in 64 bits; rows of no sequence are NaN."""
+    W = w.shape[1]
+    y = torch.full(x.shape, NAN, dtype=torch.float64)
+    mag = torch.zeros(x.shape, dtype=torch.float64)
+    new = state.clone()
+    for i, s in enumerate(slots.tolist()):
+        b, e = int(off[i]), int(off[i + 1])
+        has = 0 <= s < state.shape[0]
+        h = state[s] if has else torch.zeros_like(state[0])
+        rows = torch.cat([h, x[b:e]]).double()
+        for t in range(e - b):
+            win = rows[t:t + W]
+            v = (win * w.double().t()).sum(0) + bias.double()
+            mag[b + t] = (win * w.double().t()).abs().sum(0) + bias.double().abs()
+            y[b + t] = act64(v, act)
+        if has:
+            new[s] = rows[-(W - 1):].to(state.dtype)
+    return y, new, mag
+
+
+def check_conv(lens, channels, width, dtype, act=L.ACT_SILU, uniform=False, pitch=0, shift=0, in_place=False,
+               unused=(), lead=0, tail=0, seed=0):
+    what = "conv %s ch%d w%d %s uniform%d pitch%d shift%d" % (lens, channels, width, dtype, uniform, pitch, shift)
+    note(what)
+    g = gen(seed)
+    off, slots, n, tokens = layout(lens, seed=seed, unused=unused, lead=lead, tail=tail)
+    x = normal(g, tokens, channels, dtype=dtype)
+    inside = torch.zeros(tokens, dtype=torch.bool)
+    inside[int(off[0]):int(off[-1])] = True
+    x[~inside] = NAN
+    w, bias = normal(g, channels, width), normal(g, channels)
+    state = normal(g, n, width - 1, channels, dtype=dtype)
+    xd = placed(x, pitch, shift)
+    yd = placed(torch.full((tokens, channels), NAN, dtype=dtype), pitch, shift, fill=7.0)
+    sd = state.cuda()
+    out = sd if in_place else state.cuda()
+    op = L.make_causal_conv(channels, width, CODE[dtype], act, ldx=pitch, ldy=pitch)
+    seqs = L.make_sequences(tokens, len(lens), n, 0 if seed % 2 else max(lens + [0]), None if uniform else off.cuda(), slots.cuda())
+    L.ct_causal_conv_run(op, seqs, xd, w.cuda(), bias.cuda(), sd, out, yd, stream())
+    torch.cuda.synchronize()
+    y, new, mag = conv64(x, w, bias, state, off, slots, act)
+    bound = 1.13 * (width + 3) * U * mag + 8 * U * mag
+    bound = bound + ROUND[dtype] * (y.abs() + bound)
+    assert torch.equal(out.cpu(), new), what + ": state"
+    within(yd, y, bound, what)
+    if pitch > channels:
+        assert (yd.as_strided((tokens, pitch - channels), (pitch, 1), yd.storage_offset() + channels) == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("width", range(2, 9))
+def test_conv_widths_and_short_sequences(width, dtype):
+    check_conv([0, 1, 2, 3, width - 2, width - 1, width, 16, 17, 33, 0], 40, width, dtype, seed=width)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("channels", [1, 7, 64, 65, 520, 1032])
+def test_conv_channels(channels, dtype):
+    check_conv([5, 0, 100, 31], channels, 4, dtype, seed=1)
+    check_conv([1] * 9, channels, 4, dtype, uniform=True, seed=2, unused=(3, 5))
+    check_conv([19] * 3, channels, 3, dtype, uniform=True, act=L.ACT_NONE, seed=3)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("pitch,shift", [(96, 0), (104, 8), (97, 0), (96, 1), (0, 3)])
+def test_conv_strides_and_alignment(pitch, shift, dtype):
+    check_conv([3, 50, 0, 1], 80, 4, dtype, pitch=pitch, shift=shift, seed=4)
+    check_conv([1] * 5, 80, 4, dtype, uniform=True, pitch=pitch, shift=shift, seed=5)
+
+
+@pytest.mark.parametrize("lens", [[40, 3, 0, 2, 129], [1] * 7, [300]])
+def test_conv_state_in_place(lens):
+    check_conv(lens, 72, 4, B, in_place=True, seed=6)
+    check_conv(lens, 72, 4, F, in_place=True, seed=7, uniform=len(set(lens)) == 1)
+
+
+def test_conv_many_sequences_and_rows_of_none():
+    rng = np.random.RandomState(3)
+    lens = [int(v) for v in rng.randint(0, 9, size=5000)]
+    check_conv(lens, 8, 4, F, seed=8, unused=tuple(range(0, 5000, 7)), lead=5, tail=11)
+    check_conv([0] * 70, 16, 4, B, seed=9)
+
+
+def test_conv_without_states_starts_from_zeros():
+    g = gen(1)
+    x, w = normal(g, 37, 24, dtype=B), normal(g, 24, 4)
+    off = torch.tensor([0, 20, 37], dtype=torch.int32)
+    y = torch.empty(37, 24, dtype=B, device="cuda")
+    L.ct_causal_conv_run(L.make_causal_conv(24, 4, L.DT_BF16), L.make_sequences(37, 2, offsets=off.cuda()), x.cuda(),
+                         w.cuda(), None, None, None, y, stream())
+    zero = torch.zeros(2, 3, 24, dtype=B)
+    ref, _, mag = conv64(x, w, torch.zeros(24), zero, off, torch.tensor([0, 1]), 0)
+    within(y, ref, 16 * U * mag + ROUND[B] * (ref.abs() + mag * 16 * U), "conv without states")
+
+
+# ------------------------------------------------------------------ scan
+def scan64(s, off, slots, softplus, dtype):
+    """y, new states and the bounds of both, in 64 bits."""
+    T, D = s["u"].shape
+    N = s["a"].shape[1]
+    G = s["groups"]
+    y, ybound = torch.full((T, D), NAN, dtype=torch.float64), torch.zeros(T, D, dtype=torch.float64)
+    new, nbound = s["state"].double(), torch.zeros(s["state"].shape, dtype=torch.float64)
+    a = s["a"].double()
+    for i, slot in enumerate(slots.tolist()):
+        b, e = int(off[i]), int(off[i + 1])
+        has = 0 <= slot < s["state"].shape[0]
+        h = s["state"][slot].double() if has else torch.zeros(D, N, dtype=torch.float64)
+        err, total = torch.zeros_like(h), torch.zeros(D, dtype=torch.float64)
+        for t in range(b, e):
+            v = s["delta"][t].double() + s["dt_bias"].double()
+            if softplus:
+                dt = torch.clamp(v, min=0) + torch.log1p(torch.exp(-v.abs()))
+                # the sum's rounding and exp's argument move e by 3 |v| u and more, the logarithm and the sum add units
+                rel = (10 + 3 * v.abs()) * U
+            else:
+                dt, rel = v, torch.full_like(v, U)
+            rel = rel + U * (s["delta"][t].double().abs() + s["dt_bias"].double().abs()) / dt.abs().clamp(min=1e-30)
+            total = total + dt.abs()
+            u = s["u"][t].double()
+            bt = s["b"][t].double().reshape(G, N).repeat_interleave(D // G, 0)
+            ct = s["c"][t].double().reshape(G, N).repeat_interleave(D // G, 0)
+            arg = dt[:, None] * a
+            decay, add = torch.exp(arg), (dt * u)[:, None] * bt
+            # the exponent: rounded three times, dt's own error, and sums of steps over many tokens where a
+            # sequence is cut (each of their additions errs by a unit of the sum so far)
+            derr = decay * (4 * U + arg.abs() * (4 * U + rel[:, None]) + (a * total[:, None]).abs() * 2 * U)
+            err = decay * err + derr * (h.abs() + err) + add.abs() * (4 * U + rel[:, None])
+            h = decay * h + add
+            err = err + 2 * U * h.abs()
+            v = (ct * h).sum(1) + s["d"].double() * u
+            ve = (ct.abs() * err).sum(1) + (N + 4) * U * ((ct * h).abs().sum(1) + (s["d"].double() * u).abs())
+            if s["z"] is not None:
+                z = s["z"][t].double()
+                gate = z / (1 + torch.exp(-z))
+                v, ve = v * gate, ve * gate.abs() + (v * gate).abs() * (6 + 3 * z.abs()) * U
+            y[t] = v
+            ybound[t] = ve + ROUND[dtype] * (v.abs() + ve)
+        if has:
+            new[slot], nbound[slot] = h, err
+    return y, new, ybound, nbound
+
+
+def scan_inputs(tokens, channels, states, groups, dtype, slots, seed, z=True):
+    g = gen(seed)
+    return {"groups": groups, "u": normal(g, tokens, channels, dtype=dtype), "delta": normal(g, tokens, channels, dtype=dtype),
+            "dt_bias": normal(g, channels, mean=-3.0), "z": normal(g, tokens, channels, dtype=dtype) if z else None,
+            "a": -(1.0 + torch.arange(states)) * torch.exp(normal(g, channels, states, std=0.3)),
+            "b": normal(g, tokens, groups * states, dtype=dtype), "c": normal(g, tokens, groups * states, dtype=dtype),
+            "d": normal(g, channels), "state": normal(g, slots, channels, states)}
+
+
+def check_scan(lens, channels, states, groups, dtype, uniform=False, z=True, softplus=True, pitch=0, shift=0,
+               in_place=False, unused=(), lead=0, tail=0, seed=0, edit=None):
+    what = "scan %s ch%d n%d g%d %s uniform%d z%d pitch%d shift%d" % (lens, channels, states, groups, dtype, uniform, z,
+                                                                      pitch, shift)
+    note(what)
+    off, slots, n, tokens = layout(lens, seed=seed, unused=unused, lead=lead, tail=tail)
+    s = scan_inputs(tokens, channels, states, groups, dtype, n, seed, z)
+    if edit:
+        edit(s)
+    inside = torch.zeros(tokens, dtype=torch.bool)
+    inside[int(off[0]):int(off[-1])] = True
+    for name in ("u", "delta", "b", "c") + (("z",) if z else ()):
+        s[name][~inside] = NAN
+    gn = groups * states
+    d = {k: placed(s[k], pitch and pitch + 64 * i, shift) for i, k in enumerate(("u", "delta", "b", "c"))}
+    zd = placed(s["z"], pitch and pitch + 8, shift) if z else None
+    yd = placed(torch.full((tokens, channels), NAN, dtype=dtype), pitch, shift, fill=7.0)
+    sd = s["state"].cuda()
+    out = sd if in_place else s["state"].cuda()
+    assert not pitch or pitch >= max(channels, gn)
+    op = L.make_scan(channels, states, groups, CODE[dtype], softplus, *(
+        (pitch and pitch + 64 * i) for i in range(4)), ldz=pitch and pitch + 8, ldy=pitch)
+    seqs = L.make_sequences(tokens, len(lens), n, 0 if seed % 2 else max(lens + [0]), None if uniform else off.cuda(),
+                            slots.cuda())
+    ws = torch.full((max(1, L.ct_scan_workspace(op, seqs)),), 255, dtype=torch.uint8, device="cuda")
+    L.ct_scan_run(op, seqs, d["u"], d["delta"], s["dt_bias"].cuda(), s["a"].cuda(), d["b"], d["c"], s["d"].cuda(), zd, sd,
+                  out, yd, ws, stream())
+    torch.cuda.synchronize()
+    y, new, ybound, nbound = scan64(s, off, slots, softplus, dtype)
+    within(out, new, nbound, what + " state")
+    within(yd, y, ybound, what)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("states", [1, 3, 4, 8, 13, 16, 17, 32, 50, 64, 100, 128, 256])
+def test_scan_states(states, dtype):
+    check_scan([3, 0, 1, 21], 70, states, 1, dtype, seed=states)
+    check_scan([1] * 3, 70, states, 2, dtype, uniform=True, seed=states + 1, unused=(1,))
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("channels,groups", [(1, 1), (5, 5), (64, 1), (65, 1), (96, 3), (130, 2), (512, 4), (1030, 1)])
+def test_scan_channels_and_groups(channels, groups, dtype):
+    check_scan([9, 0, 40], channels, 16, groups, dtype, seed=channels)
+    check_scan([1] * 4, channels, 16, groups, dtype, uniform=True, seed=channels + 1)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("z", [False, True])
+def test_scan_long_and_ragged_prompts(dtype, z):
+    check_scan([700], 66, 16, 1, dtype, z=z, seed=1)
+    check_scan([700], 66, 16, 1, dtype, z=z, seed=2, uniform=True)
+    check_scan([130, 0, 64, 1, 0, 257, 63, 65, 128], 68, 16, 2, dtype, z=z, seed=3, lead=3, tail=70)
+    check_scan([200, 300], 40, 24, 2, dtype, z=z, seed=4)
+    check_scan([260] * 3, 40, 5, 1, dtype, z=z, seed=5, uniform=True)
+
+
+@pytest.mark.parametrize("lens", [[400, 3, 0, 2, 129], [1] * 7, [300]])
+def test_scan_state_in_place(lens):
+    check_scan(lens, 72, 16, 1, B, in_place=True, seed=6)
+    check_scan(lens, 72, 16, 1, F, in_place=True, seed=7, uniform=len(set(lens)) == 1)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("pitch,shift", [(128, 0), (136, 8), (129, 0), (130, 0), (128, 1), (0, 2)])
+def test_scan_strides_and_alignment(pitch, shift, dtype):
+    check_scan([5, 0, 150], 80, 16, 2, dtype, pitch=pitch, shift=shift, seed=8)
+    check_scan([1] * 3, 80, 16, 1, dtype, pitch=pitch, shift=shift, seed=9, uniform=True)
+    check_scan([90], 80, 7, 1, dtype, pitch=pitch, shift=shift, seed=10)
+
+
+def test_scan_many_sequences_and_unused_slots():
+    rng = np.random.RandomState(4)
+    lens = [int(v) for v in rng.randint(0, 6, size=600)]
+    check_scan(lens, 12, 8, 1, F, seed=11, unused=tuple(range(0, 600, 5)), lead=2, tail=3)
+    check_scan([0] * 70, 16, 16, 1, B, seed=12)
+
+
+def test_scan_without_softplus_growth_and_large_steps():
+    def growing(s):  # rates of both signs, steps of both signs
+        s["a"] = s["a"] * torch.where(torch.arange(s["a"].shape[1]) % 3 == 0, -0.05, 0.3)
+        s["dt_bias"] = s["dt_bias"] * 0 + 0.1
+        s["delta"] = (s["delta"].float() * 0.05).to(s["delta"].dtype)
+
+    def forgetting(s):  # decays that underflow
+        s["dt_bias"] = s["dt_bias"] * 0 + 30.0
+
+    def frozen(s):  # steps far below 2^-24
+        s["dt_bias"] = s["dt_bias"] * 0 - 40.0
+
+    for edit, softplus in ((growing, False), (forgetting, True), (frozen, True)):
+        check_scan([150, 3], 66, 16, 1, F, softplus=softplus, seed=13, edit=edit)
+
+
+def test_scan_nan_stays_in_its_sequence_and_channel():
+    def plant(s):
+        s["u"][40, 7] = NAN
+        s["state"][:, 9, 2] = float("inf")
+    off, slots, n, tokens = layout([30, 100, 30], seed=14)
+    s = scan_inputs(tokens, 70, 16, 1, F, n, 14)
+    plant(s)
+    op = L.make_scan(70, 16, 1, L.DT_F32)
+    seqs = L.make_sequences(tokens, 3, n, 0, off.cuda(), slots.cuda())
+    ws = torch.empty(max(1, L.ct_scan_workspace(op, seqs)), dtype=torch.uint8, device="cuda")
+    y = torch.empty(tokens, 70, device="cuda")
+    out = torch.zeros_like(s["state"]).cuda()
+    c = {k: v.cuda() for k, v in s.items() if k != "groups"}
+    L.ct_scan_run(op, seqs, c["u"], c["delta"], c["dt_bias"], c["a"], c["b"], c["c"], c["d"], c["z"], c["state"], out, y,
+                  ws, stream())
+    y = y.cpu()
+    bad = ~torch.isfinite(y)
+    expected = torch.zeros(tokens, 70, dtype=torch.bool)
+    expected[40:130, 7] = True  # from the planted token to its sequence's end
+    assert not bad[:, [i for i in range(70) if i not in (7, 9)]].any()
+    assert torch.equal(bad[:, 7], expected[:, 7])
+    assert bad[0, 9] and bad[30, 9] and bad[130, 9]
+
+
+# ------------------------------------------------------------------ streams, graphs, repeats, addresses
+def test_prompt_then_tokens_equal_one_longer_prompt():
+    """Splitting a sequence over calls changes neither the convolution's bits nor, within its bound, the scan."""
+    tokens, cut, ch = 300, 260, 72
+    s = scan_inputs(tokens, ch, 16, 1, B, 1, 20)
+    c = {k: v.cuda() for k, v in s.items() if k != "groups"}
+    w, bias = normal(gen(1), ch, 4).cuda(), normal(gen(2), ch).cuda()
+    conv, scan = L.make_causal_conv(ch, 4, L.DT_BF16, L.ACT_SILU), L.make_scan(ch, 16, 1, L.DT_BF16)
+
+    def run(pieces):
+        hist, h = torch.zeros(1, 3, ch, dtype=B, device="cuda"), torch.zeros(1, ch, 16, device="cuda")
+        x, y = torch.empty(tokens, ch, dtype=B, device="cuda"), torch.empty(tokens, ch, dtype=B, device="cuda")
+        at = 0
+        for n in pieces:
+            q = L.make_sequences(n, 1, 1)
+            ws = torch.empty(max(1, L.ct_scan_workspace(scan, q)), dtype=torch.uint8, device="cuda")
+            r = slice(at, at + n)
+            L.ct_causal_conv_run(conv, q, c["u"][r], w, bias, hist, hist, x[r], stream())
+            L.ct_scan_run(scan, q, x[r], c["delta"][r], c["dt_bias"], c["a"], c["b"][r], c["c"][r], c["d"], c["z"][r], h,
+                          h, y[r], ws, stream())
+            at += n
+        return x, y, h
+
+    x1, y1, h1 = run([tokens])
+    x2, y2, h2 = run([cut] + [1] * (tokens - cut))
+    assert torch.equal(x1, x2)
+    s["u"] = x1.cpu()
+    s["state"] = torch.zeros(1, ch, 16)
+    y, new, ybound, nbound = scan64(s, torch.tensor([0, tokens]), torch.tensor([0]), True, B)
+    for yy, hh in ((y1, h1), (y2, h2)):
+        within(yy, y, ybound, "prompt and tokens")
+        within(hh, new, nbound, "prompt and tokens: state")
+
+
+def _block_calls(seed):
+    """The three operators on one set of inputs, as a function that enqueues them on a stream, and its outputs."""
+    s = scan_inputs(500, 136, 16, 1, B, 4, seed)
+    c = {k: v.cuda() for k, v in s.items() if k != "groups"}
+    off, slots = torch.tensor([0, 350, 350, 500], dtype=torch.int32).cuda(), torch.tensor([2, 0, 3], dtype=torch.int32).cuda()
+    seqs = L.make_sequences(500, 3, 4, 0, off, slots)
+    g = gen(seed + 1)
+    w, hist = normal(g, 136, 4).cuda(), normal(g, 4, 3, 136, dtype=B).cuda()
+    wl = normal(g, 64, 136, dtype=B).cuda()
+    wide = normal(g, 80, 8192, dtype=B).cuda()
+    xw = normal(g, 24, 8192, dtype=B).cuda()
+    conv, scan = L.make_causal_conv(136, 4, L.DT_BF16, L.ACT_SILU), L.make_scan(136, 16, 1, L.DT_BF16)
+    lin, long = L.make_linear(500, 64, 136, L.DT_BF16, L.DT_F32), L.make_linear(24, 80, 8192, L.DT_BF16, L.DT_F32)
+    ws = [torch.empty(max(1, n), dtype=torch.uint8, device="cuda") for n in (
+        L.ct_scan_workspace(scan, seqs), L.ct_linear_workspace(lin), L.ct_linear_workspace(long))]
+    outs = {"x": torch.empty_like(c["u"]), "y": torch.empty_like(c["u"]), "h": torch.zeros_like(c["state"]),
+            "hist": torch.zeros_like(hist), "p": torch.empty(500, 64, device="cuda"), "q": torch.empty(24, 80, device="cuda")}
+
+    def calls(st):
+        L.ct_causal_conv_run(conv, seqs, c["u"], w, None, hist, outs["hist"], outs["x"], st)
+        L.ct_scan_run(scan, seqs, outs["x"], c["delta"], c["dt_bias"], c["a"], c["b"], c["c"], c["d"], c["z"], c["state"],
+                      outs["h"], outs["y"], ws[0], st)
+        L.ct_linear_run(lin, outs["y"], wl, None, None, outs["p"], ws[1], st)
+        L.ct_linear_run(long, xw, wide, None, None, outs["q"], ws[2], st)
+
+    return calls, outs
+
+
+def test_results_are_the_same_bits_on_every_run_and_stream():
+    calls, outs = _block_calls(30)
+    calls(stream())
+    torch.cuda.synchronize()
+    first = {k: v.clone() for k, v in outs.items()}
+    side = torch.cuda.Stream()
+    for st in (side.cuda_stream, 0, side.cuda_stream):
+        for v in outs.values():
+            v.zero_()
+        torch.cuda.synchronize()
+        calls(st)
+        torch.cuda.synchronize()
+        for k in outs:
+            assert torch.equal(outs[k], first[k]), k
+
+
+def test_capture_and_replay():
+    calls, outs = _block_calls(31)
+    calls(stream())
+    torch.cuda.synchronize()
+    first = {k: v.clone() for k, v in outs.items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls(stream())
+    for _ in range(4):
+        for v in outs.values():
+            v.fill_(3)
+        (torch.ones(1000, device="cuda") * 2).sum().item()
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in outs:
+            if k in ("h", "hist"):  # the slot of no sequence keeps what was there
+                assert torch.equal(outs[k][[2, 0, 3]], first[k][[2, 0, 3]]), k
+            else:
+                assert torch.equal(outs[k], first[k]), k
+
+
+def test_offsets_beyond_32_bits():
+    """Rows, and slots of the state arrays, past 2^31 elements and 2^32 bytes."""
+    ch, pitch, rows = 64, 1 << 20, 4200  # 8.8 GB of bf16 rows
+    big = torch.empty(rows * pitch, dtype=B, device="cuda")
+    x = big.view(rows, pitch)[:, :ch]
+    g = gen(40)
+    xs = normal(g, rows, ch, dtype=B)
+    x.copy_(xs)
+    w = normal(g, ch, 4)
+    slots = (1 << 32) // (ch * 16) + 10  # 17 GB of states
+    hist = torch.empty(slots, 3, ch, dtype=B, device="cuda")
+    state = torch.empty(slots, ch, 16, device="cuda")
+    hist[slots - 2] = 0
+    state[slots - 2] = 0
+    at = torch.tensor([slots - 2], dtype=torch.int32).cuda()
+    seqs = L.make_sequences(rows, 1, slots, 0, None, at)
+    note("conv over rows past 2^32 bytes")
+    y = torch.empty(rows, ch, dtype=B, device="cuda")
+    L.ct_causal_conv_run(L.make_causal_conv(ch, 4, L.DT_BF16, 0, ldx=pitch), seqs, x, w.cuda(), None, hist, hist, y, stream())
+    ref, new, mag = conv64(xs, w, torch.zeros(ch), torch.zeros(1, 3, ch, dtype=B), torch.tensor([0, rows]), torch.tensor([0]), 0)
+    within(y, ref, 16 * U * mag + ROUND[B] * (ref.abs() + 16 * U * mag), "conv past 32 bits")
+    assert torch.equal(hist[slots - 2].cpu(), new[0])
+    note("scan over rows and slots past 2^32")
+    s = scan_inputs(rows, ch, 16, 1, B, 1, 41, z=False)
+    s["u"], s["state"] = xs, torch.zeros(1, ch, 16)
+    c = {k: v.cuda() for k, v in s.items() if k not in ("groups", "z", "u")}
+    scan = L.make_scan(ch, 16, 1, L.DT_BF16, ldu=pitch)
+    ws = torch.empty(max(1, L.ct_scan_workspace(scan, seqs)), dtype=torch.uint8, device="cuda")
+    L.ct_scan_run(scan, seqs, x, c["delta"], c["dt_bias"], c["a"], c["b"], c["c"], c["d"], None, state, state, y, ws, stream())
+    y64, new, ybound, nbound = scan64(s, torch.tensor([0, rows]), torch.tensor([0]), True, B)
+    within(y, y64, ybound, "scan past 32 bits")
+    within(state[slots - 2].unsqueeze(0), new, nbound, "scan past 32 bits: state")
+    note("product over rows past 2^32 bytes")
+    wl = normal(g, 48, ch, dtype=B)
+    out = torch.empty(rows, 48, device="cuda")
+    for m, r0 in ((rows, 0), (5, rows - 5)):
+        op = L.make_linear(m, 48, ch, L.DT_BF16, L.DT_F32, ldx=pitch)
+        ws = torch.empty(max(1, L.ct_linear_workspace(op)), dtype=torch.uint8, device="cuda")
+        L.ct_linear_run(op, x[r0:], wl.cuda(), None, None, out, ws, stream())
+        a, b = xs[r0:].double(), wl.double()
+        within(out[:m], a @ b.t(), (ch + 4) * U * (a.abs() @ b.abs().t()), "product past 32 bits")
