@@ -7,7 +7,15 @@
 
 namespace ct {
 
-typedef __bf16 bf16_t;
+// A bf16 in memory. Arithmetic is in fp32; a result is rounded to nearest even.
+struct bf16_t {
+  unsigned short bits;
+  bf16_t() = default;
+  __device__ __forceinline__ explicit bf16_t(float v) : bits(__builtin_bit_cast(unsigned short, (__bf16)v)) {}
+  __device__ __forceinline__ explicit operator float() const {
+    return __builtin_bit_cast(float, (unsigned)bits << 16);
+  }
+};
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Refuses a launch of more waves or blocks than the kernels' 31-bit numbers can name.

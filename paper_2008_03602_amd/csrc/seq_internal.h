@@ -28,7 +28,9 @@ struct SeqView {
 
 // ---- ct_linear ----
 struct LinearPlan {
-  int split;          // partial sums of the reduction
+  int kind;           // the kernel (k_linear.hip)
+  int split;          // slices of the reduction, each with partial sums of its own
+  int per_split;      // 128-byte chunks of a row in a slice
   int64_t ws_floats;  // split * m * n where the reduction is split
 };
 LinearPlan plan_linear(const ct_linear_op& op);
