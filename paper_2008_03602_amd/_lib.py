@@ -172,6 +172,8 @@ _lib = None
 def lib():
     """The loaded library (built in-tree by ``paper_2008_03602_amd.build``)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -201,11 +203,7 @@ def _arr(a, ctype):
 
 def _ptr(t) -> int:
     """Device address of a torch tensor (or an int address)."""
-    if t is None:
-        return None
-    if isinstance(t, int):
-        return t
-    return t.data_ptr()
+    return t if t is None or t.__class__ is int else t.data_ptr()
 
 
 # ---------------------------------------------------------------- structs

@@ -23,7 +23,7 @@ struct LinearArgs {
   int act, res_mode, out_bf16;
   int vec_out;          // rows of y and r take accesses of four elements
   int tiles_m, tiles_n;
-  int split, per_split; // slices of the reduction, 128-byte chunks in each
+  int split, per_split; // slices of the reduction, elements in each (whole 128-byte chunks)
   FastDiv dgroup, dlast;
 };
 
@@ -47,47 +47,86 @@ __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 acc) {
 }
 
 // ------------------------------------------------------------------ epilogue
-__device__ __forceinline__ float finish(const LinearArgs& a, float v, float bias, float r) {
-  v += bias;
-  if (a.res_mode == CT_RES_ADD_ACT) v += r;
-  v = activate(v, a.act);
-  if (a.res_mode == CT_RES_ADD) v += r;
-  return v;
+struct Quad {
+  float v[4];
+};
+// Four elements of a row that all exist, at an address for them in one access.
+template <typename O>
+__device__ __forceinline__ Quad load_quad4(const O* p) {
+  if constexpr (sizeof(O) == 2) {
+    const u32x2 q = *(const u32x2*)p;
+    const unsigned q0 = q.x, q1 = q.y;
+    return {unpack<O>(q0, 0), unpack<O>(q0, 1), unpack<O>(q1, 0), unpack<O>(q1, 1)};
+  } else {
+    const f32x4 q = *(const f32x4*)p;
+    return {q.x, q.y, q.z, q.w};
+  }
+}
+template <typename O>
+__device__ __forceinline__ void store_quad4(O* p, const float* v) {
+  if constexpr (sizeof(O) == 2) *(u32x2*)p = (u32x2){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  else *(f32x4*)p = (f32x4){v[0], v[1], v[2], v[3]};
+}
+// Four columns of the bias, and of a row of the residual, from column j on: 0 where there
+// are none.
+__device__ __forceinline__ Quad load_bias(const LinearArgs& a, int j) {
+  Quad q = {};
+  if (!a.bias || j >= a.n) return q;
+  if (a.vec_out && j + 4 <= a.n) {
+    const f32x4 b = *(const f32x4*)(a.bias + j);
+    return {b.x, b.y, b.z, b.w};
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (j + e < a.n) q.v[e] = a.bias[j + e];
+  return q;
+}
+__device__ __forceinline__ Quad load_res(const LinearArgs& a, int i, int j) {
+  Quad q = {};
+  if (!a.res_mode || i >= a.m || j >= a.n) return q;
+  const int64_t at = i * a.ldr + j;
+  if (a.vec_out && j + 4 <= a.n)
+    return a.out_bf16 ? load_quad4((const bf16_t*)a.res + at) : load_quad4((const float*)a.res + at);
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (j + e < a.n) q.v[e] = a.out_bf16 ? (float)((const bf16_t*)a.res)[at + e] : ((const float*)a.res)[at + e];
+  return q;
+}
+// N quads of outputs from their sums, one choice of the activation for all of them.
+template <int N>
+__device__ __forceinline__ void finish(const LinearArgs& a, float (&v)[N][4], const Quad& bias, const Quad (&res)[N]) {
+  auto each = [&](auto f) __attribute__((always_inline)) {
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[q][e] = f(v[q][e], q, e);
+  };
+  each([&](float x, int, int e) { return x + bias.v[e]; });
+  if (a.res_mode == CT_RES_ADD_ACT) each([&](float x, int q, int e) { return x + res[q].v[e]; });
+  switch (a.act) {
+    case CT_ACT_RELU: each([](float x, int, int) { return activate(x, CT_ACT_RELU); }); break;
+    case CT_ACT_RELU6: each([](float x, int, int) { return activate(x, CT_ACT_RELU6); }); break;
+    case CT_ACT_SILU: each([](float x, int, int) { return activate(x, CT_ACT_SILU); }); break;
+    case CT_ACT_GELU: each([](float x, int, int) { return activate(x, CT_ACT_GELU); }); break;
+  }
+  if (a.res_mode == CT_RES_ADD) each([&](float x, int q, int e) { return x + res[q].v[e]; });
 }
 // Outputs (i, j .. j+3), those of them that exist.
-__device__ __forceinline__ void store4(const LinearArgs& a, int i, int j, f32x4 acc) {
-  float v[4] = {acc[0], acc[1], acc[2], acc[3]};
-  const int64_t at = i * a.ldy + j, rt = i * a.ldr + j;
+__device__ __forceinline__ void store4(const LinearArgs& a, int i, int j, f32x4 acc, const Quad& bias, const Quad& r) {
+  float v[1][4] = {{acc.x, acc.y, acc.z, acc.w}};
+  const Quad res[1] = {r};
+  finish(a, v, bias, res);
+  const int64_t at = i * a.ldy + j;
   if (a.vec_out && j + 4 <= a.n) {
-    f32x4 b = {}, r = {};
-    if (a.bias) b = *(const f32x4*)(a.bias + j);
-    if (a.res_mode) {
-      if (a.out_bf16) {
-        const u32x2 q = *(const u32x2*)((const bf16_t*)a.res + rt);
-        const unsigned q0 = q.x, q1 = q.y;
-        r = (f32x4){unpack<bf16_t>(q0, 0), unpack<bf16_t>(q0, 1), unpack<bf16_t>(q1, 0), unpack<bf16_t>(q1, 1)};
-      } else {
-        r = *(const f32x4*)((const float*)a.res + rt);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const float be = b[e], re = r[e];
-      v[e] = finish(a, v[e], be, re);
-    }
-    if (a.out_bf16) *(u32x2*)((bf16_t*)a.y + at) = (u32x2){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-    else *(f32x4*)((float*)a.y + at) = (f32x4){v[0], v[1], v[2], v[3]};
+    if (a.out_bf16) store_quad4((bf16_t*)a.y + at, v[0]);
+    else store_quad4((float*)a.y + at, v[0]);
     return;
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     if (j + e >= a.n) break;
-    float r = 0.f;
-    if (a.res_mode)
-      r = a.out_bf16 ? (float)((const bf16_t*)a.res)[rt + e] : ((const float*)a.res)[rt + e];
-    const float out = finish(a, v[e], a.bias ? a.bias[j + e] : 0.f, r);
-    if (a.out_bf16) ((bf16_t*)a.y)[at + e] = (bf16_t)out;
-    else ((float*)a.y)[at + e] = out;
+    if (a.out_bf16) ((bf16_t*)a.y)[at + e] = (bf16_t)v[0][e];
+    else ((float*)a.y)[at + e] = v[0][e];
   }
 }
 // Partial sums of slice sp: rows of n rounded up to four.
@@ -102,9 +141,16 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs a) {
   if (q >= (int64_t)a.m * n4) return;
   const int i = (int)(q / n4), j = (int)(q - (int64_t)i * n4) * 4;
   const float* p = a.ws + q * 4;
-  f32x4 v = *(const f32x4*)p;
-  for (int s = 1; s < a.split; ++s) v += *(const f32x4*)(p + (int64_t)s * a.m * n4 * 4);
-  store4(a, i, j, v);
+  const Quad bias = load_bias(a, j), res = load_res(a, i, j);
+  f32x4 v = {}, part[4];
+  for (int s = 0; s < a.split; s += 4) {  // four slices in flight
+#pragma unroll
+    for (int e = 0; e < 4; ++e) part[e] = *(const f32x4*)(p + (int64_t)min(s + e, a.split - 1) * a.m * n4 * 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (s + e < a.split) v += part[e];
+  }
+  store4(a, i, j, v, bias, res);
 }
 
 // ------------------------------------------------------------------ 16-byte groups of rows
@@ -114,28 +160,30 @@ constexpr unsigned kOobGroup = 0xFFFFFFF0u;
 __device__ __forceinline__ u32x4 load_quad(__amdgpu_buffer_rsrc_t r, unsigned off) {
   return __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0);
 }
-// A group at any element's address, of which the first `left` elements exist: whole words
-// around it, shifted where it starts in the middle of one, the rest masked to 0.
+// A group at any element's address: the words around it, and, once they have arrived, the
+// group itself, shifted where it starts in the middle of a word, with all but its first
+// `left` elements masked to 0.
 template <typename T>
-__device__ __forceinline__ u32x4 load_quad_any(__amdgpu_buffer_rsrc_t r, unsigned off, int left) {
-  if constexpr (sizeof(T) == 4) {
-    const u32x4 q = load_quad(r, off);
-    const unsigned a = q.x, b = q.y, c = q.z, d = q.w;
-    return (u32x4){left > 0 ? a : 0, left > 1 ? b : 0, left > 2 ? c : 0, left > 3 ? d : 0};
-  } else {
-    const unsigned at = off & ~3u;
-    const u32x4 q = load_quad(r, at);
-    const unsigned e = __builtin_amdgcn_raw_buffer_load_b32(r, (int)(at + 16), 0, 0);
-    unsigned v[5] = {q.x, q.y, q.z, q.w, e};
-    const unsigned sh = (off & 2u) * 8;
+struct RawQuad {
+  u32x4 q;
+  unsigned next;  // the fifth word of a group of bf16
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, unsigned off) {
+    q = load_quad(r, off & ~3u);
+    if constexpr (sizeof(T) == 2) next = __builtin_amdgcn_raw_buffer_load_b32(r, (int)((off & ~3u) + 16), 0, 0);
+  }
+  __device__ __forceinline__ u32x4 get(unsigned off, int left) const {
+    unsigned v[5] = {q.x, q.y, q.z, q.w, next};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[i] = __builtin_amdgcn_alignbit(v[i + 1], v[i], sh);
-      v[i] = left > 2 * i + 1 ? v[i] : left > 2 * i ? v[i] & 0xFFFFu : 0;
-    }
+    for (int i = 0; i < 4; ++i)
+      if constexpr (sizeof(T) == 4) {
+        v[i] = left > i ? v[i] : 0;
+      } else {
+        v[i] = __builtin_amdgcn_alignbit(v[i + 1], v[i], (off & 2u) * 8);
+        v[i] = left > 2 * i + 1 ? v[i] : left > 2 * i ? v[i] & 0xFFFFu : 0;
+      }
     return (u32x4){v[0], v[1], v[2], v[3]};
   }
-}
+};
 // The rows of an operand from row r0 on (at most `most` of `rows`): base on a word, bytes up
 // to the end of the last row in whole words. odd: 2 where the first row starts in the middle
 // of a word.
@@ -153,14 +201,18 @@ __device__ __forceinline__ RowsView rows_view(const void* p, int64_t ld, int r0,
 }
 
 // ------------------------------------------------------------------ tiles
-// A block computes BM x BN outputs with WM x WN waves. Operand slices of 128 bytes of each
-// row go through two LDS stages; the 16-byte groups of a row are permuted by its number, so
-// that the 16 rows of a fragment lie in distinct banks.
-template <typename T, int BM, int BN, int WM, int WN, bool DIRECT>
-__global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(LinearArgs a) {
-  constexpr int WAVES = WM * WN, ROWS = BM + BN, G = 16 / (int)sizeof(T), KC = 8 * G;
-  constexpr int NC = ROWS / 8 / WAVES, NW = BN / 8 / WAVES;  // copies of a wave, those of w first
-  constexpr int TM = BM / WM / 16, TN = BN / WN / 16, STAGE = ROWS * 128;
+// A block computes BM x BN outputs with WK teams of WM x WN waves, each team every WK-th
+// slice of 128 bytes of each operand row: where the tile is small, a slice's products take
+// less time than the waits around them. Slices go through STAGES buffers in LDS, the later
+// ones in flight while one is multiplied; the 16-byte groups of a row are permuted by its
+// number, so that the 16 rows of a fragment lie in distinct banks.
+template <typename T, int BM, int BN, int WM, int WN, int WK, int STAGES, bool DIRECT>
+__global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearArgs a) {
+  constexpr int WAVES = WM * WN, ROWS = BM + BN, G = 16 / (int)sizeof(T), ROWB = 128, NG = ROWB / 16;
+  constexpr int KC = NG * G, RPC = 64 / NG;  // elements of a slice, rows of one copy
+  constexpr int NC = ROWS / RPC / WAVES, NW = BN / RPC / WAVES;  // copies of a wave, those of w first
+  constexpr int TM = BM / WM / 16, TN = BN / WN / 16, STAGE = WK * ROWS * ROWB;
+  static_assert(BN % (RPC * WAVES) == 0 && BM % (RPC * WAVES) == 0, "every wave copies as many rows");
   extern __shared__ __align__(16) char lds[];
 
   // Each XCD takes one band of tiles, in columns four tiles wide: the tiles at work on it
@@ -176,63 +228,70 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(LinearArgs a)
     ni = grp * 4 + in - mi * a.dlast.d;
   }
   const int m0 = mi * BM, n0 = ni * BN, sp = (int)blockIdx.y;
-  const int lane = (int)threadIdx.x & 63, wave = wave_id();
-  const int c0 = sp * a.per_split, chunks = min((a.k + KC - 1) / KC - c0, a.per_split);
+  const int lane = (int)threadIdx.x & 63, team = wave_id() / WAVES, wave = wave_id() % WAVES;
+  const int k_begin = sp * a.per_split, k_end = min(a.k, k_begin + a.per_split);
+  const int chunks = (k_end - k_begin + WK * KC - 1) / (WK * KC);  // slices of a team
 
   const RowsView vw = rows_view<T>(a.w, a.ldw, n0, a.n, BN, a.k), vx = rows_view<T>(a.x, a.ldx, m0, a.m, BM, a.k);
   const __amdgpu_buffer_rsrc_t rw = make_rsrc(vw.base, vw.bytes), rx = make_rsrc(vx.base, vx.bytes);
-  unsigned off[NC];  // of this lane's group in each copy: eight rows of eight groups
-  int grp_k[NC];     // its first element in the slice
+  unsigned off[NC];  // of this lane's group in each copy
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
-    const int r = ((i < NW ? i : i - NW) * WAVES + wave) * 8 + (lane >> 3);
-    const int g = (lane & 7) ^ ((r >> 1) & 7);
-    grp_k[i] = g * G;
+    const int r = ((i < NW ? i : i - NW) * WAVES + wave) * RPC + lane / NG;
+    const int g = (lane % NG) ^ ((r >> 1) & (NG - 1));
     const bool ok = i < NW ? n0 + r < a.n : m0 + r < a.m;
     const unsigned ld = (unsigned)((i < NW ? a.ldw : a.ldx) * (int)sizeof(T));
     off[i] = ok ? (unsigned)r * ld + 16u * g + (i < NW ? vw.odd : vx.odd) : kOobGroup;
   }
+  // first element of the lane's group in copy i: rows of copies differ by multiples of 8 or 16
+  const int grp_k = ((lane % NG) ^ (((wave * RPC + lane / NG) >> 1) & (NG - 1))) * G;
+  static_assert((WAVES * RPC >> 1) % NG == 0, "every copy of a lane has the same group");
 
-  u32x4 held[DIRECT ? 1 : NC];
+  constexpr int RING = DIRECT ? 1 : NC <= 4 ? 4 : 2;  // slices on their way through registers
+  RawQuad<T> held[RING][DIRECT ? 1 : NC];
   auto fetch = [&](int c, int stage) __attribute__((always_inline)) {
-    const int k0 = (c0 + c) * KC;
-    const bool tail = k0 + KC > a.k;
-    char* dst = lds + stage * STAGE + wave * 1024;
+    const int k0 = k_begin + (c * WK + team) * KC;
+    const int left = k_end - k0 - grp_k;  // elements from the lane's group on
+    char* dst = lds + stage * STAGE + team * ROWS * ROWB + wave * 1024;
+    auto go = [&](auto tail) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < NC; ++i) {
-      const int left = a.k - k0 - grp_k[i];
-      if constexpr (DIRECT) {
-        const unsigned o = tail && left <= 0 ? kOobGroup : off[i];
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(i < NW ? rw : rx, (lds_void_t*)(dst + i * WAVES * 1024), 16, (int)o,
-                                                 k0 * (int)sizeof(T), 0, 0);
-      } else {
-        const unsigned o = off[i] == kOobGroup || left <= 0 ? kOobGroup : off[i] + (unsigned)(k0 * (int)sizeof(T));
-        held[i] = load_quad_any<T>(i < NW ? rw : rx, o, left);
+      for (int i = 0; i < NC; ++i) {
+        if constexpr (DIRECT) {
+          const unsigned o = tail.value && left <= 0 ? kOobGroup : off[i];
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(i < NW ? rw : rx, (lds_void_t*)(dst + i * WAVES * 1024), 16, (int)o,
+                                                   k0 * (int)sizeof(T), 0, 0);
+        } else {
+          const unsigned o = off[i] == kOobGroup || left <= 0 ? kOobGroup : off[i] + (unsigned)(k0 * (int)sizeof(T));
+          held[stage][i].load(i < NW ? rw : rx, o);
+        }
       }
-    }
+    };
+    if (k0 + KC <= k_end) go(std::false_type{});
+    else go(std::true_type{});
   };
-  auto put = [&](int stage) __attribute__((always_inline)) {
-    if constexpr (!DIRECT) {
+  auto put = [&](int c, int u) __attribute__((always_inline)) {
+    const int left = k_end - (k_begin + (c * WK + team) * KC) - grp_k;
 #pragma unroll
-      for (int i = 0; i < NC; ++i) *(u32x4*)(lds + stage * STAGE + (i * WAVES + wave) * 1024 + lane * 16) = held[i];
-    }
+    for (int i = 0; i < NC; ++i)
+      if constexpr (!DIRECT)
+        *(u32x4*)(lds + (u & 1) * STAGE + team * ROWS * ROWB + (i * WAVES + wave) * 1024 + lane * 16) = held[u][i].get(off[i], left);
   };
 
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
   const int lrow = lane & 15, kg = lane >> 4;
-  const int at0 = lrow * 128 + ((kg ^ (lrow >> 1)) * 16), at1 = at0 ^ 64;  // the slice's halves
+  const int at0 = lrow * ROWB + (((kg ^ (lrow >> 1)) & (NG - 1)) * 16);  // the slice's first half
   f32x4 acc[TN][TM] = {};
   auto multiply = [&](int stage) __attribute__((always_inline)) {
-    const char* sw = lds + stage * STAGE + wn * 128;
-    const char* sx = lds + stage * STAGE + (BN + wm) * 128;
+    const char* sw = lds + stage * STAGE + (team * ROWS + wn) * ROWB;
+    const char* sx = sw + (BN + wm - wn) * ROWB;
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int at = s ? at1 : at0;
+    for (int s = 0; s < NG / 4; ++s) {
+      const int at = s ? at0 ^ 64 : at0;
       u32x4 fw[TN], fx[TM];
 #pragma unroll
-      for (int i = 0; i < TN; ++i) fw[i] = *(const u32x4*)(sw + at + i * 2048);
+      for (int i = 0; i < TN; ++i) fw[i] = *(const u32x4*)(sw + at + i * 16 * ROWB);
 #pragma unroll
-      for (int j = 0; j < TM; ++j) fx[j] = *(const u32x4*)(sx + at + j * 2048);
+      for (int j = 0; j < TM; ++j) fx[j] = *(const u32x4*)(sx + at + j * 16 * ROWB);
 #pragma unroll
       for (int j = 0; j < TM; ++j)
 #pragma unroll
@@ -240,24 +299,100 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(LinearArgs a)
     }
   };
 
-  if (chunks > 0) {
-    fetch(0, 0);
-    put(0);
-    __syncthreads();
-    for (int c = 0; c < chunks; ++c) {
-      if (c + 1 < chunks) fetch(c + 1, (c + 1) & 1);
-      multiply(c & 1);
-      if (c + 1 < chunks) put((c + 1) & 1);
-      __syncthreads();
+  if constexpr (DIRECT) {
+    // Slices past the end read 0, so that STAGES - 1 of them are in flight at every wait. The
+    // barrier also says that every wave has read the stage that is filled next.
+    if (chunks > 0) {
+#pragma unroll
+      for (int c = 0; c < STAGES - 1; ++c) fetch(c, c);
+      int stage = 0;
+      for (int c = 0; c < chunks; ++c) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(NC * (STAGES - 2)) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        fetch(c + STAGES - 1, stage ? stage - 1 : STAGES - 1);
+        multiply(stage);
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
+      }
+    }
+  } else {
+    // The barrier of a slice says that every wave has read the one before it, whose stage the
+    // next slice goes to.
+    static_assert(DIRECT || (STAGES == 2 && RING % 2 == 0), "");
+#pragma unroll
+    for (int u = 0; u < RING; ++u) fetch(u, u);
+    for (int c = 0; c < chunks; c += RING) {
+#pragma unroll
+      for (int u = 0; u < RING; ++u) {
+        if (c + u >= chunks) break;
+        put(c + u, u);
+        __syncthreads();
+        fetch(c + u + RING, u);
+        multiply(u & 1);
+      }
     }
   }
 
   // The sums go through the wave's share of LDS, as many rows of its tile at a time as it
   // holds, so that each access to y and r takes whole rows of the tile.
   constexpr int RM = BM / WM, RN = BN / WN, SLOTS = RN / 4;  // 16-byte slots of a row
-  constexpr int FIT = 2 * STAGE / WAVES / (RN * 4), H = FIT < RM ? FIT : RM;
+  constexpr int FIT = STAGES * STAGE / WK / WAVES / (RN * 4) / 16 * 16, H = FIT < RM ? FIT : RM;
+  constexpr int STEP = 64 / SLOTS;  // rows of one access
+  static_assert(RM % H == 0, "");
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // slices past the end, too
+  __syncthreads();
+  if constexpr (WK > 1) {  // the teams' sums, added in their order by the first
+    constexpr int SUMS = BM * BN * 4;
+    static_assert(WK * SUMS <= STAGES * STAGE && H == RM, "");
+    if (team > 0) {
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j)
+          *(f32x4*)(lds + team * SUMS + ((wave * TN + i) * TM + j) * 1024 + lane * 16) = acc[i][j];
+    }
+    __syncthreads();
+    if (team > 0) return;
+#pragma unroll
+    for (int t = 1; t < WK; ++t)
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j)
+          acc[i][j] += *(const f32x4*)(lds + t * SUMS + ((wave * TN + i) * TM + j) * 1024 + lane * 16);
+  }
   char* mine = lds + wave * (H * RN * 4);
-  auto slot = [](int r, int s) { return (s ^ ((SLOTS == 16 ? r : r >> 1) & (SLOTS - 1))) * 16; };
+  auto slot = [](int r, int s) { return (s ^ ((SLOTS >= 16 ? r : r >> 1) & (SLOTS - 1))) * 16; };
+  const int sl = lane % SLOTS, col = n0 + wn + sl * 4, r0 = lane / SLOTS;
+  const bool whole = a.vec_out && m0 + BM <= a.m && n0 + BN <= a.n;  // no output of the tile is missing
+  const Quad bias = a.split > 1 ? Quad{} : load_bias(a, col);
+  constexpr int ROWS_EACH = H / STEP, Q = ROWS_EACH % 4 ? ROWS_EACH : 4;  // rows of a lane, and at a time
+  auto take = [&](int r) { return *(const f32x4*)(mine + r * RN * 4 + slot(r, sl)); };
+  auto finish_rows = [&](int h, auto zero) __attribute__((always_inline)) {
+    using O = decltype(zero);
+    const int64_t row = m0 + wm + h + r0;
+    O* y = (O*)a.y + row * a.ldy + col;
+    const O* rp = (const O*)a.res + row * a.ldr + col;
+#pragma unroll 1
+    for (int r = r0; r < H; r += Q * STEP) {
+      Quad res[Q] = {};
+      if (a.res_mode) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q) res[q] = load_quad4(rp + q * STEP * a.ldr);
+        rp += Q * STEP * a.ldr;
+      }
+      float v[Q][4];
+#pragma unroll
+      for (int q = 0; q < Q; ++q) {
+        const f32x4 s = take(r + q * STEP);
+        v[q][0] = s.x; v[q][1] = s.y; v[q][2] = s.z; v[q][3] = s.w;
+      }
+      finish(a, v, bias, res);
+#pragma unroll
+      for (int q = 0; q < Q; ++q) store_quad4(y + q * STEP * a.ldy, v[q]);
+      y += Q * STEP * a.ldy;
+    }
+  };
 #pragma unroll
   for (int h = 0; h < RM; h += H) {
 #pragma unroll
@@ -265,133 +400,103 @@ __global__ void __launch_bounds__(64 * WM * WN) linear_tile_kernel(LinearArgs a)
 #pragma unroll
       for (int i = 0; i < TN; ++i)
         *(f32x4*)(mine + (j * 16 + lrow) * RN * 4 + slot(j * 16 + lrow, i * 4 + kg)) = acc[i][h / 16 + j];
-    for (int q = lane; q < H * SLOTS; q += 64) {
-      const int r = q / SLOTS, s = q % SLOTS, row = m0 + wm + h + r, col = n0 + wn + s * 4;
-      if (row >= a.m || col >= a.n) continue;
-      const f32x4 v = *(const f32x4*)(mine + r * RN * 4 + slot(r, s));
-      if (a.split > 1) store_part(a, sp, row, col, v);
-      else store4(a, row, col, v);
-    }
-  }
-}
-
-// ------------------------------------------------------------------ few rows
-// Up to 16 MT rows of x: a block of WAVES waves computes 16 columns. The waves share the
-// reduction out in steps of 64 bytes of a row, D steps in flight each, and add their sums
-// through LDS in the order of the waves.
-template <typename T, int MT, int WAVES, int D, bool DIRECT>
-__global__ void __launch_bounds__(64 * WAVES) linear_rows_kernel(LinearArgs a) {
-  constexpr int G = 16 / (int)sizeof(T), KS = 4 * G;
-  __shared__ f32x4 part[WAVES][MT][64];
-  const int n0 = (int)blockIdx.x * 16, sp = (int)blockIdx.y;
-  const int lane = (int)threadIdx.x & 63, wave = wave_id();
-  const int lrow = lane & 15, kg = lane >> 4;
-  const RowsView vw = rows_view<T>(a.w, a.ldw, n0, a.n, 16, a.k), vx = rows_view<T>(a.x, a.ldx, 0, a.m, 16 * MT, a.k);
-  const __amdgpu_buffer_rsrc_t rw = make_rsrc(vw.base, vw.bytes), rx = make_rsrc(vx.base, vx.bytes);
-  const unsigned ow = n0 + lrow < a.n ? (unsigned)lrow * (unsigned)(a.ldw * (int)sizeof(T)) + vw.odd : kOobGroup;
-  unsigned ox[MT];
-#pragma unroll
-  for (int j = 0; j < MT; ++j)
-    ox[j] = 16 * j + lrow < a.m ? (unsigned)(16 * j + lrow) * (unsigned)(a.ldx * (int)sizeof(T)) + vx.odd : kOobGroup;
-
-  const int s0 = sp * a.per_split * 2, s1 = min((a.k + KS - 1) / KS, s0 + a.per_split * 2);
-  auto load = [&](__amdgpu_buffer_rsrc_t r, unsigned o, int k) __attribute__((always_inline)) {
-    const unsigned at = o == kOobGroup || k >= a.k ? kOobGroup : o + (unsigned)(k * (int)sizeof(T));
-    if constexpr (DIRECT) return load_quad(r, at);
-    else return load_quad_any<T>(r, at, a.k - k);
-  };
-  u32x4 fw[D], fx[D][MT];
-  f32x4 acc[MT] = {};
-  auto fetch = [&](int u, int s) __attribute__((always_inline)) {
-    const int k = s < s1 ? s * KS + kg * G : a.k;
-    fw[u] = load(rw, ow, k);
-#pragma unroll
-    for (int j = 0; j < MT; ++j) fx[u][j] = load(rx, ox[j], k);
-  };
-#pragma unroll
-  for (int u = 0; u < D; ++u) fetch(u, s0 + wave + u * WAVES);
-  for (int s = s0 + wave; s < s1; s += D * WAVES) {
-#pragma unroll
-    for (int u = 0; u < D; ++u) {
-#pragma unroll
-      for (int j = 0; j < MT; ++j) acc[j] = mma16<T>(fw[u], fx[u][j], acc[j]);
-      fetch(u, s + (u + D) * WAVES);
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < MT; ++j) part[wave][j][lane] = acc[j];
-  __syncthreads();
-  if (wave < MT) {
-    f32x4 v = part[0][wave][lane];
-#pragma unroll
-    for (int i = 1; i < WAVES; ++i) v += part[i][wave][lane];
-    const int row = wave * 16 + lrow, col = n0 + 4 * kg;
-    if (row < a.m && col < a.n) {
-      if (a.split > 1) store_part(a, sp, row, col, v);
-      else store4(a, row, col, v);
+    if (a.split > 1) {
+      for (int r = r0; r < H; r += STEP)
+        if (m0 + wm + h + r < a.m && col < a.n) store_part(a, sp, m0 + wm + h + r, col, take(r));
+    } else if (whole) {
+      if (a.out_bf16) finish_rows(h, bf16_t());
+      else finish_rows(h, 0.f);
+    } else {
+#pragma unroll 1
+      for (int r = r0; r < H; r += STEP) {
+        const int row = m0 + wm + h + r;
+        if (row < a.m && col < a.n) store4(a, row, col, take(r), bias, load_res(a, row, col));
+      }
     }
   }
 }
 
 // ------------------------------------------------------------------ plans and launches
-enum { LIN_ROWS, LIN_64, LIN_128, LIN_256 };
+// Tiles, from small to large. Of the two of a size the second leaves room for a second block
+// on the compute unit.
+enum { LIN_32, LIN_32_TWO, LIN_64X32, LIN_64, LIN_64_TWO, LIN_128, LIN_256, LIN_KINDS };
+struct TileShape {
+  int bm, bn, wm, wn, wk, stages;
+};
+constexpr TileShape kTiles[LIN_KINDS] = {{32, 32, 1, 2, 4, 3}, {32, 32, 1, 2, 4, 2},     {64, 32, 2, 2, 4, 3},
+                                         {64, 64, 2, 2, 2, 3}, {64, 64, 2, 2, 1, 4},     {128, 128, 2, 2, 1, 2},
+                                         {256, 256, 4, 2, 1, 2}};
 
-static int64_t tiles_of(const ct_linear_op& op, int t) {
-  return (int64_t)((op.m + t - 1) / t) * ((op.n + t - 1) / t);
+static int64_t tiles_of(const ct_linear_op& op, int kind) {
+  const TileShape t = kTiles[kind];
+  return (((int64_t)op.m + t.bm - 1) / t.bm) * (((int64_t)op.n + t.bn - 1) / t.bn);
 }
 
 LinearPlan plan_linear(const ct_linear_op& op) {
   LinearPlan p = {};
   const int chunks = (int)(((int64_t)op.k * elem_bytes(op.dtype) + 127) / 128);
-  int64_t blocks;
-  if (op.m <= 64) {
-    p.kind = LIN_ROWS;
-    blocks = (op.n + 15) / 16;
-  } else {
-    p.kind = tiles_of(op, 256) >= kPlanCus * 3 / 4 ? LIN_256 : tiles_of(op, 128) >= kPlanCus ? LIN_128 : LIN_64;
-    blocks = tiles_of(op, p.kind == LIN_256 ? 256 : p.kind == LIN_128 ? 128 : 64);
-  }
-  // Too few blocks for the compute units: slices of the reduction, of 8 chunks at least
-  int split = blocks < kPlanCus ? (int)(kPlanCus / blocks) : 1;
-  if (split > chunks / 8) split = chunks / 8;
-  if (split > 16) split = 16;
-  if (split < 1) split = 1;
-  p.per_split = chunks ? (chunks + split - 1) / split : 1;
-  p.split = chunks ? (chunks + p.per_split - 1) / p.per_split : 1;
+  // Rounds of the device, and what a round costs beside one of 128 x 128 tiles at the full
+  // rate (one of those on a compute unit alone does not reach it)
+  auto rounds = [&](int kind) { return (double)((tiles_of(op, kind) + kPlanCus - 1) / kPlanCus); };
+  const double t64 = 0.5 * rounds(LIN_64), t128 = rounds(LIN_128) > 1 ? 1.2 * rounds(LIN_128) : 1.65,
+               t256 = 4.0 * rounds(LIN_256);
+  p.kind = t64 <= t128 && t64 <= t256 ? LIN_64 : t128 <= t256 ? LIN_128 : LIN_256;
+  // Smaller tiles where 64 x 64 leaves compute units without one
+  const int64_t enough = kPlanCus * 3 / 4;
+  if (p.kind == LIN_64 && tiles_of(op, LIN_64) < enough)
+    p.kind = tiles_of(op, LIN_64X32) >= enough ? LIN_64X32 : LIN_32;
+  if (op.m <= 32) p.kind = LIN_32;
+  if (p.kind == LIN_64 && tiles_of(op, LIN_64) > kPlanCus) p.kind = LIN_64_TWO;
+  if (p.kind == LIN_32 && tiles_of(op, LIN_32) > kPlanCus) p.kind = LIN_32_TWO;
+  // A long reduction over few tiles: slices of it, of 32 chunks at least, so that they save
+  // more than the second kernel takes
+  const int64_t blocks = tiles_of(op, p.kind);
+  int split = 1;
+  if (blocks <= kPlanCus / 4 && chunks >= 128) split = (int)(kPlanCus / blocks < chunks / 32 ? kPlanCus / blocks : chunks / 32);
+  const int per = chunks ? (chunks + split - 1) / split : 1;
+  p.split = chunks ? (chunks + per - 1) / per : 1;
+  p.per_split = p.split > 1 ? per * (128 / elem_bytes(op.dtype)) : op.k;
   p.ws_floats = p.split > 1 ? (int64_t)p.split * op.m * ((op.n + 3) / 4 * 4) : 0;
   return p;
 }
 
-template <typename T, int BM, int BN, int WM, int WN, bool DIRECT>
+template <typename T, bool DIRECT, int KIND>
 static int launch_tile(LinearArgs a, hipStream_t st) {
-  a.tiles_m = (a.m + BM - 1) / BM;
-  a.tiles_n = (a.n + BN - 1) / BN;
+  constexpr TileShape t = kTiles[KIND];
+  constexpr int S = DIRECT ? t.stages : 2;
+  a.tiles_m = (a.m + t.bm - 1) / t.bm;
+  a.tiles_n = (a.n + t.bn - 1) / t.bn;
   const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
   if (tiles > 0x7FFFFFFF || 4 * (int64_t)a.tiles_m > 0x7FFFFFFF) return refuse_size("ct_linear_run");
   a.dgroup = make_fastdiv(4 * (int64_t)a.tiles_m);
   a.dlast = make_fastdiv(a.tiles_n % 4 ? a.tiles_n % 4 : 4);
-  hipLaunchKernelGGL((linear_tile_kernel<T, BM, BN, WM, WN, DIRECT>), dim3((unsigned)tiles, (unsigned)a.split),
-                     dim3(64 * WM * WN), 2 * (BM + BN) * 128, st, a);
-  return hipGetLastError() == hipSuccess ? 0 : -1;
-}
-template <typename T, int MT, bool DIRECT>
-static int launch_rows(const LinearArgs& a, hipStream_t st) {
-  constexpr int WAVES = 16, D = MT <= 2 ? 4 : 2;
-  hipLaunchKernelGGL((linear_rows_kernel<T, MT, WAVES, D, DIRECT>), dim3((unsigned)((a.n + 15) / 16), (unsigned)a.split),
-                     dim3(64 * WAVES), 0, st, a);
+  hipLaunchKernelGGL((linear_tile_kernel<T, t.bm, t.bn, t.wm, t.wn, t.wk, S, DIRECT>),
+                     dim3((unsigned)tiles, (unsigned)a.split), dim3(64 * t.wm * t.wn * t.wk),
+                     S * t.wk * (t.bm + t.bn) * 128, st, a);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
 template <typename T, bool DIRECT>
 static int linear_pick(const LinearArgs& a, int kind, hipStream_t st) {
-  switch (kind) {
-    case LIN_256:
-      if constexpr (DIRECT) return launch_tile<T, 256, 256, 2, 4, DIRECT>(a, st);
-    case LIN_128: return launch_tile<T, 128, 128, 2, 2, DIRECT>(a, st);
-    case LIN_64: return launch_tile<T, 64, 64, 2, 2, DIRECT>(a, st);
+  if constexpr (DIRECT) {
+    switch (kind) {
+      case LIN_32: return launch_tile<T, DIRECT, LIN_32>(a, st);
+      case LIN_32_TWO: return launch_tile<T, DIRECT, LIN_32_TWO>(a, st);
+      case LIN_64X32: return launch_tile<T, DIRECT, LIN_64X32>(a, st);
+      case LIN_64: return launch_tile<T, DIRECT, LIN_64>(a, st);
+      case LIN_64_TWO: return launch_tile<T, DIRECT, LIN_64_TWO>(a, st);
+      case LIN_128: return launch_tile<T, DIRECT, LIN_128>(a, st);
+      default: return launch_tile<T, DIRECT, LIN_256>(a, st);
+    }
+  } else {  // two stages whatever the tile
+    switch (kind) {
+      case LIN_32:
+      case LIN_32_TWO: return launch_tile<T, DIRECT, LIN_32>(a, st);
+      case LIN_64X32:
+      case LIN_64:
+      case LIN_64_TWO: return launch_tile<T, DIRECT, LIN_64_TWO>(a, st);
+      default: return launch_tile<T, DIRECT, LIN_128>(a, st);
+    }
   }
-  if (a.m <= 16) return launch_rows<T, 1, DIRECT>(a, st);
-  if (a.m <= 32) return launch_rows<T, 2, DIRECT>(a, st);
-  return launch_rows<T, 4, DIRECT>(a, st);
 }
 
 int launch_linear(const ct_linear_op& op, const LinearPlan& p, const void* x, const void* w, const float* bias,

@@ -30,7 +30,7 @@ struct SeqView {
 struct LinearPlan {
   int kind;           // the kernel (k_linear.hip)
   int split;          // slices of the reduction, each with partial sums of its own
-  int per_split;      // 128-byte chunks of a row in a slice
+  int per_split;      // elements of a row in a slice
   int64_t ws_floats;  // split * m * n where the reduction is split
 };
 LinearPlan plan_linear(const ct_linear_op& op);
