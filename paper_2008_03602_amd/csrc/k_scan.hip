@@ -1,9 +1,23 @@
 // Selective state space scan over packed sequences.
 //   h_t[n] = exp(dt_t a[n]) h_{t-1}[n] + dt_t u_t b_t[n],  y_t = (c_t . h_t + d u_t) silu(z_t)
 //
-// A lane holds NS states of one channel in fp32 registers and walks the tokens of a
-// sequence; P neighbouring lanes share a channel where it has more than NS states.
+// A lane holds NS states of one channel in fp32 registers and walks tokens; P neighbouring
+// lanes share a channel of more than NS states. Of a state and token the vector ALU has an
+// exponential at a quarter of its rate and four products at the full one: 32 clocks of a
+// SIMD for 64 of them, which bounds prompts (exponents of 16 states take more time than
+// all their bytes). Single tokens are bound by the states' bytes.
+//
+// Where channels and sequences are too few for the device, sequences are cut into chunks:
+//   sum:    h at each chunk's end from h = 0 at its start, and the sum of its steps;
+//   carry:  h at each chunk's start, chunk after chunk, by
+//           h(end) = exp(a * sum of steps) h(start) + h(end from 0);
+//   out:    the outputs of each chunk from h at its start.
+// That is nearly twice the exponentials, but as many chunks at once as fill the device.
+// The carries are read from state_in before any chunk's outputs write state_out, so that
+// both may be one array.
 #include <hip/hip_runtime.h>
+
+#include <type_traits>
 
 #include "k_seq.h"
 
@@ -13,93 +27,380 @@ struct ScanArgs {
   SeqView s;
   const void *u, *delta, *b, *c, *z;
   const float *dt_bias, *a, *d_skip, *state_in;
-  float* state_out;
+  float *state_out, *ws, *ws_dt;
   void* y;
   int64_t ldu, lddelta, ldb, ldc, ldz, ldy;
   int channels, states, per_group, softplus;
+  int per, chunk;     // chunks of a sequence where all are equal, tokens of a chunk
+  int64_t chunks;
   FastDiv dtiles, dgroup;  // channel tiles in all, and of one group
 };
 
-template <typename T, int NS, int P>
+template <int NS>
+struct Vals {
+  float v[NS];
+};
+// NS values from p on, 0 for those past `left`. vec: rows lie on 16-byte addresses and end on
+// a multiple of four values.
+template <int NS>
+__device__ __forceinline__ Vals<NS> load_vals(const float* p, int left, bool vec) {
+  Vals<NS> r;
+  if (vec && NS % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < NS; i += 4) {
+      f32x4 q = {};
+      if (i < left) q = *(const f32x4*)(p + i);
+      r.v[i] = q.x; r.v[i + 1] = q.y; r.v[i + 2] = q.z; r.v[i + 3] = q.w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < NS; ++i) r.v[i] = i < left ? p[i] : 0.f;
+  }
+  return r;
+}
+template <int NS>
+__device__ __forceinline__ void store_vals(float* p, const float (&v)[NS], int left, bool vec) {
+  if (vec && NS % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < NS; i += 4)
+      if (i < left) *(f32x4*)(p + i) = (f32x4){v[i], v[i + 1], v[i + 2], v[i + 3]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+      if (i < left) p[i] = v[i];
+  }
+}
+__device__ __forceinline__ bool rows_of_four(const void* p, int states) {
+  return ((uintptr_t)p % 16 | (unsigned)states % 4) == 0;
+}
+template <int P>
+__device__ __forceinline__ float add_lanes(float v) {
+#pragma unroll
+  for (int m = 1; m < P; m *= 2) v += __shfl_xor(v, m, 64);
+  return v;
+}
+
+// ------------------------------------------------------------------ prompts
+enum ScanMode { SCAN_WHOLE, SCAN_SUM, SCAN_OUT };
+
+// Four waves walk a chunk (or a whole sequence) for 4 * 64 / P channels of one group. b and c
+// of TT tokens are staged in LDS in fp32, where all channels read them; the next ones are on
+// their way meanwhile.
+template <typename T, int NS, int P, int MODE>
 __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
-  constexpr int CH = 64 / P;  // channels of a wave, all of one group
+  constexpr int CH = 64 / P, NP = NS * P, TT = NP <= 16 ? 32 : NP <= 64 ? 16 : 4, U = 4;
+  constexpr int STAGED = TT * NP / 256 ? TT * NP / 256 : 1;  // values of b (and of c) that a thread stages
+  __shared__ __align__(16) float sb[2][TT][NP], sc[MODE == SCAN_SUM ? 1 : 2][MODE == SCAN_SUM ? 1 : TT][NP];
+
+  const int id = fdiv((int)blockIdx.x, a.dtiles), tile = (int)blockIdx.x - id * a.dtiles.d;
+  const int group = fdiv(tile, a.dgroup), in_group = ((tile - group * a.dgroup.d) * 4 + wave_id()) * CH;
+  int t0, t1;
+  SeqRange r;
+  if constexpr (MODE == SCAN_WHOLE) {
+    r = seq_range(a.s, id);
+    t0 = r.begin;
+    t1 = r.end;
+  } else {
+    r = find_tile(a.s, a.per, a.chunk, id, &t0);
+    if (r.s < 0 || t0 >= r.end) return;
+    t1 = min(r.end, t0 + a.chunk);
+    if (MODE == SCAN_SUM && t1 == r.end) return;  // nothing follows this chunk
+  }
+  t0 = __builtin_amdgcn_readfirstlane(t0);
+  t1 = __builtin_amdgcn_readfirstlane(t1);
+  const int lane = (int)threadIdx.x & 63, part = lane % P, ch = in_group + lane / P;
+  const bool live = ch < a.per_group;
+  const int d = group * a.per_group + (live ? ch : a.per_group - 1), n0 = part * NS;  // spare lanes repeat a channel
+  const int left = a.states - n0;
+
+  Vals<NS> la = load_vals<NS>(a.a + (int64_t)d * a.states + n0, left, rows_of_four(a.a, a.states));
+#pragma unroll
+  for (int i = 0; i < NS; ++i) la.v[i] *= kLog2e;
+  const int slot = MODE == SCAN_SUM ? -1 : seq_slot(a.s, r.s);
+  const int64_t at = ((int64_t)slot * a.channels + d) * a.states + n0;
+  const int64_t in_ws = ((int64_t)id * a.channels + d) * a.states + n0;
+  Vals<NS> h = {};
+  if constexpr (MODE == SCAN_OUT) h = load_vals<NS>(a.ws + in_ws, left, rows_of_four(a.ws, a.states));
+  if (MODE == SCAN_WHOLE && slot >= 0 && a.state_in)
+    h = load_vals<NS>(a.state_in + at, left, rows_of_four(a.state_in, a.states));
+  const float bias = a.dt_bias ? a.dt_bias[d] : 0.f, skip = a.d_skip ? a.d_skip[d] : 0.f;
+  float total = 0.f;
+
+  // staging
+  T kb[STAGED], kc[STAGED];
+  auto fetch = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < STAGED; ++i) {
+      const int e = i * 256 + (int)threadIdx.x, row = e / NP, n = e % NP;
+      const bool ok = row < TT && t + row < t1 && n < a.states;
+      const int64_t tok = ok ? t + row : t0, at_n = (int64_t)group * a.states + (ok ? n : 0);
+      const T vb = ((const T*)a.b)[tok * a.ldb + at_n];
+      kb[i] = ok ? vb : (T)0.f;
+      if constexpr (MODE != SCAN_SUM) {
+        const T vc = ((const T*)a.c)[tok * a.ldc + at_n];
+        kc[i] = ok ? vc : (T)0.f;
+      }
+    }
+  };
+  auto put = [&](int s) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < STAGED; ++i) {
+      const int e = i * 256 + (int)threadIdx.x;
+      if (TT * NP >= 256 || e < TT * NP) {
+        (&sb[s][0][0])[e] = (float)kb[i];
+        if constexpr (MODE != SCAN_SUM) (&sc[s][0][0])[e] = (float)kc[i];
+      }
+    }
+  };
+  // the next U tokens of this lane's channel
+  T ku[U], kd[U], kz[U];
+  auto fetch_rows = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int64_t tok = min(t + i, t1 - 1);
+      ku[i] = ((const T*)a.u + tok * a.ldu)[d];
+      kd[i] = ((const T*)a.delta + tok * a.lddelta)[d];
+      if (MODE != SCAN_SUM && a.z) kz[i] = ((const T*)a.z + tok * a.ldz)[d];
+    }
+  };
+
+  if (t0 < t1) {
+    fetch(t0);
+    fetch_rows(t0);
+    for (int t = t0, s = 0; t < t1; t += TT, s ^= 1) {
+      put(s);
+      __syncthreads();  // also: every wave is done with the stage before last
+      if (t + TT < t1) fetch(t + TT);
+      auto tokens = [&](int q, auto all) __attribute__((always_inline)) {
+        float dt[U], du[U], u[U], z[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          u[i] = (float)ku[i];
+          const float v = (float)kd[i] + bias;
+          dt[i] = a.softplus ? softplus_f32(v) : v;
+          du[i] = dt[i] * u[i];
+          if constexpr (MODE != SCAN_SUM) z[i] = a.z ? silu_f32((float)kz[i]) : 1.f;
+        }
+        if (t + q + U < t1) fetch_rows(t + q + U);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+          if (!all.value && t + q + i >= t1) break;
+          float y = 0.f;
+#pragma unroll
+          for (int n = 0; n < NS; ++n) {
+            h.v[n] = fmaf(__builtin_amdgcn_exp2f(dt[i] * la.v[n]), h.v[n], du[i] * sb[s][q + i][n0 + n]);
+            if constexpr (MODE != SCAN_SUM) y = fmaf(sc[s][q + i][n0 + n], h.v[n], y);
+          }
+          if constexpr (MODE == SCAN_SUM) {
+            total += dt[i];
+          } else {
+            y = fmaf(skip, u[i], add_lanes<P>(y)) * z[i];
+            if (part == 0 && live) ((T*)a.y + (int64_t)(t + q + i) * a.ldy)[d] = from_f32<T>(y);
+          }
+        }
+      };
+#pragma unroll 1
+      for (int q = 0; q < TT && t + q < t1; q += U) {
+        if (t + q + U <= t1) tokens(q, std::true_type{});
+        else tokens(q, std::false_type{});
+      }
+    }
+  }
+  if (!live) return;
+  if constexpr (MODE == SCAN_SUM) {
+    store_vals<NS>(a.ws + in_ws, h.v, left, rows_of_four(a.ws, a.states));
+    if (part == 0) a.ws_dt[(int64_t)id * a.channels + d] = total;
+  } else if (slot >= 0 && a.state_out && t1 == r.end) {
+    store_vals<NS>(a.state_out + at, h.v, left, rows_of_four(a.state_out, a.states));
+  }
+}
+
+// h at the start of every chunk, in place of h at its end from 0. A thread has one state of
+// one channel; the loads of eight chunks are on their way together. An empty sequence hands
+// its state on.
+__global__ void __launch_bounds__(256) scan_carry_kernel(ScanArgs a) {
+  const int64_t per_seq = (int64_t)a.channels * a.states;
+  const int blocks = (int)((per_seq + 255) / 256);
+  const int s = (int)(blockIdx.x / blocks);
+  const int64_t e = (int64_t)(blockIdx.x % blocks) * 256 + threadIdx.x;
+  if (e >= per_seq) return;
+  const int d = (int)(e / a.states);
+  const SeqRange r = seq_range(a.s, s);
+  const int slot = seq_slot(a.s, s);
+  const int n = (r.end - r.begin + a.chunk - 1) / a.chunk;
+  const int64_t id = a.s.offsets ? r.begin / a.chunk + s : (int64_t)s * a.per;
+  float h = slot >= 0 && a.state_in ? a.state_in[(int64_t)slot * per_seq + e] : 0.f;
+  if (n == 0) {
+    if (slot >= 0 && a.state_out) a.state_out[(int64_t)slot * per_seq + e] = h;
+    return;
+  }
+  const float la = a.a[e] * kLog2e;
+  float* p = a.ws + id * per_seq + e;
+  const float* dt = a.ws_dt + id * a.channels + d;
+  constexpr int F = 8;
+  for (int c = 0; c < n; c += F) {
+    float end[F], sum[F];
+#pragma unroll
+    for (int i = 0; i < F; ++i) {
+      const int k = min(c + i, max(n - 2, 0));  // the last chunk's end is nobody's start
+      end[i] = n > 1 ? p[(int64_t)k * per_seq] : 0.f;
+      sum[i] = n > 1 ? dt[(int64_t)k * a.channels] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < F; ++i)
+      if (c + i < n) {
+        p[(int64_t)(c + i) * per_seq] = h;
+        h = fmaf(__builtin_amdgcn_exp2f(la * sum[i]), h, end[i]);
+      }
+  }
+}
+
+// ------------------------------------------------------------------ single tokens
+// One token of each sequence: a wave updates 64 / P channels of SEQ sequences, whose loads are
+// all on their way together; a, the bias and the skip weight are read once for them.
+template <typename T, int NS, int P, int SEQ>
+__global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
+  constexpr int CH = 64 / P;
   const int64_t g = (int64_t)blockIdx.x * 4 + wave_id();
-  if (g >= (int64_t)a.s.count * a.dtiles.d) return;
-  const int s = fdiv((int)g, a.dtiles), tile = (int)g - s * a.dtiles.d;
+  if (g >= (int64_t)((a.s.count + SEQ - 1) / SEQ) * a.dtiles.d) return;
+  const int first = fdiv((int)g, a.dtiles) * SEQ, tile = (int)g - first / SEQ * a.dtiles.d;
   const int group = fdiv(tile, a.dgroup), in_group = (tile - group * a.dgroup.d) * CH;
   const int lane = (int)(threadIdx.x & 63), part = lane % P, ch = in_group + lane / P;
   if (ch >= a.per_group) return;
-  const int d = group * a.per_group + ch, n0 = part * NS;
-  const SeqRange r = seq_range(a.s, s);
-  const int slot = seq_slot(a.s, s);
-
-  float h[NS], la[NS];
-  const int64_t at = ((int64_t)slot * a.channels + d) * a.states + n0;
-#pragma unroll
-  for (int i = 0; i < NS; ++i) {
-    const bool in = n0 + i < a.states;
-    h[i] = in && slot >= 0 && a.state_in ? a.state_in[at + i] : 0.f;
-    la[i] = in ? a.a[(int64_t)d * a.states + n0 + i] * kLog2e : 0.f;
-  }
-  const float bias = a.dt_bias ? a.dt_bias[d] : 0.f, skip = a.d_skip ? a.d_skip[d] : 0.f;
+  const int d = group * a.per_group + ch, n0 = part * NS, left = a.states - n0;
   const int64_t gn = (int64_t)group * a.states + n0;
-  for (int t = r.begin; t < r.end; ++t) {
-    float dt = (float)((const T*)a.delta)[t * a.lddelta + d] + bias;
-    if (a.softplus) dt = softplus_f32(dt);
-    const float u = (float)((const T*)a.u)[t * a.ldu + d], du = dt * u;
+  const bool vec = rows_of_four(a.state_in, a.states) && rows_of_four(a.state_out, a.states);
+
+  int slot[SEQ];
+  Vals<NS> h[SEQ], b[SEQ], c[SEQ];
+  float u[SEQ], dt[SEQ], z[SEQ];
+#pragma unroll
+  for (int q = 0; q < SEQ; ++q) slot[q] = first + q < a.s.count ? seq_slot(a.s, first + q) : -1;
+#pragma unroll
+  for (int q = 0; q < SEQ; ++q) {
+    const int t = min(first + q, a.s.count - 1);
+    h[q] = {};
+    if (slot[q] >= 0 && a.state_in)
+      h[q] = load_vals<NS>(a.state_in + ((int64_t)slot[q] * a.channels + d) * a.states + n0, left, vec);
+    u[q] = (float)((const T*)a.u + t * a.ldu)[d];
+    dt[q] = (float)((const T*)a.delta + t * a.lddelta)[d];
+    z[q] = a.z ? (float)((const T*)a.z + t * a.ldz)[d] : 0.f;
+#pragma unroll
+    for (int i = 0; i < NS; ++i) {
+      b[q].v[i] = i < left ? (float)((const T*)a.b + t * a.ldb)[gn + i] : 0.f;
+      c[q].v[i] = i < left ? (float)((const T*)a.c + t * a.ldc)[gn + i] : 0.f;
+    }
+  }
+  Vals<NS> la = load_vals<NS>(a.a + (int64_t)d * a.states + n0, left, rows_of_four(a.a, a.states));
+  const float bias = a.dt_bias ? a.dt_bias[d] : 0.f, skip = a.d_skip ? a.d_skip[d] : 0.f;
+#pragma unroll
+  for (int q = 0; q < SEQ; ++q) {
+    const float v = dt[q] + bias, step = a.softplus ? softplus_f32(v) : v, du = step * u[q];
     float y = 0.f;
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
-      const bool in = n0 + i < a.states;
-      const float b = in ? (float)((const T*)a.b)[t * a.ldb + gn + i] : 0.f;
-      const float c = in ? (float)((const T*)a.c)[t * a.ldc + gn + i] : 0.f;
-      h[i] = fmaf(__builtin_amdgcn_exp2f(dt * la[i]), h[i], du * b);
-      y = fmaf(c, h[i], y);
+      h[q].v[i] = fmaf(__builtin_amdgcn_exp2f(step * (la.v[i] * kLog2e)), h[q].v[i], du * b[q].v[i]);
+      y = fmaf(c[q].v[i], h[q].v[i], y);
     }
-#pragma unroll
-    for (int m = 1; m < P; m *= 2) y += __shfl_xor(y, m, 64);
-    y = fmaf(skip, u, y);
-    if (a.z) y *= silu_f32((float)((const T*)a.z)[t * a.ldz + d]);
-    if (part == 0) ((T*)a.y)[t * a.ldy + d] = from_f32<T>(y);
+    y = fmaf(skip, u[q], add_lanes<P>(y));
+    if (a.z) y *= silu_f32(z[q]);
+    if (first + q < a.s.count && part == 0) ((T*)a.y + (first + q) * a.ldy)[d] = from_f32<T>(y);
+    if (slot[q] >= 0 && a.state_out)
+      store_vals<NS>(a.state_out + ((int64_t)slot[q] * a.channels + d) * a.states + n0, h[q].v, left, vec);
   }
-  if (slot >= 0 && a.state_out)
-#pragma unroll
-    for (int i = 0; i < NS; ++i)
-      if (n0 + i < a.states) a.state_out[at + i] = h[i];
 }
 
-ScanPlan plan_scan(const ct_scan_op&, const ct_sequences&) { return {0, 0, 0}; }
+// ------------------------------------------------------------------ plans and launches
+// Lanes that share a channel, and states of each, in the two kinds of kernel.
+static int prompt_parts(int states) { return states <= 16 ? 1 : states <= 32 ? 2 : states <= 64 ? 4 : states <= 128 ? 8 : 16; }
 
+ScanPlan plan_scan(const ct_scan_op& op, const ct_sequences& s) {
+  ScanPlan p = {};
+  if (!s.tokens) return p;
+  const int most = s.offsets ? (s.max_len ? (s.max_len < s.tokens ? s.max_len : s.tokens) : s.tokens) : s.tokens / s.count;
+  // waves of a chunk, chunks for three waves on every SIMD, tokens of a chunk in whole stages
+  const int ch = 64 / prompt_parts(op.states), per_group = op.channels / op.groups;
+  const int64_t waves = (int64_t)op.groups * ((per_group + ch - 1) / ch);
+  int64_t chunk = ((int64_t)s.tokens * waves / (3 * 4 * kPlanCus) + 31) / 32 * 32;
+  if (chunk < 64) chunk = 64;
+  if (most <= 2 * chunk) return p;  // no sequence is worth cutting
+  p.chunk = (int)chunk;
+  p.chunks = s.offsets ? s.tokens / chunk + s.count : (int64_t)s.count * ((most + chunk - 1) / chunk);
+  p.ws_floats = p.chunks * op.channels * (op.states + 1);
+  return p;
+}
+
+template <typename T, int NS, int P, int MODE>
+static int scan_launch(ScanArgs a, int64_t pieces, hipStream_t st) {
+  constexpr int CH = 4 * 64 / P;
+  const int per = (a.per_group + CH - 1) / CH;
+  const int64_t tiles = (int64_t)per * (a.channels / a.per_group), blocks = tiles * pieces;
+  if (blocks > 0x7FFFFFFF) return refuse_size("ct_scan_run");
+  a.dgroup = make_fastdiv(per);
+  a.dtiles = make_fastdiv(tiles);
+  hipLaunchKernelGGL((scan_kernel<T, NS, P, MODE>), dim3((unsigned)blocks), dim3(256), 0, st, a);
+  return hipGetLastError() == hipSuccess ? 0 : -1;
+}
 template <typename T, int NS, int P>
-static int scan_launch(ScanArgs a, hipStream_t st) {
+static int scan_prompt(ScanArgs a, const ScanPlan& p, hipStream_t st) {
+  if (!p.chunk) return scan_launch<T, NS, P, SCAN_WHOLE>(a, a.s.count, st);
+  a.chunk = p.chunk;
+  a.chunks = p.chunks;
+  a.per = a.s.offsets ? 0 : (a.s.len + p.chunk - 1) / p.chunk;
+  a.ws_dt = a.ws + p.chunks * a.channels * a.states;
+  int rc = scan_launch<T, NS, P, SCAN_SUM>(a, p.chunks, st);
+  if (rc) return rc;
+  const int64_t blocks = (((int64_t)a.channels * a.states + 255) / 256) * a.s.count;
+  if (blocks > 0x7FFFFFFF) return refuse_size("ct_scan_run");
+  hipLaunchKernelGGL(scan_carry_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
+  if (hipGetLastError() != hipSuccess) return -1;
+  return scan_launch<T, NS, P, SCAN_OUT>(a, p.chunks, st);
+}
+template <typename T, int NS, int P, int SEQ>
+static int step_launch(ScanArgs a, hipStream_t st) {
   constexpr int CH = 64 / P;
   const int per = (a.per_group + CH - 1) / CH;
-  const int64_t tiles = (int64_t)per * (a.channels / a.per_group), waves = tiles * a.s.count;
+  const int64_t tiles = (int64_t)per * (a.channels / a.per_group), waves = tiles * ((a.s.count + SEQ - 1) / SEQ);
   if (waves > 0x7FFFFFFF) return refuse_size("ct_scan_run");
   a.dgroup = make_fastdiv(per);
   a.dtiles = make_fastdiv(tiles);
-  hipLaunchKernelGGL((scan_kernel<T, NS, P>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((scan_step_kernel<T, NS, P, SEQ>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, a);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
+template <typename T, int NS, int P>
+static int scan_step(const ScanArgs& a, hipStream_t st) {
+  // several sequences a wave once there are enough waves without
+  const int64_t waves = (int64_t)a.channels * P / 64 * a.s.count;
+  return waves >= 16 * 4 * kPlanCus ? step_launch<T, NS, P, 4>(a, st) : step_launch<T, NS, P, 1>(a, st);
+}
 template <typename T>
-static int scan_pick(const ScanArgs& a, hipStream_t st) {
-  if (a.states <= 16) return scan_launch<T, 4, 4>(a, st);
-  if (a.states <= 32) return scan_launch<T, 4, 8>(a, st);
-  if (a.states <= 64) return scan_launch<T, 8, 8>(a, st);
-  if (a.states <= 128) return scan_launch<T, 8, 16>(a, st);
-  return scan_launch<T, 16, 16>(a, st);
+static int scan_pick(const ScanArgs& a, const ScanPlan& p, hipStream_t st) {
+  if (!a.s.offsets && a.s.len == 1) {
+    if (a.states <= 16) return scan_step<T, 4, 4>(a, st);
+    if (a.states <= 32) return scan_step<T, 4, 8>(a, st);
+    if (a.states <= 64) return scan_step<T, 4, 16>(a, st);
+    if (a.states <= 128) return scan_step<T, 8, 16>(a, st);
+    return scan_step<T, 16, 16>(a, st);
+  }
+  switch (prompt_parts(a.states)) {
+    case 1: return a.states <= 8 ? scan_prompt<T, 8, 1>(a, p, st) : scan_prompt<T, 16, 1>(a, p, st);
+    case 2: return scan_prompt<T, 16, 2>(a, p, st);
+    case 4: return scan_prompt<T, 16, 4>(a, p, st);
+    case 8: return scan_prompt<T, 16, 8>(a, p, st);
+    default: return scan_prompt<T, 16, 16>(a, p, st);
+  }
 }
 
-int launch_scan(const ct_scan_op& op, const ScanPlan&, const SeqView& s, const ScanArrays& v, void* stream) {
+int launch_scan(const ct_scan_op& op, const ScanPlan& p, const SeqView& s, const ScanArrays& v, void* stream) {
   ScanArgs a = {};
   a.s = s;
   a.u = v.u; a.delta = v.delta; a.b = v.b; a.c = v.c; a.z = v.z;
   a.dt_bias = v.dt_bias; a.a = v.a; a.d_skip = v.d_skip; a.state_in = v.state_in;
-  a.state_out = v.state_out; a.y = v.y;
+  a.state_out = v.state_out; a.y = v.y; a.ws = v.ws;
   a.ldu = op.ldu; a.lddelta = op.lddelta; a.ldb = op.ldb; a.ldc = op.ldc; a.ldz = op.ldz; a.ldy = op.ldy;
   a.channels = op.channels; a.states = op.states; a.per_group = op.channels / op.groups; a.softplus = op.softplus;
-  return op.dtype == CT_DT_BF16 ? scan_pick<bf16_t>(a, (hipStream_t)stream)
-                                : scan_pick<float>(a, (hipStream_t)stream);
+  return op.dtype == CT_DT_BF16 ? scan_pick<bf16_t>(a, p, (hipStream_t)stream)
+                                : scan_pick<float>(a, p, (hipStream_t)stream);
 }
 
 }  // namespace ct

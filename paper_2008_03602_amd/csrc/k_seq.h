@@ -55,12 +55,13 @@ __device__ __forceinline__ float exp_f32(float v) { return __builtin_amdgcn_exp2
 __device__ __forceinline__ float silu_f32(float v) { return v * __builtin_amdgcn_rcpf(1.f + exp_f32(-v)); }
 // log(1 + exp(v)) = max(v, 0) + log1p(e), e = exp(-|v|). The step sizes of a scan are the
 // small values of this function, where log(1 + e) has lost e's low bits: u = 1 + e is
-// rounded, and log1p(e) = log(u) + (e - (u - 1)) / u to first order in that rounding.
+// rounded, and log1p(e) = log(u) + (e - (u - 1)) / u to first order in that rounding. The
+// division changes the correction, half a unit of u at most, by less than a unit of the sum.
 __device__ __forceinline__ float softplus_f32(float v) {
   const float e = exp_f32(-fabsf(v)), u = 1.f + e;
   const float l = __builtin_amdgcn_logf(u) * 0.6931471805599453f;
   const float top = v < 0.f ? 0.f : v;  // keeps NaN
-  return top + fmaf(e - (u - 1.f), __builtin_amdgcn_rcpf(u), l);
+  return top + (l + (e - (u - 1.f)));
 }
 // v / 2 (1 + erf(v / sqrt(2))) = v Phi(v), with the tail probability of |v| after Abramowitz
 // and Stegun, 7.1.26 (off by 7.5e-8 at most): Phi(-|v|) = t (c1 + t (c2 + ...)) exp(-v^2 / 2)
