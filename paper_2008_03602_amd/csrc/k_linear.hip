@@ -21,6 +21,7 @@ struct LinearArgs {
   int m, n, k;
   int64_t ldx, ldw, ldr, ldy;
   int act, res_mode, out_bf16;
+  int stream;           // y goes past the caches
   int vec_out;          // rows of y and r take accesses of four elements
   int tiles_m, tiles_n;
   int split, per_split; // slices of the reduction, elements in each (whole 128-byte chunks)
@@ -47,26 +48,6 @@ __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 acc) {
 }
 
 // ------------------------------------------------------------------ epilogue
-struct Quad {
-  float v[4];
-};
-// Four elements of a row that all exist, at an address for them in one access.
-template <typename O>
-__device__ __forceinline__ Quad load_quad4(const O* p) {
-  if constexpr (sizeof(O) == 2) {
-    const u32x2 q = *(const u32x2*)p;
-    const unsigned q0 = q.x, q1 = q.y;
-    return {unpack<O>(q0, 0), unpack<O>(q0, 1), unpack<O>(q1, 0), unpack<O>(q1, 1)};
-  } else {
-    const f32x4 q = *(const f32x4*)p;
-    return {q.x, q.y, q.z, q.w};
-  }
-}
-template <typename O>
-__device__ __forceinline__ void store_quad4(O* p, const float* v) {
-  if constexpr (sizeof(O) == 2) *(u32x2*)p = (u32x2){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-  else *(f32x4*)p = (f32x4){v[0], v[1], v[2], v[3]};
-}
 // Four columns of the bias, and of a row of the residual, from column j on: 0 where there
 // are none.
 __device__ __forceinline__ Quad load_bias(const LinearArgs& a, int j) {
@@ -118,8 +99,8 @@ __device__ __forceinline__ void store4(const LinearArgs& a, int i, int j, f32x4 
   finish(a, v, bias, res);
   const int64_t at = i * a.ldy + j;
   if (a.vec_out && j + 4 <= a.n) {
-    if (a.out_bf16) store_quad4((bf16_t*)a.y + at, v[0]);
-    else store_quad4((float*)a.y + at, v[0]);
+    if (a.out_bf16) store_quad4((bf16_t*)a.y + at, v[0], false);
+    else store_quad4((float*)a.y + at, v[0], false);
     return;
   }
 #pragma unroll
@@ -389,7 +370,7 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearAr
       }
       finish(a, v, bias, res);
 #pragma unroll
-      for (int q = 0; q < Q; ++q) store_quad4(y + q * STEP * a.ldy, v[q]);
+      for (int q = 0; q < Q; ++q) store_quad4(y + q * STEP * a.ldy, v[q], a.stream);
       y += Q * STEP * a.ldy;
     }
   };
@@ -507,6 +488,7 @@ int launch_linear(const ct_linear_op& op, const LinearPlan& p, const void* x, co
   a.ldx = op.ldx; a.ldw = op.ldw; a.ldr = op.ldr; a.ldy = op.ldy;
   a.act = op.act; a.res_mode = op.res; a.out_bf16 = op.out_dtype == CT_DT_BF16;
   a.split = p.split; a.per_split = p.per_split;
+  a.stream = (int64_t)op.m * op.n * elem_bytes(op.out_dtype) >= kStreamBytes;
   const int e = elem_bytes(op.dtype), four = 4 * elem_bytes(op.out_dtype);
   a.vec_out = (uintptr_t)y % four == 0 && op.ldy % 4 == 0 && (uintptr_t)bias % 16 == 0 &&
               (!op.res || ((uintptr_t)res % four == 0 && op.ldr % 4 == 0));

@@ -31,6 +31,8 @@ struct ScanArgs {
   void* y;
   int64_t ldu, lddelta, ldb, ldc, ldz, ldy;
   int channels, states, per_group, softplus;
+  int stream;         // the states go past the caches
+  int vec_bc;         // rows of b and c take accesses of four values
   int per, chunk;     // chunks of a sequence where all are equal, tokens of a chunk
   int64_t chunks;
   FastDiv dtiles, dgroup;  // channel tiles in all, and of one group
@@ -59,11 +61,11 @@ __device__ __forceinline__ Vals<NS> load_vals(const float* p, int left, bool vec
   return r;
 }
 template <int NS>
-__device__ __forceinline__ void store_vals(float* p, const float (&v)[NS], int left, bool vec) {
+__device__ __forceinline__ void store_vals(float* p, const float (&v)[NS], int left, bool vec, bool stream) {
   if (vec && NS % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < NS; i += 4)
-      if (i < left) *(f32x4*)(p + i) = (f32x4){v[i], v[i + 1], v[i + 2], v[i + 3]};
+      if (i < left) store_once((f32x4*)(p + i), (f32x4){v[i], v[i + 1], v[i + 2], v[i + 3]}, stream);
   } else {
 #pragma unroll
     for (int i = 0; i < NS; ++i)
@@ -208,10 +210,10 @@ __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
   }
   if (!live) return;
   if constexpr (MODE == SCAN_SUM) {
-    store_vals<NS>(a.ws + in_ws, h.v, left, rows_of_four(a.ws, a.states));
+    store_vals<NS>(a.ws + in_ws, h.v, left, rows_of_four(a.ws, a.states), false);
     if (part == 0) a.ws_dt[(int64_t)id * a.channels + d] = total;
   } else if (slot >= 0 && a.state_out && t1 == r.end) {
-    store_vals<NS>(a.state_out + at, h.v, left, rows_of_four(a.state_out, a.states));
+    store_vals<NS>(a.state_out + at, h.v, left, rows_of_four(a.state_out, a.states), false);
   }
 }
 
@@ -260,6 +262,7 @@ __global__ void __launch_bounds__(256) scan_carry_kernel(ScanArgs a) {
 // all on their way together; a, the bias and the skip weight are read once for them.
 template <typename T, int NS, int P, int SEQ>
 __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
+  static_assert(NS % 4 == 0, "");
   constexpr int CH = 64 / P;
   const int64_t g = (int64_t)blockIdx.x * 4 + wave_id();
   if (g >= (int64_t)((a.s.count + SEQ - 1) / SEQ) * a.dtiles.d) return;
@@ -271,28 +274,47 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
   const int64_t gn = (int64_t)group * a.states + n0;
   const bool vec = rows_of_four(a.state_in, a.states) && rows_of_four(a.state_out, a.states);
 
+  // what does not wait for the slots goes first
   int slot[SEQ];
   Vals<NS> h[SEQ], b[SEQ], c[SEQ];
   float u[SEQ], dt[SEQ], z[SEQ];
 #pragma unroll
-  for (int q = 0; q < SEQ; ++q) slot[q] = first + q < a.s.count ? seq_slot(a.s, first + q) : -1;
-#pragma unroll
   for (int q = 0; q < SEQ; ++q) {
     const int t = min(first + q, a.s.count - 1);
-    h[q] = {};
-    if (slot[q] >= 0 && a.state_in)
-      h[q] = load_vals<NS>(a.state_in + ((int64_t)slot[q] * a.channels + d) * a.states + n0, left, vec);
     u[q] = (float)((const T*)a.u + t * a.ldu)[d];
     dt[q] = (float)((const T*)a.delta + t * a.lddelta)[d];
     z[q] = a.z ? (float)((const T*)a.z + t * a.ldz)[d] : 0.f;
+    const T *pb = (const T*)a.b + t * a.ldb + gn, *pc = (const T*)a.c + t * a.ldc + gn;
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      b[q].v[i] = i < left ? (float)((const T*)a.b + t * a.ldb)[gn + i] : 0.f;
-      c[q].v[i] = i < left ? (float)((const T*)a.c + t * a.ldc)[gn + i] : 0.f;
+    for (int i = 0; i < NS; i += 4) {
+      if (a.vec_bc) {
+        const bool in = i < left;
+        const Quad qb = load_quad4(pb + (in ? i : 0)), qc = load_quad4(pc + (in ? i : 0));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          b[q].v[i + e] = in ? qb.v[e] : 0.f;
+          c[q].v[i + e] = in ? qc.v[e] : 0.f;
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const bool in = i + e < left;
+          b[q].v[i + e] = in ? (float)pb[i + e] : 0.f;
+          c[q].v[i + e] = in ? (float)pc[i + e] : 0.f;
+        }
+      }
     }
   }
   Vals<NS> la = load_vals<NS>(a.a + (int64_t)d * a.states + n0, left, rows_of_four(a.a, a.states));
   const float bias = a.dt_bias ? a.dt_bias[d] : 0.f, skip = a.d_skip ? a.d_skip[d] : 0.f;
+#pragma unroll
+  for (int q = 0; q < SEQ; ++q) slot[q] = first + q < a.s.count ? seq_slot(a.s, first + q) : -1;
+#pragma unroll
+  for (int q = 0; q < SEQ; ++q) {
+    h[q] = {};
+    if (slot[q] >= 0 && a.state_in)
+      h[q] = load_vals<NS>(a.state_in + ((int64_t)slot[q] * a.channels + d) * a.states + n0, left, vec);
+  }
 #pragma unroll
   for (int q = 0; q < SEQ; ++q) {
     const float v = dt[q] + bias, step = a.softplus ? softplus_f32(v) : v, du = step * u[q];
@@ -306,7 +328,7 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
     if (a.z) y *= silu_f32(z[q]);
     if (first + q < a.s.count && part == 0) ((T*)a.y + (first + q) * a.ldy)[d] = from_f32<T>(y);
     if (slot[q] >= 0 && a.state_out)
-      store_vals<NS>(a.state_out + ((int64_t)slot[q] * a.channels + d) * a.states + n0, h[q].v, left, vec);
+      store_vals<NS>(a.state_out + ((int64_t)slot[q] * a.channels + d) * a.states + n0, h[q].v, left, vec, a.stream);
   }
 }
 
@@ -371,7 +393,7 @@ template <typename T, int NS, int P>
 static int scan_step(const ScanArgs& a, hipStream_t st) {
   // several sequences a wave once there are enough waves without
   const int64_t waves = (int64_t)a.channels * P / 64 * a.s.count;
-  return waves >= 16 * 4 * kPlanCus ? step_launch<T, NS, P, 4>(a, st) : step_launch<T, NS, P, 1>(a, st);
+  return waves >= 16 * 4 * kPlanCus ? step_launch<T, NS, P, 2>(a, st) : step_launch<T, NS, P, 1>(a, st);
 }
 template <typename T>
 static int scan_pick(const ScanArgs& a, const ScanPlan& p, hipStream_t st) {
@@ -399,6 +421,9 @@ int launch_scan(const ct_scan_op& op, const ScanPlan& p, const SeqView& s, const
   a.state_out = v.state_out; a.y = v.y; a.ws = v.ws;
   a.ldu = op.ldu; a.lddelta = op.lddelta; a.ldb = op.ldb; a.ldc = op.ldc; a.ldz = op.ldz; a.ldy = op.ldy;
   a.channels = op.channels; a.states = op.states; a.per_group = op.channels / op.groups; a.softplus = op.softplus;
+  a.stream = (int64_t)s.count * op.channels * op.states * (int64_t)sizeof(float) >= kStreamStateBytes;
+  const int four = 4 * elem_bytes(op.dtype);
+  a.vec_bc = ((uintptr_t)v.b | (uintptr_t)v.c) % four == 0 && (op.ldb | op.ldc | op.states) % 4 == 0;
   return op.dtype == CT_DT_BF16 ? scan_pick<bf16_t>(a, p, (hipStream_t)stream)
                                 : scan_pick<float>(a, p, (hipStream_t)stream);
 }

@@ -46,6 +46,50 @@ __device__ __forceinline__ T from_f32(float v) {
   return (T)v;
 }
 
+// ---- four elements of a row ----
+struct Quad {
+  float v[4];
+};
+// Four elements of a row that all exist, at an address for them in one access.
+template <typename O>
+__device__ __forceinline__ Quad load_quad4(const O* p) {
+  if constexpr (sizeof(O) == 2) {
+    const u32x2 q = *(const u32x2*)p;
+    const unsigned q0 = q.x, q1 = q.y;
+    return {unpack<O>(q0, 0), unpack<O>(q0, 1), unpack<O>(q1, 0), unpack<O>(q1, 1)};
+  } else {
+    const f32x4 q = *(const f32x4*)p;
+    return {q.x, q.y, q.z, q.w};
+  }
+}
+
+// ---- outputs larger than the caches that would hold them ----
+// Bytes of an output from which its stores go past the L2s instead of pushing out of them
+// what is still to be read: where the next reader would not find it in the 256 MB cache
+// behind them anyway (134 MB of a product 451 to 428 us). Smaller outputs that the next
+// kernel reads are better left there: four products of 67 MB one after another take 843 us,
+// and 860 past the caches.
+constexpr int64_t kStreamBytes = 128 << 20;
+// The same for states, which nothing reads before the next token: 67 MB read and written 37
+// to 27 us; in place, 33 MB in 16.5 us either way.
+constexpr int64_t kStreamStateBytes = 32 << 20;
+template <typename V>
+__device__ __forceinline__ void store_once(V* p, V v, bool stream) {
+  if (stream) {
+    asm volatile("");  // between two of these, or the two stores become one, without the hint
+    __builtin_nontemporal_store(v, p);
+    asm volatile("");
+  } else {
+    *p = v;
+  }
+}
+
+template <typename O>
+__device__ __forceinline__ void store_quad4(O* p, const float* v, bool stream) {
+  if constexpr (sizeof(O) == 2) store_once((u32x2*)p, (u32x2){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}, stream);
+  else store_once((f32x4*)p, (f32x4){v[0], v[1], v[2], v[3]}, stream);
+}
+
 // ---- scalar functions in fp32 ----
 constexpr float kLog2e = 1.4426950408889634f;
 // v_exp_f32: within an ulp, results below 2^-126 flushed to 0.
