@@ -64,6 +64,8 @@ struct Pack {
 
 template <typename T, int W, int VEC, int U>
 __global__ void __launch_bounds__(256) causal_conv_kernel(ConvArgs a) {
+  // a sequence's second tile reads no row before the sequence
+  static_assert(U == 1 || U >= W - 1, "one token: of sequences that have no second tile");
   using P = Pack<T, VEC>;
   // a block has four tiles of the same 64 VEC channels, whose weights it lays out by tap
   __shared__ __align__(16) float sw[W][64 * VEC];
@@ -158,7 +160,9 @@ static int conv_pick(const ConvArgs& a, bool wide, hipStream_t st) {
   // shorter tiles where those of eight tokens are fewer than one wave for every SIMD: 1020
   // tokens of 2048 channels 6.9 to 5.9 us (8192 of 4096: 34.1 and 34.3)
   const int64_t waves = (int64_t)(a.s.tokens / 8) * ((a.channels + 64 * V - 1) / (64 * V));
-  return waves < 4 * kPlanCus ? conv_launch<T, W, V, 4>(a, st) : conv_launch<T, W, V, 8>(a, st);
+  if constexpr (W <= 5)
+    if (waves < 4 * kPlanCus) return conv_launch<T, W, V, 4>(a, st);
+  return conv_launch<T, W, V, 8>(a, st);
 }
 template <typename T>
 static int conv_pick_width(const ConvArgs& a, int width, bool wide, hipStream_t st) {

@@ -138,30 +138,23 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs a) {
 // Byte offset past every operand tile: reads as 0.
 constexpr unsigned kOobGroup = 0xFFFFFFF0u;
 
-__device__ __forceinline__ u32x4 load_quad(__amdgpu_buffer_rsrc_t r, unsigned off) {
-  return __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0);
-}
-// A group at any element's address: the words around it, and, once they have arrived, the
-// group itself, shifted where it starts in the middle of a word, with all but its first
+// A group of bf16 at any element's address: the words around it, and, once they have arrived,
+// the group itself, shifted where it starts in the middle of a word, with all but its first
 // `left` elements masked to 0.
-template <typename T>
-struct RawQuad {
+struct RawGroup {
   u32x4 q;
-  unsigned next;  // the fifth word of a group of bf16
+  unsigned next;  // the fifth word
   __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, unsigned off) {
-    q = load_quad(r, off & ~3u);
-    if constexpr (sizeof(T) == 2) next = __builtin_amdgcn_raw_buffer_load_b32(r, (int)((off & ~3u) + 16), 0, 0);
+    q = __builtin_amdgcn_raw_buffer_load_b128(r, (int)(off & ~3u), 0, 0);
+    next = __builtin_amdgcn_raw_buffer_load_b32(r, (int)((off & ~3u) + 16), 0, 0);
   }
   __device__ __forceinline__ u32x4 get(unsigned off, int left) const {
     unsigned v[5] = {q.x, q.y, q.z, q.w, next};
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if constexpr (sizeof(T) == 4) {
-        v[i] = left > i ? v[i] : 0;
-      } else {
-        v[i] = __builtin_amdgcn_alignbit(v[i + 1], v[i], (off & 2u) * 8);
-        v[i] = left > 2 * i + 1 ? v[i] : left > 2 * i ? v[i] & 0xFFFFu : 0;
-      }
+    for (int i = 0; i < 4; ++i) {
+      v[i] = __builtin_amdgcn_alignbit(v[i + 1], v[i], (off & 2u) * 8);
+      v[i] = left > 2 * i + 1 ? v[i] : left > 2 * i ? v[i] & 0xFFFFu : 0;
+    }
     return (u32x4){v[0], v[1], v[2], v[3]};
   }
 };
@@ -181,16 +174,23 @@ __device__ __forceinline__ RowsView rows_view(const void* p, int64_t ld, int r0,
   return {(const void*)(at - odd), (unsigned)bytes, odd};
 }
 
+// One wave instruction: lane i copies BYTES bytes at byte offset off + k of r to lds + BYTES i.
+template <int BYTES>
+__device__ __forceinline__ void copy_lds(__amdgpu_buffer_rsrc_t r, char* lds, unsigned off, int k) {
+  if constexpr (BYTES == 4) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)lds, 4, (int)off, k, 0, 0);
+  else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)lds, 16, (int)off, k, 0, 0);
+}
+
 // ------------------------------------------------------------------ tiles
 // A block computes BM x BN outputs with WK teams of WM x WN waves, each team every WK-th
 // slice of 128 bytes of each operand row: where the tile is small, a slice's products take
 // less time than the waits around them. Slices go through STAGES buffers in LDS, the later
 // ones in flight while one is multiplied; the 16-byte groups of a row are permuted by its
 // number, so that the 16 rows of a fragment lie in distinct banks.
-template <typename T, int BM, int BN, int WM, int WN, int WK, int STAGES, bool DIRECT>
+template <typename T, int BM, int BN, int WM, int WN, int WK, int STAGES, int COPY>
 __global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearArgs a) {
   constexpr int WAVES = WM * WN, ROWS = BM + BN, G = 16 / (int)sizeof(T), ROWB = 128, NG = ROWB / 16;
-  constexpr int KC = NG * G, RPC = 64 / NG;  // elements of a slice, rows of one copy
+  constexpr int KC = NG * G, LPR = COPY == 4 ? 32 : 8, RPC = 64 / LPR;  // elements of a slice, lanes of a row, rows of a copy
   constexpr int NC = ROWS / RPC / WAVES, NW = BN / RPC / WAVES;  // copies of a wave, those of w first
   constexpr int TM = BM / WM / 16, TN = BN / WN / 16, STAGE = WK * ROWS * ROWB;
   static_assert(BN % (RPC * WAVES) == 0 && BM % (RPC * WAVES) == 0, "every wave copies as many rows");
@@ -215,35 +215,39 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearAr
 
   const RowsView vw = rows_view<T>(a.w, a.ldw, n0, a.n, BN, a.k), vx = rows_view<T>(a.x, a.ldx, m0, a.m, BM, a.k);
   const __amdgpu_buffer_rsrc_t rw = make_rsrc(vw.base, vw.bytes), rx = make_rsrc(vx.base, vx.bytes);
-  unsigned off[NC];  // of this lane's group in each copy
+  // Copy i of a wave: RPC whole rows, lane by lane in LDS, so that the permutation of a row's
+  // groups is one of the addresses that its lanes read. `first`: a lane's first element in
+  // the slice.
+  constexpr int EACH = (COPY == 4 ? 4 : 16) / (int)sizeof(T), BYTES = RPC * ROWB;
+  auto row_of = [&](int i) { return ((i < NW ? i : i - NW) * WAVES + wave) * RPC + lane / LPR; };
+  auto first = [&](int i) {
+    const int key = (row_of(COPY == 4 ? i : 0) >> 1) & (NG - 1);  // of eight rows each: the same for every copy
+    return ((lane % LPR) ^ (COPY == 4 ? key * 4 : key)) * EACH;
+  };
+  static_assert(COPY == 4 || (WAVES * RPC >> 1) % NG == 0, "");
+  unsigned off[NC];
 #pragma unroll
   for (int i = 0; i < NC; ++i) {
-    const int r = ((i < NW ? i : i - NW) * WAVES + wave) * RPC + lane / NG;
-    const int g = (lane % NG) ^ ((r >> 1) & (NG - 1));
+    const int r = row_of(i);
     const bool ok = i < NW ? n0 + r < a.n : m0 + r < a.m;
     const unsigned ld = (unsigned)((i < NW ? a.ldw : a.ldx) * (int)sizeof(T));
-    off[i] = ok ? (unsigned)r * ld + 16u * g + (i < NW ? vw.odd : vx.odd) : kOobGroup;
+    off[i] = ok ? (unsigned)r * ld + (unsigned)(first(i) * (int)sizeof(T)) + (i < NW ? vw.odd : vx.odd) : kOobGroup;
   }
-  // first element of the lane's group in copy i: rows of copies differ by multiples of 8 or 16
-  const int grp_k = ((lane % NG) ^ (((wave * RPC + lane / NG) >> 1) & (NG - 1))) * G;
-  static_assert((WAVES * RPC >> 1) % NG == 0, "every copy of a lane has the same group");
 
-  constexpr int RING = DIRECT ? 1 : NC <= 4 ? 4 : 2;  // slices on their way through registers
-  RawQuad<T> held[RING][DIRECT ? 1 : NC];
+  constexpr int RING = COPY ? 1 : NC <= 4 ? 4 : 2;  // slices on their way through registers
+  RawGroup held[RING][COPY ? 1 : NC];
   auto fetch = [&](int c, int stage) __attribute__((always_inline)) {
     const int k0 = k_begin + (c * WK + team) * KC;
-    const int left = k_end - k0 - grp_k;  // elements from the lane's group on
-    char* dst = lds + stage * STAGE + team * ROWS * ROWB + wave * 1024;
+    char* dst = lds + stage * STAGE + team * ROWS * ROWB + wave * BYTES;
     auto go = [&](auto tail) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
-        if constexpr (DIRECT) {
-          const unsigned o = tail.value && left <= 0 ? kOobGroup : off[i];
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(i < NW ? rw : rx, (lds_void_t*)(dst + i * WAVES * 1024), 16, (int)o,
-                                                   k0 * (int)sizeof(T), 0, 0);
+        const bool out = tail.value && k0 + first(i) >= k_end;
+        if constexpr (COPY > 0) {
+          copy_lds<COPY>(i < NW ? rw : rx, dst + i * WAVES * BYTES, out ? kOobGroup : off[i], k0 * (int)sizeof(T));
         } else {
-          const unsigned o = off[i] == kOobGroup || left <= 0 ? kOobGroup : off[i] + (unsigned)(k0 * (int)sizeof(T));
-          held[stage][i].load(i < NW ? rw : rx, o);
+          held[stage][i].load(i < NW ? rw : rx,
+                              off[i] == kOobGroup || out ? kOobGroup : off[i] + (unsigned)(k0 * (int)sizeof(T)));
         }
       }
     };
@@ -251,11 +255,12 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearAr
     else go(std::true_type{});
   };
   auto put = [&](int c, int u) __attribute__((always_inline)) {
-    const int left = k_end - (k_begin + (c * WK + team) * KC) - grp_k;
+    const int k0 = k_begin + (c * WK + team) * KC;
 #pragma unroll
     for (int i = 0; i < NC; ++i)
-      if constexpr (!DIRECT)
-        *(u32x4*)(lds + (u & 1) * STAGE + team * ROWS * ROWB + (i * WAVES + wave) * 1024 + lane * 16) = held[u][i].get(off[i], left);
+      if constexpr (COPY == 0)
+        *(u32x4*)(lds + (u & 1) * STAGE + team * ROWS * ROWB + (i * WAVES + wave) * BYTES + lane * 16) =
+            held[u][i].get(off[i], k_end - k0 - first(i));
   };
 
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
@@ -280,7 +285,7 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearAr
     }
   };
 
-  if constexpr (DIRECT) {
+  if constexpr (COPY > 0) {
     // Slices past the end read 0, so that STAGES - 1 of them are in flight at every wait. The
     // barrier also says that every wave has read the stage that is filled next.
     if (chunks > 0) {
@@ -299,7 +304,7 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearAr
   } else {
     // The barrier of a slice says that every wave has read the one before it, whose stage the
     // next slice goes to.
-    static_assert(DIRECT || (STAGES == 2 && RING % 2 == 0), "");
+    static_assert(COPY > 0 || (STAGES == 2 && RING % 2 == 0), "");
 #pragma unroll
     for (int u = 0; u < RING; ++u) fetch(u, u);
     for (int c = 0; c < chunks; c += RING) {
@@ -441,42 +446,42 @@ LinearPlan plan_linear(const ct_linear_op& op) {
   return p;
 }
 
-template <typename T, bool DIRECT, int KIND>
+template <typename T, int COPY, int KIND>
 static int launch_tile(LinearArgs a, hipStream_t st) {
   constexpr TileShape t = kTiles[KIND];
-  constexpr int S = DIRECT ? t.stages : 2;
+  constexpr int S = COPY ? t.stages : 2;
   a.tiles_m = (a.m + t.bm - 1) / t.bm;
   a.tiles_n = (a.n + t.bn - 1) / t.bn;
   const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
   if (tiles > 0x7FFFFFFF || 4 * (int64_t)a.tiles_m > 0x7FFFFFFF) return refuse_size("ct_linear_run");
   a.dgroup = make_fastdiv(4 * (int64_t)a.tiles_m);
   a.dlast = make_fastdiv(a.tiles_n % 4 ? a.tiles_n % 4 : 4);
-  hipLaunchKernelGGL((linear_tile_kernel<T, t.bm, t.bn, t.wm, t.wn, t.wk, S, DIRECT>),
+  hipLaunchKernelGGL((linear_tile_kernel<T, t.bm, t.bn, t.wm, t.wn, t.wk, S, COPY>),
                      dim3((unsigned)tiles, (unsigned)a.split), dim3(64 * t.wm * t.wn * t.wk),
                      S * t.wk * (t.bm + t.bn) * 128, st, a);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }
-template <typename T, bool DIRECT>
+template <typename T, int COPY>
 static int linear_pick(const LinearArgs& a, int kind, hipStream_t st) {
-  if constexpr (DIRECT) {
-    switch (kind) {
-      case LIN_32: return launch_tile<T, DIRECT, LIN_32>(a, st);
-      case LIN_32_TWO: return launch_tile<T, DIRECT, LIN_32_TWO>(a, st);
-      case LIN_64X32: return launch_tile<T, DIRECT, LIN_64X32>(a, st);
-      case LIN_64: return launch_tile<T, DIRECT, LIN_64>(a, st);
-      case LIN_64_TWO: return launch_tile<T, DIRECT, LIN_64_TWO>(a, st);
-      case LIN_128: return launch_tile<T, DIRECT, LIN_128>(a, st);
-      default: return launch_tile<T, DIRECT, LIN_256>(a, st);
-    }
-  } else {  // two stages whatever the tile
-    switch (kind) {
-      case LIN_32:
-      case LIN_32_TWO: return launch_tile<T, DIRECT, LIN_32>(a, st);
-      case LIN_64X32:
-      case LIN_64:
-      case LIN_64_TWO: return launch_tile<T, DIRECT, LIN_64_TWO>(a, st);
-      default: return launch_tile<T, DIRECT, LIN_128>(a, st);
-    }
+  switch (kind) {
+    case LIN_32: return launch_tile<T, COPY, LIN_32>(a, st);
+    case LIN_32_TWO: return launch_tile<T, COPY, LIN_32_TWO>(a, st);
+    case LIN_64X32: return launch_tile<T, COPY, LIN_64X32>(a, st);
+    case LIN_64: return launch_tile<T, COPY, LIN_64>(a, st);
+    case LIN_64_TWO: return launch_tile<T, COPY, LIN_64_TWO>(a, st);
+    case LIN_128: return launch_tile<T, COPY, LIN_128>(a, st);
+    default: return launch_tile<T, COPY, LIN_256>(a, st);
+  }
+}
+// Through registers a tile has two stages whatever its plan, and 256 x 256 has no room.
+static int linear_pick_odd(const LinearArgs& a, int kind, hipStream_t st) {
+  switch (kind) {
+    case LIN_32:
+    case LIN_32_TWO: return launch_tile<bf16_t, 0, LIN_32>(a, st);
+    case LIN_64X32:
+    case LIN_64:
+    case LIN_64_TWO: return launch_tile<bf16_t, 0, LIN_64_TWO>(a, st);
+    default: return launch_tile<bf16_t, 0, LIN_128>(a, st);
   }
 }
 
@@ -492,14 +497,17 @@ int launch_linear(const ct_linear_op& op, const LinearPlan& p, const void* x, co
   const int e = elem_bytes(op.dtype), four = 4 * elem_bytes(op.out_dtype);
   a.vec_out = (uintptr_t)y % four == 0 && op.ldy % 4 == 0 && (uintptr_t)bias % 16 == 0 &&
               (!op.res || ((uintptr_t)res % four == 0 && op.ldr % 4 == 0));
-  const bool direct = ((uintptr_t)x | (uintptr_t)w) % 16 == 0 && op.ldx * e % 16 == 0 && op.ldw * e % 16 == 0 &&
-                      op.k * (int64_t)e % 16 == 0;
+  // What rows of both operands lie on, and end on, decides how they are copied: 16 bytes a
+  // lane, a word a lane, or (bf16 only) through registers
+  const int64_t on = (int64_t)((uintptr_t)x | (uintptr_t)w) | op.ldx * e | op.ldw * e | op.k * (int64_t)e;
   hipStream_t st = (hipStream_t)stream;
   int rc;
-  if (op.dtype == CT_DT_BF16)
-    rc = direct ? linear_pick<bf16_t, true>(a, p.kind, st) : linear_pick<bf16_t, false>(a, p.kind, st);
+  if (op.dtype == CT_DT_F32)
+    rc = on % 16 == 0 ? linear_pick<float, 16>(a, p.kind, st) : linear_pick<float, 4>(a, p.kind, st);
   else
-    rc = direct ? linear_pick<float, true>(a, p.kind, st) : linear_pick<float, false>(a, p.kind, st);
+    rc = on % 16 == 0  ? linear_pick<bf16_t, 16>(a, p.kind, st)
+         : on % 4 == 0 ? linear_pick<bf16_t, 4>(a, p.kind, st)
+                       : linear_pick_odd(a, p.kind, st);
   if (rc || p.split == 1) return rc;
   const int64_t quads = (int64_t)op.m * ((op.n + 3) / 4);
   hipLaunchKernelGGL(linear_join_kernel, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a);
