@@ -22,7 +22,6 @@ struct LinearArgs {
   int64_t ldx, ldw, ldr, ldy;
   int act, res_mode, out_bf16;
   int stream;           // y goes past the caches
-  int vec_out;          // rows of y and r take accesses of four elements
   int tiles_m, tiles_n;
   int split, per_split; // slices of the reduction, elements in each (whole 128-byte chunks)
   FastDiv dgroup, dlast;
@@ -53,10 +52,7 @@ __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 acc) {
 __device__ __forceinline__ Quad load_bias(const LinearArgs& a, int j) {
   Quad q = {};
   if (!a.bias || j >= a.n) return q;
-  if (a.vec_out && j + 4 <= a.n) {
-    const f32x4 b = *(const f32x4*)(a.bias + j);
-    return {b.x, b.y, b.z, b.w};
-  }
+  if (j + 4 <= a.n) return load_quad4(a.bias + j);
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     if (j + e < a.n) q.v[e] = a.bias[j + e];
@@ -66,7 +62,7 @@ __device__ __forceinline__ Quad load_res(const LinearArgs& a, int i, int j) {
   Quad q = {};
   if (!a.res_mode || i >= a.m || j >= a.n) return q;
   const int64_t at = i * a.ldr + j;
-  if (a.vec_out && j + 4 <= a.n)
+  if (j + 4 <= a.n)
     return a.out_bf16 ? load_quad4((const bf16_t*)a.res + at) : load_quad4((const float*)a.res + at);
 #pragma unroll
   for (int e = 0; e < 4; ++e)
@@ -98,7 +94,7 @@ __device__ __forceinline__ void store4(const LinearArgs& a, int i, int j, f32x4 
   const Quad res[1] = {r};
   finish(a, v, bias, res);
   const int64_t at = i * a.ldy + j;
-  if (a.vec_out && j + 4 <= a.n) {
+  if (j + 4 <= a.n) {
     if (a.out_bf16) store_quad4((bf16_t*)a.y + at, v[0], false);
     else store_quad4((float*)a.y + at, v[0], false);
     return;
@@ -350,7 +346,7 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearAr
   char* mine = lds + wave * (H * RN * 4);
   auto slot = [](int r, int s) { return (s ^ ((SLOTS >= 16 ? r : r >> 1) & (SLOTS - 1))) * 16; };
   const int sl = lane % SLOTS, col = n0 + wn + sl * 4, r0 = lane / SLOTS;
-  const bool whole = a.vec_out && m0 + BM <= a.m && n0 + BN <= a.n;  // no output of the tile is missing
+  const bool whole = m0 + BM <= a.m && n0 + BN <= a.n;  // no output of the tile is missing
   const Quad bias = a.split > 1 ? Quad{} : load_bias(a, col);
   constexpr int ROWS_EACH = H / STEP, Q = ROWS_EACH % 4 ? ROWS_EACH : 4;  // rows of a lane, and at a time
   auto take = [&](int r) { return *(const f32x4*)(mine + r * RN * 4 + slot(r, sl)); };
@@ -405,13 +401,13 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearAr
 // ------------------------------------------------------------------ plans and launches
 // Tiles, from small to large. Of the two of a size the second leaves room for a second block
 // on the compute unit.
-enum { LIN_32, LIN_32_TWO, LIN_64X32, LIN_64, LIN_64_TWO, LIN_128, LIN_256, LIN_KINDS };
+enum { LIN_32, LIN_32_TWO, LIN_64X32, LIN_32X64, LIN_64, LIN_64_TWO, LIN_128, LIN_256, LIN_KINDS };
 struct TileShape {
   int bm, bn, wm, wn, wk, stages;
 };
-constexpr TileShape kTiles[LIN_KINDS] = {{32, 32, 1, 2, 4, 3}, {32, 32, 1, 2, 4, 2},     {64, 32, 2, 2, 4, 3},
-                                         {64, 64, 2, 2, 2, 3}, {64, 64, 2, 2, 1, 4},     {128, 128, 2, 2, 1, 2},
-                                         {256, 256, 4, 2, 1, 2}};
+constexpr TileShape kTiles[LIN_KINDS] = {{32, 32, 1, 2, 4, 3}, {32, 32, 1, 2, 4, 2},   {64, 32, 2, 2, 4, 3},
+                                         {32, 64, 1, 4, 1, 3}, {64, 64, 2, 2, 2, 3},   {64, 64, 2, 2, 1, 4},
+                                         {128, 128, 2, 2, 1, 2}, {256, 256, 4, 2, 1, 2}};
 
 static int64_t tiles_of(const ct_linear_op& op, int kind) {
   const TileShape t = kTiles[kind];
@@ -431,6 +427,9 @@ LinearPlan plan_linear(const ct_linear_op& op) {
   const int64_t enough = kPlanCus * 3 / 4;
   if (p.kind == LIN_64 && tiles_of(op, LIN_64) < enough)
     p.kind = tiles_of(op, LIN_64X32) >= enough ? LIN_64X32 : LIN_32;
+  // fp32 is bound by the matrix cores at this size too: half the tile where its rounds are fewer
+  else if (p.kind == LIN_64 && op.dtype == CT_DT_F32 && 0.52 * rounds(LIN_32X64) < rounds(LIN_64))
+    p.kind = LIN_32X64;
   if (op.m <= 32) p.kind = LIN_32;
   if (p.kind == LIN_64 && tiles_of(op, LIN_64) > kPlanCus) p.kind = LIN_64_TWO;
   if (p.kind == LIN_32 && tiles_of(op, LIN_32) > kPlanCus) p.kind = LIN_32_TWO;
@@ -467,6 +466,8 @@ static int linear_pick(const LinearArgs& a, int kind, hipStream_t st) {
     case LIN_32: return launch_tile<T, COPY, LIN_32>(a, st);
     case LIN_32_TWO: return launch_tile<T, COPY, LIN_32_TWO>(a, st);
     case LIN_64X32: return launch_tile<T, COPY, LIN_64X32>(a, st);
+    case LIN_32X64:
+      if constexpr (sizeof(T) == 4) return launch_tile<T, COPY, LIN_32X64>(a, st);
     case LIN_64: return launch_tile<T, COPY, LIN_64>(a, st);
     case LIN_64_TWO: return launch_tile<T, COPY, LIN_64_TWO>(a, st);
     case LIN_128: return launch_tile<T, COPY, LIN_128>(a, st);
@@ -494,9 +495,7 @@ int launch_linear(const ct_linear_op& op, const LinearPlan& p, const void* x, co
   a.act = op.act; a.res_mode = op.res; a.out_bf16 = op.out_dtype == CT_DT_BF16;
   a.split = p.split; a.per_split = p.per_split;
   a.stream = (int64_t)op.m * op.n * elem_bytes(op.out_dtype) >= kStreamBytes;
-  const int e = elem_bytes(op.dtype), four = 4 * elem_bytes(op.out_dtype);
-  a.vec_out = (uintptr_t)y % four == 0 && op.ldy % 4 == 0 && (uintptr_t)bias % 16 == 0 &&
-              (!op.res || ((uintptr_t)res % four == 0 && op.ldr % 4 == 0));
+  const int e = elem_bytes(op.dtype);
   // What rows of both operands lie on, and end on, decides how they are copied: 16 bytes a
   // lane, a word a lane, or (bf16 only) through registers
   const int64_t on = (int64_t)((uintptr_t)x | (uintptr_t)w) | op.ldx * e | op.ldw * e | op.k * (int64_t)e;

@@ -50,15 +50,17 @@ __device__ __forceinline__ T from_f32(float v) {
 struct Quad {
   float v[4];
 };
-// Four elements of a row that all exist, at an address for them in one access.
+// Four elements of a row that all exist, in one access wherever the row lies.
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
 template <typename O>
 __device__ __forceinline__ Quad load_quad4(const O* p) {
   if constexpr (sizeof(O) == 2) {
-    const u32x2 q = *(const u32x2*)p;
+    const u32x2 q = *(const u32x2_any*)p;
     const unsigned q0 = q.x, q1 = q.y;
     return {unpack<O>(q0, 0), unpack<O>(q0, 1), unpack<O>(q1, 0), unpack<O>(q1, 1)};
   } else {
-    const f32x4 q = *(const f32x4*)p;
+    const f32x4 q = *(const f32x4_any*)p;
     return {q.x, q.y, q.z, q.w};
   }
 }
@@ -73,8 +75,8 @@ constexpr int64_t kStreamBytes = 128 << 20;
 // The same for states, which nothing reads before the next token: 67 MB read and written 37
 // to 27 us; in place, 33 MB in 16.5 us either way.
 constexpr int64_t kStreamStateBytes = 32 << 20;
-template <typename V>
-__device__ __forceinline__ void store_once(V* p, V v, bool stream) {
+template <typename P, typename V>
+__device__ __forceinline__ void store_once(P* p, V v, bool stream) {
   if (stream) {
     asm volatile("");  // between two of these, or the two stores become one, without the hint
     __builtin_nontemporal_store(v, p);
@@ -86,8 +88,8 @@ __device__ __forceinline__ void store_once(V* p, V v, bool stream) {
 
 template <typename O>
 __device__ __forceinline__ void store_quad4(O* p, const float* v, bool stream) {
-  if constexpr (sizeof(O) == 2) store_once((u32x2*)p, (u32x2){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}, stream);
-  else store_once((f32x4*)p, (f32x4){v[0], v[1], v[2], v[3]}, stream);
+  if constexpr (sizeof(O) == 2) store_once((u32x2_any*)p, (u32x2){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}, stream);
+  else store_once((f32x4_any*)p, (f32x4){v[0], v[1], v[2], v[3]}, stream);
 }
 
 // ---- scalar functions in fp32 ----
