@@ -406,7 +406,7 @@ struct TileShape {
   int bm, bn, wm, wn, wk, stages;
 };
 constexpr TileShape kTiles[LIN_KINDS] = {{32, 32, 1, 2, 4, 3}, {32, 32, 1, 2, 4, 2},   {64, 32, 2, 2, 4, 3},
-                                         {32, 64, 1, 4, 1, 3}, {64, 64, 2, 2, 2, 3},   {64, 64, 2, 2, 1, 4},
+                                         {32, 64, 1, 4, 1, 3}, {64, 64, 2, 2, 2, 3},   {64, 64, 2, 2, 1, 3},
                                          {128, 128, 2, 2, 1, 2}, {256, 256, 4, 2, 1, 2}};
 
 static int64_t tiles_of(const ct_linear_op& op, int kind) {

@@ -217,19 +217,20 @@ __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
   }
 }
 
-// h at the start of every chunk, in place of h at its end from 0. A thread has one state of
-// one channel; the loads of eight chunks are on their way together. An empty sequence hands
-// its state on.
-__global__ void __launch_bounds__(256) scan_carry_kernel(ScanArgs a) {
+// h at the start of every chunk, in place of h at its end from 0. A lane has one state of one
+// channel; the loads of the next eight to 16 chunks are on their way while it walks (with
+// eight and none ahead 256 chunks of 32768 states took 34 us, 13 % of their scan; now 20).
+// An empty sequence hands its state on.
+__global__ void __launch_bounds__(64) scan_carry_kernel(ScanArgs a) {
   const int64_t per_seq = (int64_t)a.channels * a.states;
-  const int blocks = (int)((per_seq + 255) / 256);
+  const int blocks = (int)((per_seq + 63) / 64);
   const int s = (int)(blockIdx.x / blocks);
-  const int64_t e = (int64_t)(blockIdx.x % blocks) * 256 + threadIdx.x;
+  const int64_t e = (int64_t)(blockIdx.x % blocks) * 64 + threadIdx.x;
   if (e >= per_seq) return;
   const int d = (int)(e / a.states);
   const SeqRange r = seq_range(a.s, s);
   const int slot = seq_slot(a.s, s);
-  const int n = (r.end - r.begin + a.chunk - 1) / a.chunk;
+  const int n = __builtin_amdgcn_readfirstlane((r.end - r.begin + a.chunk - 1) / a.chunk);
   const int64_t id = a.s.offsets ? r.begin / a.chunk + s : (int64_t)s * a.per;
   float h = slot >= 0 && a.state_in ? a.state_in[(int64_t)slot * per_seq + e] : 0.f;
   if (n == 0) {
@@ -240,21 +241,33 @@ __global__ void __launch_bounds__(256) scan_carry_kernel(ScanArgs a) {
   float* p = a.ws + id * per_seq + e;
   const float* dt = a.ws_dt + id * a.channels + d;
   constexpr int F = 8;
-  for (int c = 0; c < n; c += F) {
-    float end[F], sum[F];
+  float end[2][F], sum[2][F];
+  auto fetch = [&](int u, int c) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < F; ++i) {
-      const int k = min(c + i, max(n - 2, 0));  // the last chunk's end is nobody's start
-      end[i] = n > 1 ? p[(int64_t)k * per_seq] : 0.f;
-      sum[i] = n > 1 ? dt[(int64_t)k * a.channels] : 0.f;
+      const int k = min(c + i, n - 2);  // the last chunk's end is nobody's start
+      end[u][i] = p[(int64_t)k * per_seq];
+      sum[u][i] = dt[(int64_t)k * a.channels];
     }
+  };
+  auto walk = [&](int u, int c) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < F; ++i)
-      if (c + i < n) {
+      if (c + i < n - 1) {
         p[(int64_t)(c + i) * per_seq] = h;
-        h = fmaf(__builtin_amdgcn_exp2f(la * sum[i]), h, end[i]);
+        h = fmaf(__builtin_amdgcn_exp2f(la * sum[u][i]), h, end[u][i]);
       }
+  };
+  if (n > 1) {
+    fetch(0, 0);
+    for (int c = 0; c < n - 1; c += 2 * F) {
+      fetch(1, c + F);
+      walk(0, c);
+      fetch(0, c + 2 * F);
+      walk(1, c + F);
+    }
   }
+  p[(int64_t)(n - 1) * per_seq] = h;
 }
 
 // ------------------------------------------------------------------ single tokens
@@ -340,11 +353,13 @@ ScanPlan plan_scan(const ct_scan_op& op, const ct_sequences& s) {
   ScanPlan p = {};
   if (!s.tokens) return p;
   const int most = s.offsets ? (s.max_len ? (s.max_len < s.tokens ? s.max_len : s.tokens) : s.tokens) : s.tokens / s.count;
-  // waves of a chunk, chunks for three waves on every SIMD, tokens of a chunk in whole stages
+  // Waves of a chunk, and as many tokens in it as leave eight blocks of four waves for every
+  // compute unit: those at work together take turns evenly, and the last ones are short (a
+  // third of them: 8192 ragged tokens of 4096 channels 246 to 275 us). Whole stages of 32.
   const int ch = 64 / prompt_parts(op.states), per_group = op.channels / op.groups;
   const int64_t waves = (int64_t)op.groups * ((per_group + ch - 1) / ch);
-  int64_t chunk = ((int64_t)s.tokens * waves / (3 * 4 * kPlanCus) + 31) / 32 * 32;
-  if (chunk < 64) chunk = 64;
+  int64_t chunk = ((int64_t)s.tokens * waves / (8 * 4 * kPlanCus) + 16) / 32 * 32;
+  if (chunk < 32) chunk = 32;
   if (most <= 2 * chunk) return p;  // no sequence is worth cutting
   p.chunk = (int)chunk;
   p.chunks = s.offsets ? s.tokens / chunk + s.count : (int64_t)s.count * ((most + chunk - 1) / chunk);
@@ -372,9 +387,9 @@ static int scan_prompt(ScanArgs a, const ScanPlan& p, hipStream_t st) {
   a.ws_dt = a.ws + p.chunks * a.channels * a.states;
   int rc = scan_launch<T, NS, P, SCAN_SUM>(a, p.chunks, st);
   if (rc) return rc;
-  const int64_t blocks = (((int64_t)a.channels * a.states + 255) / 256) * a.s.count;
+  const int64_t blocks = (((int64_t)a.channels * a.states + 63) / 64) * a.s.count;
   if (blocks > 0x7FFFFFFF) return refuse_size("ct_scan_run");
-  hipLaunchKernelGGL(scan_carry_kernel, dim3((unsigned)blocks), dim3(256), 0, st, a);
+  hipLaunchKernelGGL(scan_carry_kernel, dim3((unsigned)blocks), dim3(64), 0, st, a);
   if (hipGetLastError() != hipSuccess) return -1;
   return scan_launch<T, NS, P, SCAN_OUT>(a, p.chunks, st);
 }
