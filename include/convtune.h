@@ -538,8 +538,8 @@ int ct_test_xcd_band(int tiles, int32_t *tile_of_block);
  * need ct_init. Results do not depend on timing: the same inputs give the same
  * bits. Pointers are to device memory and aligned to their element; rows are
  * contiguous, and lie ld* elements apart. Rows and pointers at multiples of 16
- * bytes are read faster. A product's rows are at most 4 MiB apart (x, w) and
- * its sums are in fp32. */
+ * bytes are read faster. Rows of a product's x and w, and of a scan's u,
+ * delta, z and y, are at most 4 MiB apart. Sums and states are in fp32. */
 
 #define CT_ACT_NONE  0
 #define CT_ACT_RELU  1

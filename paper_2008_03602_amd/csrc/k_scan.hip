@@ -154,36 +154,57 @@ __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
       }
     }
   };
-  // the next U tokens of this lane's channel
-  T ku[U], kd[U], kz[U];
-  auto fetch_rows = [&](int t) __attribute__((always_inline)) {
+  // The next U tokens of this lane's channel, from rows that start with the stage's. Lanes that
+  // store nothing have an offset past every row.
+  constexpr int E = (int)sizeof(T);
+  const unsigned off = (unsigned)d * (unsigned)E, off_y = part == 0 && live ? off : kOob;
+  const int step_u = (int)a.ldu * E, step_d = (int)a.lddelta * E, step_z = (int)a.ldz * E, step_y = (int)a.ldy * E;
+  __amdgpu_buffer_rsrc_t ru, rd, rz, ry;
+  auto aim = [&](int t) __attribute__((always_inline)) {
+    const int rows = min(t1 - t, TT + U);
+    ru = rows_rsrc((const T*)a.u + t * a.ldu, rows, a.ldu, a.channels);
+    rd = rows_rsrc((const T*)a.delta + t * a.lddelta, rows, a.lddelta, a.channels);
+    if constexpr (MODE != SCAN_SUM) {
+      rz = rows_rsrc((const T*)a.z + t * a.ldz, a.z ? rows : 1, a.ldz, a.z ? a.channels : 0);
+      ry = rows_rsrc((const T*)a.y + t * a.ldy, rows, a.ldy, a.channels);
+    }
+  };
+  float ku[U], kd[U], kz[U];
+  auto fetch_rows = [&](int q) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-      const int64_t tok = min(t + i, t1 - 1);
-      ku[i] = ((const T*)a.u + tok * a.ldu)[d];
-      kd[i] = ((const T*)a.delta + tok * a.lddelta)[d];
-      if (MODE != SCAN_SUM && a.z) kz[i] = ((const T*)a.z + tok * a.ldz)[d];
+      ku[i] = load_elem<T>(ru, off, (q + i) * step_u);
+      kd[i] = load_elem<T>(rd, off, (q + i) * step_d);
     }
+    if (MODE != SCAN_SUM && a.z)
+#pragma unroll
+      for (int i = 0; i < U; ++i) kz[i] = load_elem<T>(rz, off, (q + i) * step_z);
   };
 
   if (t0 < t1) {
     fetch(t0);
-    fetch_rows(t0);
+    aim(t0);
+    fetch_rows(0);
     for (int t = t0, s = 0; t < t1; t += TT, s ^= 1) {
       put(s);
       __syncthreads();  // also: every wave is done with the stage before last
       if (t + TT < t1) fetch(t + TT);
+      if (t > t0) aim(t);
       auto tokens = [&](int q, auto all) __attribute__((always_inline)) {
         float dt[U], du[U], u[U], z[U];
+        auto each = [](auto f) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < U; ++i) {
-          u[i] = (float)ku[i];
-          const float v = (float)kd[i] + bias;
-          dt[i] = a.softplus ? softplus_f32(v) : v;
-          du[i] = dt[i] * u[i];
-          if constexpr (MODE != SCAN_SUM) z[i] = a.z ? silu_f32((float)kz[i]) : 1.f;
-        }
-        if (t + q + U < t1) fetch_rows(t + q + U);
+          for (int i = 0; i < U; ++i) f(i);
+        };
+        each([&](int i) {
+          u[i] = ku[i];
+          dt[i] = kd[i] + bias;
+          z[i] = 1.f;
+        });
+        if (a.softplus) each([&](int i) { dt[i] = softplus_f32(dt[i]); });
+        if (MODE != SCAN_SUM && a.z) each([&](int i) { z[i] = silu_f32(kz[i]); });
+        each([&](int i) { du[i] = dt[i] * u[i]; });
+        fetch_rows(q + U);
 #pragma unroll
         for (int i = 0; i < U; ++i) {
           if (!all.value && t + q + i >= t1) break;
@@ -197,7 +218,7 @@ __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
             total += dt[i];
           } else {
             y = fmaf(skip, u[i], add_lanes<P>(y)) * z[i];
-            if (part == 0 && live) ((T*)a.y + (int64_t)(t + q + i) * a.ldy)[d] = from_f32<T>(y);
+            store_elem<T>(ry, off_y, (q + i) * step_y, y);
           }
         }
       };

@@ -92,6 +92,29 @@ __device__ __forceinline__ void store_quad4(O* p, const float* v, bool stream) {
   else store_once((f32x4_any*)p, (f32x4){v[0], v[1], v[2], v[3]}, stream);
 }
 
+// ---- rows that lanes take an element of each ----
+// `rows` rows from `base` on, `pitch` elements apart, of `cols` elements: a lane's byte offset
+// in a row and the row's uniform one need no address arithmetic on the vector ALU. Past the
+// last row a load is 0 and a store does nothing (fewer than 2^31 bytes in all).
+template <typename T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const T* base, int rows, int64_t pitch, int cols) {
+  return make_rsrc(base, ((int64_t)(rows - 1) * pitch + cols) * (int64_t)sizeof(T));
+}
+template <typename T>
+__device__ __forceinline__ float load_elem(__amdgpu_buffer_rsrc_t r, unsigned off, int row) {
+  if constexpr (sizeof(T) == 4)
+    return __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(r, (int)off, row, 0));
+  else
+    return __builtin_bit_cast(float, (unsigned)__builtin_amdgcn_raw_buffer_load_b16(r, (int)off, row, 0) << 16);
+}
+template <typename T>
+__device__ __forceinline__ void store_elem(__amdgpu_buffer_rsrc_t r, unsigned off, int row, float v) {
+  if constexpr (sizeof(T) == 4)
+    __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), r, (int)off, row, 0);
+  else
+    __builtin_amdgcn_raw_buffer_store_b16(bf16_t(v).bits, r, (int)off, row, 0);
+}
+
 // ---- scalar functions in fp32 ----
 constexpr float kLog2e = 1.4426950408889634f;
 // v_exp_f32: within an ulp, results below 2^-126 flushed to 0.
@@ -106,8 +129,7 @@ __device__ __forceinline__ float silu_f32(float v) { return v * __builtin_amdgcn
 __device__ __forceinline__ float softplus_f32(float v) {
   const float e = exp_f32(-fabsf(v)), u = 1.f + e;
   const float l = __builtin_amdgcn_logf(u) * 0.6931471805599453f;
-  const float top = v < 0.f ? 0.f : v;  // keeps NaN
-  return top + (l + (e - (u - 1.f)));
+  return fmaxf(v, 0.f) + (l + (e - (u - 1.f)));  // NaN stays in l
 }
 // v / 2 (1 + erf(v / sqrt(2))) = v Phi(v), with the tail probability of |v| after Abramowitz
 // and Stegun, 7.1.26 (off by 7.5e-8 at most): Phi(-|v|) = t (c1 + t (c2 + ...)) exp(-v^2 / 2)

@@ -80,6 +80,9 @@ int check_scan(const ct_scan_op* op) {
   if (!pitch_ok(op->ldu, op->channels) || !pitch_ok(op->lddelta, op->channels) || !pitch_ok(op->ldb, gn) ||
       !pitch_ok(op->ldc, gn) || !pitch_ok(op->ldy, op->channels))
     return refuse(me, "row pitch shorter than the row");
+  const int64_t e = elem_bytes(op->dtype);
+  if (op->ldu * e > kMaxPitchBytes || op->lddelta * e > kMaxPitchBytes || op->ldy * e > kMaxPitchBytes)
+    return refuse(me, "rows of u, delta or y more than 4 MiB apart");
   return CT_OK;
 }
 
@@ -170,6 +173,7 @@ int ct_scan_run(const ct_scan_op* op, const ct_sequences* seqs, const void* u, c
     const char* me = "ct_scan_run";
     if (const int rc = check_scan(op)) return rc;
     if (z && !pitch_ok(op->ldz, op->channels)) return refuse(me, "row pitch shorter than the row");
+    if (z && op->ldz * elem_bytes(op->dtype) > kMaxPitchBytes) return refuse(me, "rows of z more than 4 MiB apart");
     if (const int rc = check_sequences(me, seqs, state_in || state_out)) return rc;
     if (!op->channels || !seqs->count) return CT_OK;
     if (!a || (seqs->tokens && (!u || !delta || !b || !c || !y))) return refuse(me, "null array");
