@@ -609,7 +609,7 @@ def ct_linear_workspace(op: ct_linear_op) -> int:
 
 def _ws(ws, nbytes):
     """(address, bytes) of a workspace tensor, or of an address with its size."""
-    if ws is None or isinstance(ws, int):
+    if ws is None or ws.__class__ is int:
         return ws, nbytes
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
@@ -617,13 +617,27 @@ def _ws(ws, nbytes):
 def ct_linear_run(op: ct_linear_op, x, w, bias, res, y, ws=None, stream: int = 0, ws_bytes: int = 0) -> None:
     """Enqueued on `stream` (a raw HIP stream handle, 0 = the null stream); returns without waiting."""
     ws, nbytes = _ws(ws, ws_bytes)
-    _check(lib().ct_linear_run(op, _ptr(x), _ptr(w), _ptr(bias), _ptr(res), _ptr(y), ws, nbytes, stream or None))
+    f = (_lib or lib()).ct_linear_run
+    try:  # tensors, without a call for each: a decode step is as long as its calls
+        rc = f(op, x.data_ptr(), w.data_ptr(), None if bias is None else bias.data_ptr(),
+               None if res is None else res.data_ptr(), y.data_ptr(), ws, nbytes, stream or None)
+    except AttributeError:  # addresses among them
+        rc = f(op, *map(_ptr, (x, w, bias, res, y)), ws, nbytes, stream or None)
+    if rc:
+        _check(rc)
 
 
 def ct_causal_conv_run(op: ct_causal_conv_op, seqs: ct_sequences, x, w, bias, state_in, state_out, y,
                        stream: int = 0) -> None:
-    _check(lib().ct_causal_conv_run(op, seqs, _ptr(x), _ptr(w), _ptr(bias), _ptr(state_in), _ptr(state_out), _ptr(y),
-                                    stream or None))
+    f = (_lib or lib()).ct_causal_conv_run
+    try:
+        rc = f(op, seqs, x.data_ptr(), w.data_ptr(), None if bias is None else bias.data_ptr(),
+               None if state_in is None else state_in.data_ptr(), None if state_out is None else state_out.data_ptr(),
+               y.data_ptr(), stream or None)
+    except AttributeError:
+        rc = f(op, seqs, *map(_ptr, (x, w, bias, state_in, state_out, y)), stream or None)
+    if rc:
+        _check(rc)
 
 
 def ct_scan_workspace(op: ct_scan_op, seqs: ct_sequences) -> int:
@@ -636,8 +650,17 @@ def ct_scan_workspace(op: ct_scan_op, seqs: ct_sequences) -> int:
 def ct_scan_run(op: ct_scan_op, seqs: ct_sequences, u, delta, dt_bias, a, b, c, d_skip, z, state_in, state_out, y,
                 ws=None, stream: int = 0, ws_bytes: int = 0) -> None:
     ws, nbytes = _ws(ws, ws_bytes)
-    _check(lib().ct_scan_run(op, seqs, _ptr(u), _ptr(delta), _ptr(dt_bias), _ptr(a), _ptr(b), _ptr(c), _ptr(d_skip),
-                             _ptr(z), _ptr(state_in), _ptr(state_out), _ptr(y), ws, nbytes, stream or None))
+    f = (_lib or lib()).ct_scan_run
+    try:
+        rc = f(op, seqs, u.data_ptr(), delta.data_ptr(), None if dt_bias is None else dt_bias.data_ptr(), a.data_ptr(),
+               b.data_ptr(), c.data_ptr(), None if d_skip is None else d_skip.data_ptr(),
+               None if z is None else z.data_ptr(), None if state_in is None else state_in.data_ptr(),
+               None if state_out is None else state_out.data_ptr(), y.data_ptr(), ws, nbytes, stream or None)
+    except AttributeError:
+        rc = f(op, seqs, *map(_ptr, (u, delta, dt_bias, a, b, c, d_skip, z, state_in, state_out, y)), ws, nbytes,
+               stream or None)
+    if rc:
+        _check(rc)
 
 
 def header_functions(header_path: Optional[str] = None) -> List[str]:

@@ -148,7 +148,7 @@ static int conv_launch(ConvArgs a, hipStream_t st) {
   a.dblocks = make_fastdiv((a.channels + 64 * VEC - 1) / (64 * VEC));
   const int64_t blocks = (n.total + 3) / 4 * a.dblocks.d;
   a.tiles = (int)n.total;
-  if (n.total > 0x7FFFFFF0 || blocks > 0x7FFFFFFF) return refuse_size("ct_causal_conv_run");
+  if (n.total > 0x7FFFFFF0 || !fits_launch(blocks, 256)) return refuse_size("ct_causal_conv_run");
   hipLaunchKernelGGL((causal_conv_kernel<T, W, VEC, U>), dim3((unsigned)blocks), dim3(256), 0, st, a);
   return hipGetLastError() == hipSuccess ? 0 : -1;
 }

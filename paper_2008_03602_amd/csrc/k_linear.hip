@@ -284,6 +284,7 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearAr
   if constexpr (COPY > 0) {
     // Slices past the end read 0, so that STAGES - 1 of them are in flight at every wait. The
     // barrier also says that every wave has read the stage that is filled next.
+    static_assert(NC * (STAGES - 2) <= 63, "the counter of loads on their way has six bits");
     if (chunks > 0) {
 #pragma unroll
       for (int c = 0; c < STAGES - 1; ++c) fetch(c, c);
@@ -452,7 +453,8 @@ static int launch_tile(LinearArgs a, hipStream_t st) {
   a.tiles_m = (a.m + t.bm - 1) / t.bm;
   a.tiles_n = (a.n + t.bn - 1) / t.bn;
   const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
-  if (tiles > 0x7FFFFFFF || 4 * (int64_t)a.tiles_m > 0x7FFFFFFF) return refuse_size("ct_linear_run");
+  if (!fits_launch(tiles, 64 * t.wm * t.wn * t.wk) || 4 * (int64_t)a.tiles_m > 0x7FFFFFFF)
+    return refuse_size("ct_linear_run");
   a.dgroup = make_fastdiv(4 * (int64_t)a.tiles_m);
   a.dlast = make_fastdiv(a.tiles_n % 4 ? a.tiles_n % 4 : 4);
   hipLaunchKernelGGL((linear_tile_kernel<T, t.bm, t.bn, t.wm, t.wn, t.wk, S, COPY>),

@@ -393,7 +393,7 @@ static int scan_launch(ScanArgs a, int64_t pieces, hipStream_t st) {
   constexpr int CH = 4 * 64 / P;
   const int per = (a.per_group + CH - 1) / CH;
   const int64_t tiles = (int64_t)per * (a.channels / a.per_group), blocks = tiles * pieces;
-  if (blocks > 0x7FFFFFFF) return refuse_size("ct_scan_run");
+  if (!fits_launch(blocks, 256)) return refuse_size("ct_scan_run");
   a.dgroup = make_fastdiv(per);
   a.dtiles = make_fastdiv(tiles);
   hipLaunchKernelGGL((scan_kernel<T, NS, P, MODE>), dim3((unsigned)blocks), dim3(256), 0, st, a);
@@ -409,7 +409,7 @@ static int scan_prompt(ScanArgs a, const ScanPlan& p, hipStream_t st) {
   int rc = scan_launch<T, NS, P, SCAN_SUM>(a, p.chunks, st);
   if (rc) return rc;
   const int64_t blocks = (((int64_t)a.channels * a.states + 63) / 64) * a.s.count;
-  if (blocks > 0x7FFFFFFF) return refuse_size("ct_scan_run");
+  if (!fits_launch(blocks, 64)) return refuse_size("ct_scan_run");
   hipLaunchKernelGGL(scan_carry_kernel, dim3((unsigned)blocks), dim3(64), 0, st, a);
   if (hipGetLastError() != hipSuccess) return -1;
   return scan_launch<T, NS, P, SCAN_OUT>(a, p.chunks, st);
@@ -419,7 +419,7 @@ static int step_launch(ScanArgs a, hipStream_t st) {
   constexpr int CH = 64 / P;
   const int per = (a.per_group + CH - 1) / CH;
   const int64_t tiles = (int64_t)per * (a.channels / a.per_group), waves = tiles * ((a.s.count + SEQ - 1) / SEQ);
-  if (waves > 0x7FFFFFFF) return refuse_size("ct_scan_run");
+  if (waves > 0x7FFFFFF0 || !fits_launch((waves + 3) / 4, 256)) return refuse_size("ct_scan_run");
   a.dgroup = make_fastdiv(per);
   a.dtiles = make_fastdiv(tiles);
   hipLaunchKernelGGL((scan_step_kernel<T, NS, P, SEQ>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, a);

@@ -18,7 +18,10 @@ struct bf16_t {
 };
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// Refuses a launch of more waves or blocks than the kernels' 31-bit numbers can name.
+// Whether `blocks` blocks fit one launch: block numbers of 31 bits, threads of 32.
+inline bool fits_launch(int64_t blocks, int threads) {
+  return blocks <= 0x7FFFFFFF && blocks * threads <= 0xFFFFFFFFll;
+}
 inline int refuse_size(const char* who) {
   set_error(std::string(who) + ": too large for one launch");
   return -2;
@@ -211,7 +214,8 @@ __device__ __forceinline__ SeqRange find_tile(const SeqView& v, int per, int ste
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
   const SeqRange r = seq_range(v, lo);
-  *first = r.begin + (id - (r.begin / step + lo)) * step;
+  const int k = id - (r.begin / step + lo);  // past the sequence, and perhaps far, where offsets do not ascend
+  *first = k > v.tokens / step ? r.end : r.begin + k * step;
   return r;
 }
 

@@ -25,10 +25,14 @@ bool pitch_ok(int64_t ld, int64_t cols) { return ld >= cols && ld <= ((int64_t)1
 // Rows of an operand lie at most this far apart, so that a tile's offsets fit 32 bits.
 constexpr int64_t kMaxPitchBytes = 4 << 20;
 
+// A row number plus a tile of rows is still an int.
+constexpr int32_t kMostRows = 0x7FFFFFFF - 4096;
+
 int check_linear(const ct_linear_op* op) {
   const char* me = "ct_linear";
   if (!op) return refuse(me, "null op");
   if (op->m < 0 || op->n < 0 || op->k < 0) return refuse(me, "negative size");
+  if (op->m > kMostRows || op->n > kMostRows) return refuse(me, "too many rows");
   if (!dtype_ok(op->dtype) || !dtype_ok(op->out_dtype)) return refuse(me, "unknown dtype");
   if (op->act < CT_ACT_NONE || op->act > CT_ACT_GELU) return refuse(me, "unknown activation");
   if (op->res < CT_RES_NONE || op->res > CT_RES_ADD_ACT) return refuse(me, "unknown residual mode");
@@ -45,6 +49,7 @@ int check_linear(const ct_linear_op* op) {
 int check_sequences(const char* me, const ct_sequences* s, bool states) {
   if (!s) return refuse(me, "null sequences");
   if (s->tokens < 0 || s->count < 0 || s->num_slots < 0 || s->max_len < 0) return refuse(me, "negative count");
+  if (s->tokens > kMostRows || s->count > kMostRows) return refuse(me, "too many rows");
   if (!aligned(s->offsets, 4) || !aligned(s->slots, 4)) return refuse(me, "misaligned offsets or slots");
   if (!s->offsets && (s->count ? s->tokens % s->count != 0 : s->tokens != 0))
     return refuse(me, "without offsets the tokens are a multiple of the sequences");

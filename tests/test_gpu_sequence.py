@@ -276,6 +276,13 @@ def test_conv_strides_and_alignment(pitch, shift, dtype):
     check_conv([1] * 5, 80, 4, dtype, uniform=True, pitch=pitch, shift=shift, seed=5)
 
 
+def test_sequences_of_no_tokens_hand_their_states_on():
+    for dtype in (B, F):
+        check_conv([0] * 5, 24, 4, dtype, uniform=True, seed=1, unused=(2,))
+        check_scan([0] * 5, 24, 16, 1, dtype, uniform=True, seed=1, unused=(2,))
+        check_scan([0] * 5, 24, 16, 1, dtype, uniform=True, in_place=True, seed=1)
+
+
 @pytest.mark.parametrize("lens", [[40, 3, 0, 2, 129], [1] * 7, [300]])
 def test_conv_state_in_place(lens):
     check_conv(lens, 72, 4, B, in_place=True, seed=6)

@@ -27,7 +27,7 @@ def run_linear(op, x=OK, w=OK, bias=OK, res=OK, y=OK, ws=None, ws_bytes=0):
 
 @pytest.mark.parametrize("field,value,what", [
     ("m", -1, "negative"), ("n", -1, "negative"), ("k", -5, "negative"), ("dtype", 2, "dtype"), ("out_dtype", 7, "dtype"),
-    ("act", 5, "activation"), ("act", -1, "activation"), ("res", 3, "residual"), ("reserved", 1, "reserved"),
+    ("m", 0x7FFFFFFF, "too many"), ("n", 0x7FFFF000, "too many"), ("act", 5, "activation"), ("act", -1, "activation"), ("res", 3, "residual"), ("reserved", 1, "reserved"),
     ("ldx", 15, "pitch"), ("ldw", 15, "pitch"), ("ldy", 23, "pitch"), ("ldx", (4 << 20) // 2 + 1, "4 MiB"),
     ("ldw", (4 << 20) // 2 + 1, "4 MiB"), ("ldy", (1 << 31) + 1, "pitch")])
 def test_linear_refuses_a_wrong_description(field, value, what):
@@ -76,6 +76,7 @@ def test_valid_calls_need_an_initialised_device():
 SEQS = [(dict(tokens=-1, count=2), "negative"), (dict(tokens=4, count=-2), "negative"),
         (dict(tokens=4, count=2, num_slots=-1), "negative"), (dict(tokens=4, count=2, max_len=-1), "negative"),
         (dict(tokens=5, count=2, num_slots=2), "multiple"), (dict(tokens=5, count=0), "multiple"),
+        (dict(tokens=0x7FFFFFF0, count=1), "too many"), (dict(tokens=8, count=0x7FFFFFF0, offsets=OK), "too many"),
         (dict(tokens=4, count=2, num_slots=1), "slots"), (dict(tokens=4, count=2, offsets=OK + 2), "misaligned"),
         (dict(tokens=4, count=2, num_slots=2, slots=OK + 1), "misaligned")]
 
@@ -111,7 +112,8 @@ def test_causal_conv_refuses_wrong_arrays():
     ("channels", -2, "negative"), ("states", 0, "states"), ("states", 257, "states"), ("groups", 0, "groups"),
     ("groups", 3, "groups"), ("dtype", -1, "dtype"), ("softplus", 2, "flag"), ("reserved", 1, "flag"),
     ("ldu", 7, "pitch"), ("lddelta", 7, "pitch"), ("ldb", 7, "pitch"), ("ldc", 7, "pitch"), ("ldy", 7, "pitch"),
-    ("ldz", 7, "pitch")])
+    ("ldz", 7, "pitch"), ("ldu", (2 << 20) + 1, "4 MiB"), ("lddelta", (2 << 20) + 1, "4 MiB"),
+    ("ldy", (2 << 20) + 1, "4 MiB"), ("ldz", (2 << 20) + 1, "4 MiB")])
 def test_scan_refuses_a_wrong_description(field, value, what):
     op = L.make_scan(8, 4, 2, 1)
     setattr(op, field, value)
