@@ -2,7 +2,26 @@
 //
 // x (m x k) and w (n x k) are both contiguous along the reduction, so a fragment of either
 // is 16 bytes of a row. The weights are the matrix instruction's first operand: a lane's
-// four consecutive accumulators are then four consecutive outputs of one row of y.
+// four consecutive accumulators are then four consecutive outputs of one row of y. Products
+// of bf16 are exact in fp32 and sums are in fp32; only an output is rounded.
+//
+// What bounds it, and what was chosen for it:
+//   * Large products: the matrix cores. 256 x 256 tiles, eight waves of 64 x 128, two slices
+//     of 64 KB in LDS, copied straight into it. 8192 x 4096 by 8192 with bias and GELU, bf16:
+//     430-465 us, 1.18-1.28 PFLOP/s (a library's bare product: 453 us). Measured and left:
+//     waves of 128 x 64 (5 % slower), the 32 x 32 instruction (5 %), slices of 64 bytes with
+//     three to five stages (8-12 %), the next slice asked for after the products (16 %), and,
+//     with no effect, two groups of waves in turn, priorities, columns of eight tiles.
+//   * Few rows: the weights' bytes. 32 x 32 tiles and four teams of waves over the slices, so
+//     that 128 tiles keep 8 MB on their way: 24 x 8192 by 4096, bf16, 14.6 us, 4.7 TB/s.
+//     Fragments read straight into registers, 16 rows of 64 bytes a load, took 24.5 us.
+//   * In between: rounds of the device and, below 64 x 64, a wait and a barrier (0.19 us)
+//     every slice, which the teams share out (64 x 4096 by 4096: 12.3 to 9.5 us).
+//   * Short reductions: the epilogue. It takes whole rows of the tile through LDS, chooses
+//     the activation once for 16 values, and checks nothing where the whole tile exists
+//     (12544 x 32 by 192, fp32 out: 9.5 to 5.5 us).
+// Rows off 16 bytes are copied a word a lane, which is bound by the copies (471 x 3882 by 2368,
+// bf16: 44 us; through registers 51); rows of bf16 off words go through registers.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -184,6 +203,9 @@ __device__ __forceinline__ void copy_lds(__amdgpu_buffer_rsrc_t r, char* lds, un
 // less time than the waits around them. Slices go through STAGES buffers in LDS, the later
 // ones in flight while one is multiplied; the 16-byte groups of a row are permuted by its
 // number, so that the 16 rows of a fragment lie in distinct banks.
+// Every address is in bounds: an operand's rows are a buffer that ends with the last of the
+// tile's rows, rows and slices past the end have an offset past it, and reads beyond k within
+// a row are kept out one group (or word, or element) at a time.
 template <typename T, int BM, int BN, int WM, int WN, int WK, int STAGES, int COPY>
 __global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearArgs a) {
   constexpr int WAVES = WM * WN, ROWS = BM + BN, G = 16 / (int)sizeof(T), ROWB = 128, NG = ROWB / 16;
