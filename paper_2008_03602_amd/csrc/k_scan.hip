@@ -79,10 +79,18 @@ __device__ __forceinline__ void store_vals(float* p, const float (&v)[NS], int l
 __device__ __forceinline__ bool rows_of_four(const void* p, int states) {
   return ((uintptr_t)p % 16 | (unsigned)states % 4) == 0;
 }
+// The sum over P neighbouring lanes, in all of them: pairs and quads by permutation, then the
+// other quad and the other eight of a row of 16 by mirroring, whose lanes hold equal sums.
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v) {
+  return v + __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
 template <int P>
 __device__ __forceinline__ float add_lanes(float v) {
-#pragma unroll
-  for (int m = 1; m < P; m *= 2) v += __shfl_xor(v, m, 64);
+  if constexpr (P > 1) v = add_dpp<0xB1>(v);   // quad_perm [1, 0, 3, 2]
+  if constexpr (P > 2) v = add_dpp<0x4E>(v);   // quad_perm [2, 3, 0, 1]
+  if constexpr (P > 4) v = add_dpp<0x141>(v);  // row_half_mirror
+  if constexpr (P > 8) v = add_dpp<0x140>(v);  // row_mirror
   return v;
 }
 
@@ -374,29 +382,42 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
 }
 
 // ------------------------------------------------------------------ plans and launches
-// Lanes that share a channel, and states of each, in the two kinds of kernel.
-static int prompt_parts(int states) { return states <= 16 ? 1 : states <= 32 ? 2 : states <= 64 ? 4 : states <= 128 ? 8 : 16; }
+// Lanes that share a channel of a prompt: 16 states a lane, or four where that leaves the
+// device idle.
+static int prompt_parts(int states, bool narrow) {
+  int parts = 1;
+  while (parts * (narrow ? 4 : 16) < states) parts *= 2;
+  return narrow && parts < 4 ? 4 : parts;
+}
 
 ScanPlan plan_scan(const ct_scan_op& op, const ct_sequences& s) {
   ScanPlan p = {};
   if (!s.tokens) return p;
   const int most = s.offsets ? (s.max_len ? (s.max_len < s.tokens ? s.max_len : s.tokens) : s.tokens) : s.tokens / s.count;
-  // Waves of a chunk, and as many tokens in it as leave eight blocks of four waves for every
-  // compute unit: those at work together take turns evenly, and the last ones are short (a
-  // third of them: 8192 ragged tokens of 4096 channels 246 to 275 us). Whole stages of 32.
-  const int ch = 64 / prompt_parts(op.states), per_group = op.channels / op.groups;
-  const int64_t waves = (int64_t)op.groups * ((per_group + ch - 1) / ch);
+  const double simds = 4 * kPlanCus;
+  auto waves_of = [&]() {  // of a chunk
+    const int ch = 64 / prompt_parts(op.states, p.narrow), per_group = op.channels / op.groups;
+    return (int64_t)op.groups * ((per_group + ch - 1) / ch);
+  };
+  // Four states a lane below 28 tokens of a wave for each SIMD: a token takes 0.24 us instead
+  // of 0.4, and four times the waves (778 tokens of 1005 channels of 13 states 33 to 27 us, 64
+  // tokens of 2048 channels 27 to 17; 1024 of 2048: 36.5 and 39.4).
+  p.narrow = op.states <= 64 && (double)s.tokens * (double)waves_of() < 28 * simds;
+  // As many tokens in a chunk as leave eight blocks of four waves for every compute unit:
+  // those at work together take turns evenly, and the last ones are short (a third of them:
+  // 8192 ragged tokens of 4096 channels 246 to 275 us). Whole stages of 32.
+  const int64_t waves = waves_of();
   int64_t chunk = ((int64_t)s.tokens * waves / (8 * 4 * kPlanCus) + 16) / 32 * 32;
   if (chunk < 32) chunk = 32;
   // Whether to cut at all, by what either takes in us (16 states, bf16; measured on 1 to 256
   // sequences of 8 to 2048 tokens, where the choice is the faster or within 7 % of it). A SIMD
-  // with n waves gives each a token in 0.38 + 0.13 n, and the longest sequence takes as many
-  // tokens; cut, all tokens are walked twice at the full rate, by three kernels. 32 x 512
-  // tokens of 4096 channels: 332 whole, 459 cut; 16 x 1024: 493 and 430.
-  const double simds = 4 * kPlanCus, per_simd = (double)s.tokens * (double)waves / simds;
-  double whole = most * 0.38 + 0.13 * per_simd;
+  // with n waves gives each a token in 0.38 + 0.13 n (0.23 + 0.09 n), and the longest sequence
+  // takes as many tokens; cut, all tokens are walked twice at the full rate, by three kernels.
+  // 32 x 512 tokens of 4096 channels: 332 whole, 459 cut; 16 x 1024: 493 and 430.
+  const double per_simd = (double)s.tokens * (double)waves / simds;
+  double whole = p.narrow ? most * 0.23 + 0.09 * per_simd : most * 0.38 + 0.13 * per_simd;
   if (whole < 0.27 * per_simd) whole = 0.27 * per_simd;
-  if (whole <= 28 + 0.4 * per_simd) return p;
+  if (whole <= (p.narrow ? 16 + 0.19 * per_simd : 28 + 0.4 * per_simd)) return p;
   p.chunk = (int)chunk;
   p.chunks = s.offsets ? s.tokens / chunk + s.count : (int64_t)s.count * ((most + chunk - 1) / chunk);
   p.ws_floats = p.chunks * op.channels * (op.states + 1);
@@ -455,7 +476,12 @@ static int scan_pick(const ScanArgs& a, const ScanPlan& p, hipStream_t st) {
     if (a.states <= 128) return scan_step<T, 8, 16>(a, st);
     return scan_step<T, 16, 16>(a, st);
   }
-  switch (prompt_parts(a.states)) {
+  if (p.narrow) switch (prompt_parts(a.states, true)) {
+      case 4: return scan_prompt<T, 4, 4>(a, p, st);
+      case 8: return scan_prompt<T, 4, 8>(a, p, st);
+      default: return scan_prompt<T, 4, 16>(a, p, st);
+    }
+  switch (prompt_parts(a.states, false)) {
     case 1: return a.states <= 8 ? scan_prompt<T, 8, 1>(a, p, st) : scan_prompt<T, 16, 1>(a, p, st);
     case 2: return scan_prompt<T, 16, 2>(a, p, st);
     case 4: return scan_prompt<T, 16, 4>(a, p, st);

@@ -45,6 +45,7 @@ int launch_causal_conv(const ct_causal_conv_op& op, const SeqView& s, const void
 
 // ---- ct_scan ----
 struct ScanPlan {
+  bool narrow;        // a prompt's lanes have four states, not 16
   int chunk;          // tokens per chunk (0: every sequence in one piece)
   int64_t chunks;     // chunks in all, an upper bound
   int64_t ws_floats;

@@ -153,6 +153,15 @@ def test_linear_many_tiles(m, n):
     check_linear(m, n, 136, B, F, L.ACT_NONE, L.RES_ADD, bias=False, seed=10)
 
 
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("more", [0, 2, 1])  # of k: rows on 16 bytes, on words, (bf16) on neither
+@pytest.mark.parametrize("m,n,k", [(20, 8300, 136), (300, 1000, 96), (512, 800, 72), (1021, 1277, 40), (1000, 960, 64),
+                                   (1300, 1300, 136), (1500, 2600, 72), (2000, 4090, 64), (4000, 4000, 72)])
+def test_linear_every_tile(m, n, k, more, dtype):
+    """Sizes that take each of the tiles, small to large, with ragged edges."""
+    check_linear(m, n, k + more, dtype, dtype, L.ACT_RELU, L.RES_ADD, seed=m + more)
+
+
 @pytest.mark.parametrize("m,n,k", [(4, 64, 64), (150, 132, 64), (40, 64, 8192)])
 def test_linear_residual_in_place(m, n, k):
     check_linear(m, n, k, B, B, 0, L.RES_ADD, seed=1, in_place=True)
@@ -422,6 +431,16 @@ def test_scan_long_and_ragged_prompts(dtype, z):
     check_scan([260] * 3, 40, 5, 1, dtype, z=z, seed=5, uniform=True)
 
 
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("lens,channels,states,groups", [
+    ([300, 0, 1, 170], 4090, 13, 1), ([470], 4096, 16, 2), ([20] * 110, 836, 16, 1), ([310, 200], 4100, 8, 4),
+    ([25] * 70, 1030, 5, 1), ([240], 4096, 24, 1), ([30] * 40, 1100, 32, 2), ([190, 40], 2050, 40, 1), ([12] * 90, 516, 64, 3)])
+def test_scan_enough_channels_and_tokens_to_fill_the_device(lens, channels, states, groups, dtype):
+    """From 28 tokens of a wave for each SIMD on a lane has 16 states: whole sequences and cut ones."""
+    uniform = len(set(lens)) == 1
+    check_scan(lens, channels, states, groups, dtype, uniform=uniform, seed=2 * states, lead=0 if uniform else 3)
+
+
 @pytest.mark.parametrize("lens", [[400, 3, 0, 2, 129], [1] * 7, [300]])
 def test_scan_state_in_place(lens):
     check_scan(lens, 72, 16, 1, B, in_place=True, seed=6)
@@ -580,6 +599,51 @@ def test_capture_and_replay():
                 assert torch.equal(outs[k][[2, 0, 3]], first[k][[2, 0, 3]]), k
             else:
                 assert torch.equal(outs[k], first[k]), k
+
+
+def test_outputs_that_go_past_the_caches():
+    """Outputs of 128 MiB and states of 32 MiB are stored past the caches: the same formulas, in 64 bits on the GPU."""
+    g = gen(50)
+    m, n, k = 8200, 8192, 32
+    x, w, r = (normal(g, *s, dtype=B).cuda() for s in ((m, k), (n, k), (1, n)))
+    r = r.expand(m, n).contiguous()
+    for out in (B, F):
+        op = L.make_linear(m, n, k, L.DT_BF16, CODE[out], L.ACT_SILU, L.RES_ADD if out == B else L.RES_NONE)
+        y = torch.full((m, n), NAN, dtype=out, device="cuda")
+        note("product of %d MiB" % (y.numel() * y.element_size() >> 20))
+        L.ct_linear_run(op, x, w, None, r, y, None, stream())
+        v = x.double() @ w.double().t().contiguous()
+        ref = v / (1 + torch.exp(-v)) + (r.double() if out == B else 0)
+        bound = 1.13 * (k + 4) * U * (x.double().abs() @ w.double().abs().t().contiguous()) + 12 * U * v.abs() + U * ref.abs()
+        assert ((y.double() - ref).abs() <= bound + ROUND[out] * (ref.abs() + bound)).all()
+        del v, ref, bound
+    tokens, ch = 16500, 4096
+    x, w = normal(g, tokens, ch, dtype=B).cuda(), normal(g, ch, 4).cuda()
+    y = torch.full((tokens, ch), NAN, dtype=B, device="cuda")
+    note("convolution of %d MiB" % (y.numel() * 2 >> 20))
+    L.ct_causal_conv_run(L.make_causal_conv(ch, 4, L.DT_BF16), L.make_sequences(tokens, 1), x, w, None, None, None, y,
+                         stream())
+    past = torch.cat([torch.zeros(3, ch, dtype=torch.float64, device="cuda"), x.double()])
+    terms = [past[j:j + tokens] * w[:, j].double() for j in range(4)]
+    ref, mag = sum(terms), sum(t.abs() for t in terms)
+    assert ((y.double() - ref).abs() <= 8 * U * mag + ROUND[B] * (ref.abs() + 8 * U * mag)).all()
+    del past, terms, ref, mag
+    count, ch, n = 131, 4100, 16
+    s = {k: (v.cuda() if torch.is_tensor(v) else v) for k, v in scan_inputs(count, ch, n, 1, B, count, 51).items()}
+    out, y = torch.full_like(s["state"], NAN), torch.empty(count, ch, dtype=B, device="cuda")
+    note("states of %d MiB" % (out.numel() * 4 >> 20))
+    L.ct_scan_run(L.make_scan(ch, n, 1, L.DT_BF16), L.make_sequences(count, count, count), s["u"], s["delta"], s["dt_bias"],
+                  s["a"], s["b"], s["c"], s["d"], s["z"], s["state"], out, y, None, stream())
+    d = {k: (v.double() if torch.is_tensor(v) else v) for k, v in s.items()}
+    v = d["delta"] + d["dt_bias"]
+    dt = torch.clamp(v, min=0) + torch.log1p(torch.exp(-v.abs()))
+    arg = dt[..., None] * d["a"]
+    add = (dt * d["u"])[..., None] * d["b"][:, None]
+    h = torch.exp(arg) * d["state"] + add
+    rel = (10 + 3 * v.abs()) * U + U * (d["delta"].abs() + d["dt_bias"].abs()) / dt
+    bound = torch.exp(arg) * d["state"].abs() * (4 * U + arg.abs() * (4 * U + rel[..., None])) + add.abs() * (
+        4 * U + rel[..., None]) + 2 * U * h.abs()
+    assert ((out.double() - h).abs() <= bound).all()
 
 
 def test_offsets_beyond_32_bits():
