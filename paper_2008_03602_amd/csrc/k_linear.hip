@@ -442,26 +442,31 @@ LinearPlan plan_linear(const ct_linear_op& op) {
   LinearPlan p = {};
   const int chunks = (int)(((int64_t)op.k * elem_bytes(op.dtype) + 127) / 128);
   // Rounds of the device, and what a round costs beside one of 128 x 128 tiles at the full
-  // rate (one of those on a compute unit alone does not reach it). Measured in bf16 on 4096^3,
-  // 2048^3, 2048 x 4096 by 1024, 11020 x 320 by 3520, 6000 x 640 by 1024, 1500^3 and 512 x
-  // 2048 by 2048: the choice is the fastest or within 5 % of it.
+  // rate. In bf16 small tiles, and one of 128 x 128 on a compute unit alone, do not reach it;
+  // in fp32 the matrix cores bound all of them. Measured in bf16 on 4096^3, 2048^3, 2048 x
+  // 4096 by 1024, 11020 x 320 by 3520, 6000 x 640 by 1024, 1500^3, 512 x 2048 by 2048 and
+  // reductions of 64 to 512, in fp32 on 4096^2 by 64 to 2048, 2048^3, 3000 x 1000 by 501, 889
+  // x 5384 by 64 and 1021 x 1277 by 515: the choice is the fastest or within 5 % of it.
   auto rounds = [&](int kind) { return (double)((tiles_of(op, kind) + kPlanCus - 1) / kPlanCus); };
-  const double t64 = 0.5 * rounds(LIN_64), t128x64 = op.dtype == CT_DT_BF16 ? 0.8 * rounds(LIN_128X64) : 1e30,
-               t128 = rounds(LIN_128) > 1 ? 1.2 * rounds(LIN_128) : 1.65, t256 = 4.0 * rounds(LIN_256);
-  double best = t64;
-  p.kind = LIN_64;
-  for (auto [kind, t] : {std::pair<int, double>{LIN_128X64, t128x64}, {LIN_128, t128}, {LIN_256, t256}})
-    if (t < best) {
-      best = t;
+  const double r128 = rounds(LIN_128);
+  const std::pair<int, double> bf16_costs[] = {{LIN_64, 0.5 * rounds(LIN_64)},
+                                               {LIN_128X64, 0.8 * rounds(LIN_128X64)},
+                                               {LIN_128, r128 > 1 ? 1.2 * r128 : 1.65},
+                                               {LIN_256, 4.0 * rounds(LIN_256)}},
+                               f32_costs[] = {{LIN_64, 0.27 * rounds(LIN_64)},
+                                              {LIN_32X64, 0.14 * rounds(LIN_32X64)},
+                                              {LIN_128, r128 > 1 ? r128 : 1.12},
+                                              {LIN_256, 3.97 * rounds(LIN_256)}};
+  double least = 1e300;
+  for (auto [kind, cost] : op.dtype == CT_DT_BF16 ? bf16_costs : f32_costs)
+    if (cost < least) {
+      least = cost;
       p.kind = kind;
     }
   // Smaller tiles where 64 x 64 leaves compute units without one
   const int64_t enough = kPlanCus * 3 / 4;
-  if (p.kind == LIN_64 && tiles_of(op, LIN_64) < enough)
+  if ((p.kind == LIN_64 || p.kind == LIN_32X64) && tiles_of(op, LIN_64) < enough)
     p.kind = tiles_of(op, LIN_64X32) >= enough ? LIN_64X32 : LIN_32;
-  // fp32 is bound by the matrix cores at this size too: half the tile where its rounds are fewer
-  else if (p.kind == LIN_64 && op.dtype == CT_DT_F32 && 0.52 * rounds(LIN_32X64) < rounds(LIN_64))
-    p.kind = LIN_32X64;
   if (op.m <= 32) p.kind = LIN_32;
   if (p.kind == LIN_64 && tiles_of(op, LIN_64) > kPlanCus) p.kind = LIN_64_TWO;
   if (p.kind == LIN_32 && tiles_of(op, LIN_32) > kPlanCus) p.kind = LIN_32_TWO;
