@@ -13,10 +13,12 @@
 //           h(end) = exp(a * sum of steps) h(start) + h(end from 0);
 //   out:    the outputs of each chunk from h at its start.
 // That is nearly twice the exponentials, but as many chunks at once as fill the device: the
-// 16384 tokens take 255 us (sum 104, carry 22, out 135), whole sequences alone 29 ms. The
+// 16384 tokens take 233 us (kernels: sum 95, carry 22, out 129), whole sequences alone 29 ms. The
 // vector ALU is busy 84-88 % of sum and out, with 112 instructions a token in out, 80 of them
 // the states'. b and c through scalar registers instead of LDS lost 5 % (no room to have the
-// next token's on their way), five waves on a SIMD instead of four spill.
+// next token's on their way), five waves on a SIMD instead of four spill, and the products
+// dt u b as rank-one updates on the matrix cores, 12 vector instructions a token fewer, lost
+// 3-4 %.
 // The carries are read from state_in before any chunk's outputs write state_out, so that
 // both may be one array.
 #include <hip/hip_runtime.h>
@@ -307,7 +309,7 @@ __global__ void __launch_bounds__(64) scan_carry_kernel(ScanArgs a) {
 // One token of each sequence: a wave updates 64 / P channels of SEQ sequences, whose loads are
 // all on their way together; a, the bias and the skip weight are read once for them. Four
 // states a lane make every access to the states one of 1 KB: 256 sequences of 4096 channels
-// of 16 states (67 MB read, 67 MB written) 25.6 us, 5.6 TB/s; one sequence a wave 30 us, 16
+// of 16 states (67 MB read, 67 MB written) 25.3 us, 5.6 TB/s; one sequence a wave 30 us, 16
 // states a lane 45 (of which the stores through the caches are 10).
 template <typename T, int NS, int P, int SEQ>
 __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
