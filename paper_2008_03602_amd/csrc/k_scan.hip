@@ -13,7 +13,7 @@
 //           h(end) = exp(a * sum of steps) h(start) + h(end from 0);
 //   out:    the outputs of each chunk from h at its start.
 // That is nearly twice the exponentials, but as many chunks at once as fill the device: the
-// 16384 tokens take 233 us (kernels: sum 95, carry 22, out 129), whole sequences alone 29 ms. The
+// 16384 tokens take 233 us (kernels: sum 95, carry 22, out 129), whole sequences alone 4 ms. The
 // vector ALU is busy 84-88 % of sum and out, with 112 instructions a token in out, 80 of them
 // the states'. b and c through scalar registers instead of LDS lost 5 % (no room to have the
 // next token's on their way), five waves on a SIMD instead of four spill, and the products
@@ -104,7 +104,11 @@ enum ScanMode { SCAN_WHOLE, SCAN_SUM, SCAN_OUT };
 // their way meanwhile.
 template <typename T, int NS, int P, int MODE>
 __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
-  constexpr int CH = 64 / P, NP = NS * P, TT = NP <= 16 ? 32 : NP <= 64 ? 16 : 4, U = 4;
+  constexpr int CH = 64 / P, NP = NS * P, TT = NP <= 16 ? 32 : NP <= 64 ? 16 : 4;
+  // Tokens whose rows are on their way while as many are walked: a wave that is nearly alone on
+  // its SIMD waits for them (32 x 512 tokens of 4096 channels, whole: four 321 us, eight 287,
+  // 16 280 and slower with more waves). The outputs of chunks keep a fourth wave instead.
+  constexpr int U = TT > 4 && MODE != SCAN_OUT ? 8 : 4;
   constexpr int STAGED = TT * NP / 256 ? TT * NP / 256 : 1;  // values of b (and of c) that a thread stages
   __shared__ __align__(16) float sb[2][TT][NP], sc[MODE == SCAN_SUM ? 1 : 2][MODE == SCAN_SUM ? 1 : TT][NP];
 
@@ -397,29 +401,39 @@ ScanPlan plan_scan(const ct_scan_op& op, const ct_sequences& s) {
   if (!s.tokens) return p;
   const int most = s.offsets ? (s.max_len ? (s.max_len < s.tokens ? s.max_len : s.tokens) : s.tokens) : s.tokens / s.count;
   const double simds = 4 * kPlanCus;
-  auto waves_of = [&]() {  // of a chunk
-    const int ch = 64 / prompt_parts(op.states, p.narrow), per_group = op.channels / op.groups;
+  auto waves_of = [&](bool narrow) {  // of a chunk
+    const int ch = 64 / prompt_parts(op.states, narrow), per_group = op.channels / op.groups;
     return (int64_t)op.groups * ((per_group + ch - 1) / ch);
   };
-  // Four states a lane below 28 tokens of a wave for each SIMD: a token takes 0.24 us instead
-  // of 0.4, and four times the waves (778 tokens of 1005 channels of 13 states 33 to 27 us, 64
-  // tokens of 2048 channels 27 to 17; 1024 of 2048: 36.5 and 39.4).
-  p.narrow = op.states <= 64 && (double)s.tokens * (double)waves_of() < 28 * simds;
+  // 16 states a lane (8 where a channel has no more) or four, cut or whole: what takes the
+  // fewest us by fits to bf16 (1 to 128 sequences of 32 to 2048 tokens and 300 to 4096 channels
+  // of 8 to 64 states; the choice is the fastest or within 5 % of it). A SIMD with n waves gives
+  // each a token in token + wave n, its vector ALU one in full, and the longest sequence takes
+  // as many; cut, all tokens are walked twice at the full rate, by three kernels. whole / cut of
+  // 16 states: 32 x 512 tokens of 4096 channels 287 / 444, in fours 483 / 495; 8 x 128 of 2048:
+  // 52 / 37, in fours 33 / 41; 1 x 256 of 2048: 90 / 29, in fours 53 / 21.
+  struct Fit { double token, wave, full, cut, cut_token; };
+  const Fit wide = op.states <= 8 ? Fit{0.2, 0.11, 0.2, 20, 0.29} : Fit{0.29, 0.13, 0.25, 26, 0.42};
+  const Fit four = {0.17, 0.09, 0.09, 16, 0.19};
+  double least = 1e300;
+  bool cut = false;
+  for (const bool narrow : {false, true}) {
+    if (narrow && op.states > 64) break;
+    const double per_simd = (double)s.tokens * (double)waves_of(narrow) / simds;
+    const Fit& f = narrow ? four : wide;
+    double whole = f.token * most + f.wave * per_simd;
+    if (whole < f.full * per_simd + 0.03 * most) whole = f.full * per_simd + 0.03 * most;
+    whole += 4;
+    const double chunks = f.cut + f.cut_token * per_simd;
+    if (whole < least) least = whole, p.narrow = narrow, cut = false;
+    if (chunks < least) least = chunks, p.narrow = narrow, cut = true;
+  }
+  if (!cut) return p;
   // As many tokens in a chunk as leave eight blocks of four waves for every compute unit:
   // those at work together take turns evenly, and the last ones are short (a third of them:
   // 8192 ragged tokens of 4096 channels 246 to 275 us). Whole stages of 32.
-  const int64_t waves = waves_of();
-  int64_t chunk = ((int64_t)s.tokens * waves / (8 * 4 * kPlanCus) + 16) / 32 * 32;
+  int64_t chunk = ((int64_t)s.tokens * waves_of(p.narrow) / (8 * 4 * kPlanCus) + 16) / 32 * 32;
   if (chunk < 32) chunk = 32;
-  // Whether to cut at all, by what either takes in us (16 states, bf16; measured on 1 to 256
-  // sequences of 8 to 2048 tokens, where the choice is the faster or within 7 % of it). A SIMD
-  // with n waves gives each a token in 0.38 + 0.13 n (0.23 + 0.09 n), and the longest sequence
-  // takes as many tokens; cut, all tokens are walked twice at the full rate, by three kernels.
-  // 32 x 512 tokens of 4096 channels: 332 whole, 459 cut; 16 x 1024: 493 and 430.
-  const double per_simd = (double)s.tokens * (double)waves / simds;
-  double whole = p.narrow ? most * 0.23 + 0.09 * per_simd : most * 0.38 + 0.13 * per_simd;
-  if (whole < 0.27 * per_simd) whole = 0.27 * per_simd;
-  if (whole <= (p.narrow ? 16 + 0.19 * per_simd : 28 + 0.4 * per_simd)) return p;
   p.chunk = (int)chunk;
   p.chunks = s.offsets ? s.tokens / chunk + s.count : (int64_t)s.count * ((most + chunk - 1) / chunk);
   p.ws_floats = p.chunks * op.channels * (op.states + 1);

@@ -436,9 +436,19 @@ def test_scan_long_and_ragged_prompts(dtype, z):
     ([300, 0, 1, 170], 4090, 13, 1), ([470], 4096, 16, 2), ([20] * 110, 836, 16, 1), ([310, 200], 4100, 8, 4),
     ([25] * 70, 1030, 5, 1), ([240], 4096, 24, 1), ([30] * 40, 1100, 32, 2), ([190, 40], 2050, 40, 1), ([12] * 90, 516, 64, 3)])
 def test_scan_enough_channels_and_tokens_to_fill_the_device(lens, channels, states, groups, dtype):
-    """From 28 tokens of a wave for each SIMD on a lane has 16 states: whole sequences and cut ones."""
+    """Where waves of 16 states a lane fill the device: whole sequences and cut ones."""
     uniform = len(set(lens)) == 1
     check_scan(lens, channels, states, groups, dtype, uniform=uniform, seed=2 * states, lead=0 if uniform else 3)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("lens,channels,states,groups", [
+    ([600], 2048, 40, 1), ([150, 0, 301], 130, 100, 2), ([333], 70, 200, 1), ([4] * 33 + [190], 130, 128, 1),
+    ([33, 32, 31, 9, 8, 7], 2050, 16, 1), ([48] * 20, 1024, 16, 1), ([40] * 9, 4100, 7, 1)])
+def test_scan_many_states_cut_and_lengths_around_a_stage(lens, channels, states, groups, dtype):
+    """Several lanes a channel where sequences are cut, and the last tokens of stages of 32, 16 and four."""
+    uniform = len(set(lens)) == 1
+    check_scan(lens, channels, states, groups, dtype, uniform=uniform, seed=2 * states + 1, lead=0 if uniform else 5)
 
 
 @pytest.mark.parametrize("lens", [[400, 3, 0, 2, 129], [1] * 7, [300]])
