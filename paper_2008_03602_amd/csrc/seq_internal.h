@@ -49,6 +49,7 @@ struct ScanPlan {
   int chunk;          // tokens per chunk (0: every sequence in one piece)
   int64_t chunks;     // chunks in all, an upper bound
   int64_t ws_floats;
+  bool fold;          // the outputs of a chunk fold those before it themselves
 };
 ScanPlan plan_scan(const ct_scan_op& op, const ct_sequences& s);
 struct ScanArrays {

@@ -451,6 +451,18 @@ def test_scan_many_states_cut_and_lengths_around_a_stage(lens, channels, states,
     check_scan(lens, channels, states, groups, dtype, uniform=uniform, seed=2 * states + 1, lead=0 if uniform else 5)
 
 
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("lens,channels,states,groups", [
+    ([240, 0, 33, 0, 1, 32], 515, 16, 1), ([0, 0, 96, 95], 66, 5, 2), ([256, 0], 70, 64, 1), ([250, 0, 7, 64, 0], 2050, 13, 1),
+    ([200, 0, 64], 2050, 40, 1), ([128, 0, 127], 68, 100, 2), ([256] * 3, 130, 16, 1)])
+def test_scan_of_a_few_chunks(lens, channels, states, groups, in_place, dtype):
+    """Up to eight chunks of a sequence go without a kernel for their carries, empty sequences among them."""
+    uniform = len(set(lens)) == 1
+    check_scan(lens, channels, states, groups, dtype, uniform=uniform, in_place=in_place, unused=(1,), seed=2 * states,
+               lead=0 if uniform else 40, tail=0 if uniform else 70)
+
+
 @pytest.mark.parametrize("lens", [[400, 3, 0, 2, 129], [1] * 7, [300]])
 def test_scan_state_in_place(lens):
     check_scan(lens, 72, 16, 1, B, in_place=True, seed=6)
