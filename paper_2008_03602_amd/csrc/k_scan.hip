@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
   const int lane = (int)(threadIdx.x & 63), part = lane % P, ch = in_group + lane / P;
   if (ch >= a.per_group) return;
   const int d = group * a.per_group + ch, n0 = part * NS, left = a.states - n0;
-  const int64_t gn = (int64_t)group * a.states + n0;
+  const int64_t in_row = (int64_t)group * a.states;
   const bool vec = rows_of_four(a.state_in, a.states) && rows_of_four(a.state_out, a.states);
 
   // what does not wait for the slots goes first
@@ -370,12 +370,13 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
     u[q] = (float)((const T*)a.u + t * a.ldu)[d];
     dt[q] = (float)((const T*)a.delta + t * a.lddelta)[d];
     z[q] = a.z ? (float)((const T*)a.z + t * a.ldz)[d] : 0.f;
-    const T *pb = (const T*)a.b + t * a.ldb + gn, *pc = (const T*)a.c + t * a.ldc + gn;
+    const T *pb = (const T*)a.b + t * a.ldb + in_row, *pc = (const T*)a.c + t * a.ldc + in_row;
 #pragma unroll
     for (int i = 0; i < NS; i += 4) {
       if (a.vec_bc) {
         const bool in = i < left;
-        const Quad qb = load_quad4(pb + (in ? i : 0)), qc = load_quad4(pc + (in ? i : 0));
+        const int col = quad_column(n0 + i, a.states);
+        const Quad qb = load_quad4(pb + col), qc = load_quad4(pc + col);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           b[q].v[i + e] = in ? qb.v[e] : 0.f;
@@ -385,8 +386,8 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const bool in = i + e < left;
-          b[q].v[i + e] = in ? (float)pb[i + e] : 0.f;
-          c[q].v[i + e] = in ? (float)pc[i + e] : 0.f;
+          b[q].v[i + e] = in ? (float)pb[n0 + i + e] : 0.f;
+          c[q].v[i + e] = in ? (float)pc[n0 + i + e] : 0.f;
         }
       }
     }

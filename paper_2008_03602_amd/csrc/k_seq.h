@@ -67,6 +67,9 @@ __device__ __forceinline__ Quad load_quad4(const O* p) {
     return {q.x, q.y, q.z, q.w};
   }
 }
+// The column that a lane's four states from state n on are read from, of a row that ends on a
+// multiple of four: the row's first four, whose values are not used, where there is no state n.
+constexpr int quad_column(int n, int states) { return n < states ? n : 0; }
 
 // ---- outputs larger than the caches that would hold them ----
 // Bytes of an output from which its stores go past the L2s instead of pushing out of them

@@ -1,0 +1,32 @@
+"""Which rows and columns the sequence-block kernels read, as the rules that they are compiled
+from say: constant evaluation goes through the cases (and refuses a signed overflow), in a
+syntax check of the host side."""
+import subprocess
+
+from paper_2008_03602_amd import build as B
+
+
+def holds(tmp_path, unit):
+    src = tmp_path / "unit.hip"
+    src.write_text('#include "k_seq.h"\n' + unit)
+    cmd = [B._hipcc()] + B.HIP_FLAGS + ["--offload-host-only", "-fsyntax-only", "-fconstexpr-steps=100000000", str(src)]
+    r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
+    assert r.returncode == 0, r.stdout[-3000:]
+
+
+def test_lanes_without_a_state_read_columns_that_exist(tmp_path):
+    # lanes of 4, 8 or 16 states, up to 16 of them a channel, over every row of whole quads
+    holds(tmp_path, r"""
+constexpr bool inside() {
+  for (int states = 4; states <= 256; states += 4)
+    for (int ns = 4; ns <= 16; ns *= 2)
+      for (int part = 0; part < 16; ++part)
+        for (int i = 0; i < ns; i += 4) {
+          const int n = part * ns + i, col = ct::quad_column(n, states);
+          if (col < 0 || col + 4 > states) return false;
+          if (n < states && col != n) return false;
+        }
+  return true;
+}
+static_assert(inside(), "");
+""")
