@@ -203,14 +203,15 @@ __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
       }
     }
   };
-  // The next U tokens of this lane's channel, from rows that start with the stage's. Lanes that
-  // store nothing have an offset past every row.
+  // The next U tokens of this lane's channel, from rows that start with the stage's; past the
+  // last token the last row again. Lanes that store nothing have an offset past every row.
   constexpr int E = (int)sizeof(T);
   const unsigned off = (unsigned)d * (unsigned)E, off_y = part == 0 && live ? off : kOob;
   const int step_u = (int)a.ldu * E, step_d = (int)a.lddelta * E, step_z = (int)a.ldz * E, step_y = (int)a.ldy * E;
   __amdgpu_buffer_rsrc_t ru, rd, rz, ry;
+  int rows = 0;
   auto aim = [&](int t) __attribute__((always_inline)) {
-    const int rows = min(t1 - t, TT + U);
+    rows = min(t1 - t, TT + U);
     ru = rows_rsrc((const T*)a.u + t * a.ldu, rows, a.ldu, a.channels);
     rd = rows_rsrc((const T*)a.delta + t * a.lddelta, rows, a.lddelta, a.channels);
     if constexpr (MODE != SCAN_SUM) {
@@ -220,14 +221,17 @@ __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
   };
   float ku[U], kd[U], kz[U];
   auto fetch_rows = [&](int q) __attribute__((always_inline)) {
+    auto go = [&](auto row) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      ku[i] = load_elem<T>(ru, off, (q + i) * step_u);
-      kd[i] = load_elem<T>(rd, off, (q + i) * step_d);
-    }
-    if (MODE != SCAN_SUM && a.z)
+      for (int i = 0; i < U; ++i) {
+        ku[i] = load_elem<T>(ru, off, row(q + i) * step_u);
+        kd[i] = load_elem<T>(rd, off, row(q + i) * step_d);
+      }
+      if (MODE != SCAN_SUM && a.z)
 #pragma unroll
-      for (int i = 0; i < U; ++i) kz[i] = load_elem<T>(rz, off, (q + i) * step_z);
+        for (int i = 0; i < U; ++i) kz[i] = load_elem<T>(rz, off, row(q + i) * step_z);
+    };
+    go([&](int r) __attribute__((always_inline)) { return row_or_last(r, rows); });
   };
 
   if (t0 < t1) {

@@ -100,12 +100,14 @@ __device__ __forceinline__ void store_quad4(O* p, const float* v, bool stream) {
 
 // ---- rows that lanes take an element of each ----
 // `rows` rows from `base` on, `pitch` elements apart, of `cols` elements: a lane's byte offset
-// in a row and the row's uniform one need no address arithmetic on the vector ALU. Past the
-// last row a load is 0 and a store does nothing (fewer than 2^31 bytes in all).
+// in a row and the row's uniform one need no address arithmetic on the vector ALU. The range
+// check is only asked about the lane's offset, which is the one that is past every row (fewer
+// than 2^31 bytes in all): the uniform one stays among the rows.
 template <typename T>
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_rsrc(const T* base, int rows, int64_t pitch, int cols) {
   return make_rsrc(base, ((int64_t)(rows - 1) * pitch + cols) * (int64_t)sizeof(T));
 }
+constexpr int row_or_last(int row, int rows) { return row < rows ? row : rows - 1; }
 template <typename T>
 __device__ __forceinline__ float load_elem(__amdgpu_buffer_rsrc_t r, unsigned off, int row) {
   if constexpr (sizeof(T) == 4)

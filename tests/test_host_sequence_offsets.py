@@ -30,3 +30,28 @@ constexpr bool inside() {
 }
 static_assert(inside(), "");
 """)
+
+
+def test_rows_asked_for_ahead_of_the_tokens_exist(tmp_path):
+    # stages of TT tokens, U at a time, the next U asked for before these are walked: also after the last
+    holds(tmp_path, r"""
+constexpr bool inside(int tokens, int TT, int U) {
+  for (int t = 0; t < tokens; t += TT) {
+    const int rows = tokens - t < TT + U ? tokens - t : TT + U;
+    for (int q = 0; q < TT + U; ++q) {
+      const int row = ct::row_or_last(q, rows);
+      if (row < 0 || t + row >= tokens) return false;
+      if (t + q < tokens && row != q) return false;
+    }
+  }
+  return true;
+}
+constexpr bool all_inside() {
+  for (int tokens = 1; tokens <= 140; ++tokens)
+    for (int TT : {4, 16, 32})
+      for (int U : {4, 8})
+        if (U <= TT && !inside(tokens, TT, U)) return false;
+  return true;
+}
+static_assert(all_inside(), "");
+""")
