@@ -151,9 +151,6 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs a) {
 }
 
 // ------------------------------------------------------------------ 16-byte groups of rows
-// Byte offset past every operand tile: reads as 0.
-constexpr unsigned kOobGroup = 0xFFFFFFF0u;
-
 // A group of bf16 at any element's address: the words around it, and, once they have arrived,
 // the group itself, shifted where it starts in the middle of a word, with all but its first
 // `left` elements masked to 0.
@@ -259,14 +256,17 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearAr
     const int k0 = k_begin + (c * WK + team) * KC;
     char* dst = lds + stage * STAGE + team * ROWS * ROWB + wave * BYTES;
     auto go = [&](auto tail) __attribute__((always_inline)) {
+      const unsigned k = (unsigned)(k0 * (int)sizeof(T));
+      const SliceView sw = slice_view(vw.bytes, k, tail.value), sx = slice_view(vx.bytes, k, tail.value);
+      const __amdgpu_buffer_rsrc_t tw = tail.value ? make_rsrc((const char*)vw.base + sw.base, sw.bytes) : rw,
+                                   tx = tail.value ? make_rsrc((const char*)vx.base + sx.base, sx.bytes) : rx;
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
         const bool out = tail.value && k0 + first(i) >= k_end;
         if constexpr (COPY > 0) {
-          copy_lds<COPY>(i < NW ? rw : rx, dst + i * WAVES * BYTES, out ? kOobGroup : off[i], k0 * (int)sizeof(T));
+          copy_lds<COPY>(i < NW ? tw : tx, dst + i * WAVES * BYTES, out ? kOobGroup : off[i], sw.uniform);
         } else {
-          held[stage][i].load(i < NW ? rw : rx,
-                              off[i] == kOobGroup || out ? kOobGroup : off[i] + (unsigned)(k0 * (int)sizeof(T)));
+          held[stage][i].load(i < NW ? rw : rx, off[i] == kOobGroup || out ? kOobGroup : off[i] + k);
         }
       }
     };

@@ -123,6 +123,23 @@ __device__ __forceinline__ void store_elem(__amdgpu_buffer_rsrc_t r, unsigned of
     __builtin_amdgcn_raw_buffer_store_b16(bf16_t(v).bits, r, (int)off, row, 0);
 }
 
+// ---- 16-byte groups, or words, of an operand's rows ----
+// Byte offset past every operand tile: reads as 0.
+constexpr unsigned kOobGroup = 0xFFFFFFF0u;
+// What the copies of a slice, k bytes into the rows of a buffer, are relative to. The range
+// check need not count a copy's uniform offset, and where it subtracts it from the buffer's
+// size the difference must not pass below 0: a slice of which every row has all bytes keeps k
+// there, less than any row holds; the last one, and those past the end, have a buffer that
+// starts with them.
+struct SliceView {
+  unsigned base, bytes;
+  int uniform;
+};
+constexpr SliceView slice_view(unsigned bytes, unsigned k, bool tail) {
+  if (!tail) return {0, bytes, (int)k};
+  return {k, k < bytes ? bytes - k : 0, 0};
+}
+
 // ---- scalar functions in fp32 ----
 constexpr float kLog2e = 1.4426950408889634f;
 // v_exp_f32: within an ulp, results below 2^-126 flushed to 0.

@@ -55,3 +55,36 @@ constexpr bool all_inside() {
 }
 static_assert(all_inside(), "");
 """)
+
+
+def test_copies_past_the_end_of_a_row_are_outside_by_any_range_check(tmp_path):
+    # slices of 128 bytes of rows of `row` bytes, `have` rows `pitch` apart, also the slices past the
+    # end; the check may look at the lane's offset alone or subtract the uniform one in 32 bits
+    holds(tmp_path, r"""
+constexpr bool sound(unsigned row, unsigned pitch, unsigned have, unsigned each) {
+  const unsigned bytes = (have - 1) * pitch + row;
+  for (unsigned k = 0; k < row + 3 * 128; k += 128)
+    for (unsigned r = 0; r < have + 2; ++r)
+      for (unsigned first = 0; first < 128; first += each) {
+        const bool exists = k + first < row, mine = r < have;
+        const ct::SliceView v = ct::slice_view(bytes, k, k + 128 > row);
+        const unsigned lane = mine && exists ? r * pitch + first : ct::kOobGroup, u = (unsigned)v.uniform;
+        const bool alone = lane < v.bytes, subtracted = lane < v.bytes - u;
+        if (mine && exists) {
+          if (!alone || !subtracted || v.base + lane + u != r * pitch + k + first ||
+              v.base + v.bytes > bytes || lane + u + each > v.bytes) return false;
+        } else if (alone || subtracted) {
+          return false;
+        }
+      }
+  return true;
+}
+constexpr bool all_sound() {
+  for (unsigned each : {4u, 16u})
+    for (unsigned row = each; row <= 400; row += each)
+      for (unsigned have : {1u, 2u, 5u})
+        if (!sound(row, row, have, each) || !sound(row, row + 3 * each, have, each)) return false;
+  return true;
+}
+static_assert(all_sound(), "");
+""")
