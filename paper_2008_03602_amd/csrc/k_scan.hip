@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
     r = find_tile(a.s, a.per, a.chunk, id, &t0);
     const bool hands_on = MODE == SCAN_OUT && a.fold && r.begin == r.end && t0 == r.begin;  // an empty sequence
     if (r.s < 0 || (t0 >= r.end && !hands_on)) return;
-    t1 = min(r.end, t0 + a.chunk);
+    t1 = tile_end(t0, r.end, a.chunk);
     if (MODE == SCAN_SUM && t1 == r.end && !a.fold) return;  // nothing follows this chunk
   }
   t0 = __builtin_amdgcn_readfirstlane(t0);

@@ -211,6 +211,8 @@ inline SeqTiles seq_tiles(const SeqView& v, int step) {
   const int per = v.len > step ? (v.len + step - 1) / step : 1;
   return {(int64_t)per * v.count, per};
 }
+// The end of a tile that starts at row t0 of a sequence: 2^31 rows may be less than a tile away.
+constexpr int tile_end(int t0, int end, int step) { return end - t0 > step ? t0 + step : end; }
 // The sequence that tile `id` belongs to (s = -1: none) and, in *first, the row that the tile
 // starts at: at or past the end for an unused number. Uniform over the wave, which looks
 // 64 sequences up at a time.

@@ -88,3 +88,18 @@ constexpr bool all_sound() {
 }
 static_assert(all_sound(), "");
 """)
+
+
+def test_tiles_end_within_their_sequence_up_to_the_most_rows(tmp_path):
+    holds(tmp_path, r"""
+constexpr int most = 0x7FFFFFFF - 4096;
+constexpr bool ends(int begin, int end, int step) {
+  for (int t = begin;; t = ct::tile_end(t, end, step)) {
+    const int e = ct::tile_end(t, end, step);
+    if (e < t || e > end || e - t > step || (e == t && t != end) || (e - t < step && e != end)) return false;
+    if (e == end) return true;
+  }
+}
+static_assert(ends(0, 0, 32) && ends(0, 1, 32) && ends(5, 37, 32) && ends(5, 38, 32) && ends(7, 1000, 8), "");
+static_assert(ends(0, most, 262144) && ends(most - 1, most, 262144) && ends(most - 300000, most, 262144), "");
+""")
