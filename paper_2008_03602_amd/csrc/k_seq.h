@@ -213,8 +213,13 @@ inline SeqTiles seq_tiles(const SeqView& v, int step) {
 }
 // The end of a tile that starts at row t0 of a sequence: 2^31 rows may be less than a tile away.
 constexpr int tile_end(int t0, int end, int step) { return end - t0 > step ? t0 + step : end; }
+// The row that tile k of a sequence starts at: its end at most, -1 for a number past that (and
+// perhaps far, where offsets do not ascend).
+constexpr int tile_start(int begin, int end, int step, int k) {
+  return k > (end - begin) / step ? -1 : begin + k * step;
+}
 // The sequence that tile `id` belongs to (s = -1: none) and, in *first, the row that the tile
-// starts at: at or past the end for an unused number. Uniform over the wave, which looks
+// starts at: the sequence's end for a number that it does not use. Uniform over the wave, which looks
 // 64 sequences up at a time.
 __device__ __forceinline__ SeqRange find_tile(const SeqView& v, int per, int step, int id, int* first) {
   if (!v.offsets) {
@@ -238,9 +243,8 @@ __device__ __forceinline__ SeqRange find_tile(const SeqView& v, int per, int ste
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
   const SeqRange r = seq_range(v, lo);
-  const int k = id - (r.begin / step + lo);  // past the sequence, and perhaps far, where offsets do not ascend
-  *first = k > v.tokens / step ? r.end : r.begin + k * step;
-  return r;
+  *first = tile_start(r.begin, r.end, step, id - (r.begin / step + lo));
+  return *first < 0 ? SeqRange{-1, 0, 0} : r;
 }
 
 }  // namespace ct

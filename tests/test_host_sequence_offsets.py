@@ -103,3 +103,23 @@ constexpr bool ends(int begin, int end, int step) {
 static_assert(ends(0, 0, 32) && ends(0, 1, 32) && ends(5, 37, 32) && ends(5, 38, 32) && ends(7, 1000, 8), "");
 static_assert(ends(0, most, 262144) && ends(most - 1, most, 262144) && ends(most - 300000, most, 262144), "");
 """)
+
+
+def test_tile_numbers_that_no_rows_use_start_nowhere(tmp_path):
+    # the last sequence is left with the numbers up to tokens / step, and with all of them where offsets do not ascend
+    holds(tmp_path, r"""
+constexpr int most = 0x7FFFFFFF - 4096;
+constexpr bool starts(int tokens, int begin, int end, int step) {
+  for (int k = 0; k <= tokens / step; k = k < 100 ? k + 1 : 2 * k) {
+    const int t = ct::tile_start(begin, end, step, k);
+    const bool used = (int64_t)begin + (int64_t)k * step < end || (k == 0 && begin == end);
+    if (used ? t != begin + k * step : t != -1 && t != end) return false;
+    if (begin == end && k > 0 && t != -1) return false;  // an empty sequence has one tile
+  }
+  const int last = ct::tile_start(begin, end, step, tokens / step);
+  return last == -1 || (last >= begin && last <= end);
+}
+static_assert(starts(100, 0, 100, 8) && starts(100, 3, 50, 8) && starts(100, 60, 60, 8) && starts(96, 0, 96, 32), "");
+static_assert(starts(most, 262143, most, 262144) && starts(most, 262143, most - 5, 262144), "");
+static_assert(starts(most, most - 3, most, 8) && starts(most, most, most, 8) && starts(most, most - 9, most - 9, 262144), "");
+""")
