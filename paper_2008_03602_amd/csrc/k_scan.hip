@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(64) scan_carry_kernel(ScanArgs a) {
   const int d = (int)(e / a.states);
   const SeqRange r = seq_range(a.s, s);
   const int slot = seq_slot(a.s, s);
-  const int n = __builtin_amdgcn_readfirstlane((r.end - r.begin + a.chunk - 1) / a.chunk);
+  const int n = __builtin_amdgcn_readfirstlane(tiles_in(r.end - r.begin, a.chunk));
   const int64_t id = a.s.offsets ? r.begin / a.chunk + s : (int64_t)s * a.per;
   float h = slot >= 0 && a.state_in ? a.state_in[(int64_t)slot * per_seq + e] : 0.f;
   if (n == 0) {
@@ -496,7 +496,7 @@ static int scan_prompt(ScanArgs a, const ScanPlan& p, hipStream_t st) {
   a.chunk = p.chunk;
   a.fold = p.fold;
   a.chunks = p.chunks;
-  a.per = a.s.offsets ? 0 : (a.s.len + p.chunk - 1) / p.chunk;
+  a.per = a.s.offsets ? 0 : tiles_in(a.s.len, p.chunk);
   a.ws_dt = a.ws + p.chunks * a.channels * a.states;
   int rc = scan_launch<T, NS, P, SCAN_SUM>(a, p.chunks, st);
   if (rc) return rc;

@@ -202,13 +202,14 @@ __device__ __forceinline__ int seq_slot(const SeqView& v, int s) {
 // owns the tile numbers from begin / step + s on: at least one, so that an empty sequence
 // has a tile too, and never more than begin to end can need. A few numbers at the end of a
 // sequence are unused.
+constexpr int tiles_in(int rows, int step) { return rows / step + (rows % step != 0); }
 struct SeqTiles {
   int64_t total;
   int per;  // tiles of each sequence where the lengths are equal
 };
 inline SeqTiles seq_tiles(const SeqView& v, int step) {
   if (v.offsets) return {(int64_t)v.tokens / step + v.count, 0};
-  const int per = v.len > step ? (v.len + step - 1) / step : 1;
+  const int per = v.len > step ? tiles_in(v.len, step) : 1;
   return {(int64_t)per * v.count, per};
 }
 // The end of a tile that starts at row t0 of a sequence: 2^31 rows may be less than a tile away.

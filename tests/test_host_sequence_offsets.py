@@ -123,3 +123,11 @@ static_assert(starts(100, 0, 100, 8) && starts(100, 3, 50, 8) && starts(100, 60,
 static_assert(starts(most, 262143, most, 262144) && starts(most, 262143, most - 5, 262144), "");
 static_assert(starts(most, most - 3, most, 8) && starts(most, most, most, 8) && starts(most, most - 9, most - 9, 262144), "");
 """)
+
+
+def test_tiles_are_counted_up_to_the_most_rows(tmp_path):
+    holds(tmp_path, r"""
+constexpr int most = 0x7FFFFFFF - 4096;
+static_assert(ct::tiles_in(0, 32) == 0 && ct::tiles_in(1, 32) == 1 && ct::tiles_in(32, 32) == 1 && ct::tiles_in(33, 32) == 2, "");
+static_assert(ct::tiles_in(most, 262144) == 8192 && ct::tiles_in(most, 8) == most / 8 + 1 && ct::tiles_in(most, most) == 1, "");
+""")
