@@ -8,8 +8,9 @@ Seven calls on one stream (``ct_linear_run`` four times, ``ct_causal_conv_run``,
 and nothing between them): the halves and slices are read in place through row pitches, and the
 residual is added in the last product's epilogue. Histories and states live in slots that the
 caller hands out, so prompts of unequal lengths, single tokens of many sequences and rows that
-belong to no sequence go through the same code. All buffers are made once for the most rows that
-a call may bring, and a call allocates nothing: it may be captured into a HIP graph.
+belong to no sequence go through the same code. Buffers are made once for the most rows that a
+call may bring, workspaces with the plans, and a call allocates nothing: it may be captured into
+a HIP graph.
 
 Usage: ``python -m paper_2008_03602_amd.sequence [--model 1024] [--tokens 2048] [--sequences 8]``:
 packed prompts and a decode loop of a block with random weights; prints one JSON line.
@@ -68,7 +69,7 @@ class SequenceBlock:
 
         self._xz, self._u, self._p = rows(2 * inner), rows(inner), rows(rank + 2 * states)
         self._step, self._y = rows(inner), rows(inner)
-        self._ws = None
+        self._workspaces = []  # each larger than the ones before; all of them, for graphs keep their addresses
 
     def reset(self) -> None:
         """Forgets every slot."""
@@ -83,7 +84,8 @@ class SequenceBlock:
         return L.make_sequences(rows, count, self.slots, max_len, offsets, slots)
 
     def plan(self, seqs: L.ct_sequences) -> dict:
-        """The calls' descriptions for these rows; grows the workspace to what they need."""
+        """The calls' descriptions for these rows, and a workspace of what they need. Workspaces are
+        kept as long as the block: a graph that was captured with one goes on using it."""
         m, dt, width = seqs.tokens, CODES[self.dtype], self.rank + 2 * self.states
         if m > self.max_rows:
             raise ValueError("%d rows, but the block's buffers hold %d" % (m, self.max_rows))
@@ -97,8 +99,9 @@ class SequenceBlock:
              "out": L.make_linear(m, self.model, self.inner, dt, dt, res=L.RES_ADD)}
         need = max([L.ct_linear_workspace(p[k]) for k in ("in", "x", "step", "out")] +
                    [L.ct_scan_workspace(p["scan"], seqs), 16])
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+        if not self._workspaces or self._workspaces[-1].numel() < need:
+            self._workspaces.append(torch.empty(need, dtype=torch.uint8, device="cuda"))
+        p["ws"] = self._workspaces[-1]
         return p
 
     def run(self, plan: dict, x: torch.Tensor, y: torch.Tensor) -> torch.Tensor:
@@ -108,7 +111,7 @@ class SequenceBlock:
             if t.dtype != self.dtype or not t.is_cuda or t.shape != (plan["seqs"].tokens, self.model) or \
                     not t.is_contiguous():
                 raise ValueError("x and y are contiguous device tensors of rows x model in the block's type")
-        st, ws, s = _stream(), self._ws, plan["seqs"]
+        st, ws, s = _stream(), plan["ws"], plan["seqs"]
         z, b, c = self._xz[:, self.inner:], self._p[:, self.rank:], self._p[:, self.rank + self.states:]
         L.ct_linear_run(plan["in"], x, self.w_in, None, None, self._xz, ws, st)
         L.ct_causal_conv_run(plan["conv"], s, self._xz, self.w_conv, self.b_conv, self.history, self.history, self._u, st)

@@ -1,0 +1,42 @@
+"""The sequence block as a program serves with it: what passes, plans and graphs leave to each other."""
+import pytest
+import torch
+
+from paper_2008_03602_amd import _lib as L
+from paper_2008_03602_amd.sequence import SequenceBlock
+from gpu_util import device_ready, note
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _device():
+    device_ready()
+    yield
+
+
+def test_a_captured_step_outlives_plans_of_longer_prompts():
+    """A step whose products use a workspace is replayed after a plan that needed a larger one."""
+    block = SequenceBlock(48, 4096, states=16, rank=8, slots=6, max_rows=512, dtype=torch.float32)
+    step = block.plan(block.sequences(4, 4, 1))
+    need = max(L.ct_linear_workspace(step[k]) for k in ("in", "x", "step", "out"))
+    assert need > 16
+    x, y = torch.randn(4, 48, device="cuda"), torch.empty(4, 48, device="cuda")
+    note("sequence block: a step with a workspace")
+    block.run(step, x, y)
+    block.reset()
+    block.run(step, x, y)
+    want, state = y.clone(), block.state.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        block.run(step, x, y)
+    plan = block.plan(block.sequences(512, 1))
+    assert plan["ws"].numel() > step["ws"].numel()
+    others = [torch.full((step["ws"].numel() + 4096 * i,), 7, dtype=torch.uint8, device="cuda") for i in range(8)]
+    for _ in range(3):
+        block.reset()
+        y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(block.state, state)
+    assert all((o == 7).all() for o in others)
