@@ -106,7 +106,8 @@ class SequenceBlock:
 
     def run(self, plan: dict, x: torch.Tensor, y: torch.Tensor) -> torch.Tensor:
         """One pass over x (rows x model) into y on the current stream; the slots move on. The
-        calls follow each other on one stream, so they share a workspace."""
+        calls follow each other on one stream, so they share a workspace. Rows of no sequence
+        come out as they went in."""
         for t in (x, y):
             if t.dtype != self.dtype or not t.is_cuda or t.shape != (plan["seqs"].tokens, self.model) or \
                     not t.is_contiguous():
@@ -117,6 +118,8 @@ class SequenceBlock:
         L.ct_causal_conv_run(plan["conv"], s, self._xz, self.w_conv, self.b_conv, self.history, self.history, self._u, st)
         L.ct_linear_run(plan["x"], self._u, self.w_x, None, None, self._p, ws, st)
         L.ct_linear_run(plan["step"], self._p, self.w_step, None, None, self._step, ws, st)
+        if s.offsets:  # the scan writes no row of no sequence, and the last product takes them all
+            self._y[:s.tokens].zero_()
         L.ct_scan_run(plan["scan"], s, self._u, self._step, self.b_step, self.a, b, c, self.skip, z, self.state,
                       self.state, self._y, ws, st)
         L.ct_linear_run(plan["out"], self._y, self.w_out, None, x, y, ws, st)

@@ -40,3 +40,24 @@ def test_a_captured_step_outlives_plans_of_longer_prompts():
         torch.cuda.synchronize()
         assert torch.equal(y, want) and torch.equal(block.state, state)
     assert all((o == 7).all() for o in others)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_of_no_sequence_pass_through(dtype):
+    """Nothing of an earlier pass, or of memory that was never written, is left in them."""
+    block = SequenceBlock(48, 96, states=16, rank=8, slots=6, max_rows=160, dtype=dtype)
+    for t in (block._xz, block._u, block._p, block._step, block._y):
+        t.fill_(float("nan"))
+    g = torch.Generator().manual_seed(5)
+    off = torch.tensor([3, 63, 63, 64, 97], dtype=torch.int32).cuda()  # rows 0-2 and 97-99 belong to nobody
+    nobody = [0, 1, 2, 97, 98, 99]
+    packed, full = block.plan(block.sequences(100, 4, 0, off)), block.plan(block.sequences(100, 2))
+    for i in range(2):
+        x = torch.randn(100, 48, generator=g).to(dtype).cuda()
+        y = torch.full_like(x, float("nan"))
+        note("sequence block: rows of nobody, pass %d" % i)
+        block.run(packed, x, y)
+        assert torch.equal(y[nobody], x[nobody]), i
+        assert torch.isfinite(y).all() and not torch.equal(y[3:97], x[3:97])
+        block.run(full, torch.randn(100, 48, generator=g).to(dtype).cuda(), y)  # leaves every row of the buffers full
+        assert torch.isfinite(y).all()
