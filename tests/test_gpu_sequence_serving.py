@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2008_03602_amd import _lib as L
-from paper_2008_03602_amd.sequence import SequenceBlock
+from paper_2008_03602_amd.sequence import SequenceBlock, serve
 from gpu_util import device_ready, note
 
 pytestmark = pytest.mark.gpu
@@ -61,3 +61,21 @@ def test_rows_of_no_sequence_pass_through(dtype):
         assert torch.isfinite(y).all() and not torch.equal(y[3:97], x[3:97])
         block.run(full, torch.randn(100, 48, generator=g).to(dtype).cuda(), y)  # leaves every row of the buffers full
         assert torch.isfinite(y).all()
+
+
+@pytest.mark.parametrize("lens", [[20, 0, 7, 0], [0, 9], [0, 0, 0]])
+def test_sequences_without_a_prompt_start_from_zeros(lens):
+    block = SequenceBlock(48, 96, states=16, rank=8, slots=6, max_rows=160, dtype=torch.float32)
+    note("sequence block: prompts %s" % lens)
+    r = serve(block, lens, 3)
+    steps = r["steps"]
+    assert torch.isfinite(steps).all()
+    alone = serve(block, [0], 3)["steps"][:, 0]  # the same sequence with nobody beside it
+    at = 0
+    for i, n in enumerate(lens):
+        if n:
+            at += n
+            assert torch.equal(steps[0, i], torch.tanh(r["prompt"][at - 1]))
+        else:
+            assert not steps[0, i].any()
+            assert torch.equal(steps[:, i], alone)
