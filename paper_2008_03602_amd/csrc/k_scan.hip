@@ -137,25 +137,43 @@ __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
   const int d = group * a.per_group + (live ? ch : a.per_group - 1), n0 = part * NS;  // spare lanes repeat a channel
   const int left = a.states - n0;
 
-  Vals<NS> la = load_vals<NS>(a.a + (int64_t)d * a.states + n0, left, rows_of_four(a.a, a.states));
+  // Lanes have NP states. Those past the last one repeat states from the first on, so that no
+  // product in them is NaN where the state's own is not (of an infinite step or input and a
+  // state of zeros it would be), and c of a copy is small enough to add nothing that counts.
+  const bool spare = a.states < NP;
+  const float inv = spare ? 1.f / (float)a.states : 0.f;
+  // Arrays of channels x states from uniform addresses on, which leaves the lanes one offset: at
+  // most 2^31 bytes, for rows of u hold fewer than 2^21 channels.
+  const unsigned at = ((unsigned)d * (unsigned)a.states + (unsigned)n0) * 4u;
+  auto load_states = [&](const float* all, bool vec) __attribute__((always_inline)) {
+    if (!spare) return load_vals<NS>((const float*)((const char*)all + at), NS, vec);
+    Vals<NS> r;
+#pragma unroll
+    for (int i = 0; i < NS; ++i)
+      r.v[i] = *(const float*)((const char*)all + (at + (unsigned)(i - qdiv(n0 + i, inv) * a.states) * 4u));
+    return r;
+  };
+  auto store_states = [&](float* all, const Vals<NS>& v, bool vec) __attribute__((always_inline)) {
+    store_vals<NS>((float*)((char*)all + at), v.v, left, vec, false);
+  };
+
+  Vals<NS> la = load_states(a.a, rows_of_four(a.a, a.states));
 #pragma unroll
   for (int i = 0; i < NS; ++i) la.v[i] *= kLog2e;
-  const int slot = MODE == SCAN_SUM && !a.fold ? -1 : seq_slot(a.s, r.s);
-  const int64_t at = ((int64_t)slot * a.channels + d) * a.states + n0;
-  const int64_t in_ws = ((int64_t)id * a.channels + d) * a.states + n0;
+  const int slot = MODE == SCAN_SUM && !a.fold ? -1 : __builtin_amdgcn_readfirstlane(seq_slot(a.s, r.s));
+  const int64_t per_chunk = (int64_t)a.channels * a.states, in_state = slot * per_chunk, in_ws = id * per_chunk;
   Vals<NS> h = {};
   const bool vec_ws = rows_of_four(a.ws, a.states);
   if (MODE == SCAN_WHOLE || (MODE == SCAN_SUM ? a.fold && t1 == r.end : t0 == t1)) {
-    if (slot >= 0 && a.state_in) h = load_vals<NS>(a.state_in + at, left, rows_of_four(a.state_in, a.states));
+    if (slot >= 0 && a.state_in) h = load_states(a.state_in + in_state, rows_of_four(a.state_in, a.states));
     if constexpr (MODE == SCAN_SUM) {
-      if (live) store_vals<NS>(a.ws + in_ws, h.v, left, vec_ws, false);
+      if (live) store_states(a.ws + in_ws, h, vec_ws);
       return;
     }
   } else if constexpr (MODE == SCAN_OUT) {
-    const int64_t per_chunk = (int64_t)a.channels * a.states;
     const int before = a.fold ? (t0 - r.begin) / a.chunk : 0;
     const int at_start = a.fold ? (r.end - t0 - 1) / a.chunk : 0;  // chunks up to the last
-    h = load_vals<NS>(a.ws + in_ws + at_start * per_chunk, left, vec_ws);
+    h = load_states(a.ws + in_ws + at_start * per_chunk, vec_ws);
     constexpr int F = NS <= 4 ? 8 : 2;
     const float *end = a.ws + in_ws - before * per_chunk, *sum = a.ws_dt + (int64_t)(id - before) * a.channels + d;
     for (int k = 0; k < before; k += F) {
@@ -164,7 +182,9 @@ __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
 #pragma unroll
       for (int i = 0; i < F; ++i) {
         const int c = min(k + i, before - 1);
-        e[i] = load_vals<NS>(end + c * per_chunk, left, vec_ws);
+        // lanes of more than four states have none to spare here (plan_scan)
+        if constexpr (NS <= 4) e[i] = load_states(end + c * per_chunk, vec_ws);
+        else e[i] = load_vals<NS>((const float*)((const char*)(end + c * per_chunk) + at), NS, vec_ws);
         dt[i] = sum[(int64_t)c * a.channels];
       }
 #pragma unroll
@@ -177,14 +197,19 @@ __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
   const float bias = a.dt_bias ? a.dt_bias[d] : 0.f, skip = a.d_skip ? a.d_skip[d] : 0.f;
   float total = 0.f;
 
-  // staging
+  // staging: a thread's values are all of one state
   T kb[STAGED], kc[STAGED];
+  const int nb = (int)threadIdx.x % NP, copies = spare ? qdiv(nb, inv) : 0;
+  const float weight = copies ? 0x1p-28f : 1.f;
   auto fetch = [&](int t) __attribute__((always_inline)) {
+    int at_n = nb - copies * a.states;
+    asm volatile("" : "+v"(at_n));  // or addresses are held from stage to stage, and waves on a SIMD are fewer
+    at_n += group * a.states;
 #pragma unroll
     for (int i = 0; i < STAGED; ++i) {
-      const int e = i * 256 + (int)threadIdx.x, row = e / NP, n = e % NP;
-      const bool ok = row < TT && t + row < t1 && n < a.states;
-      const int64_t tok = ok ? t + row : t0, at_n = (int64_t)group * a.states + (ok ? n : 0);
+      const int row = (i * 256 + (int)threadIdx.x) / NP;
+      const bool ok = row < TT && t + row < t1;
+      const int64_t tok = ok ? t + row : t0;
       const T vb = ((const T*)a.b)[tok * a.ldb + at_n];
       kb[i] = ok ? vb : (T)0.f;
       if constexpr (MODE != SCAN_SUM) {
@@ -199,7 +224,7 @@ __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
       const int e = i * 256 + (int)threadIdx.x;
       if (TT * NP >= 256 || e < TT * NP) {
         (&sb[s][0][0])[e] = (float)kb[i];
-        if constexpr (MODE != SCAN_SUM) (&sc[s][0][0])[e] = (float)kc[i];
+        if constexpr (MODE != SCAN_SUM) (&sc[s][0][0])[e] = (float)kc[i] * weight;
       }
     }
   };
@@ -284,10 +309,10 @@ __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
   }
   if (!live) return;
   if constexpr (MODE == SCAN_SUM) {
-    store_vals<NS>(a.ws + in_ws, h.v, left, vec_ws, false);
+    store_states(a.ws + in_ws, h, vec_ws);
     if (part == 0) a.ws_dt[(int64_t)id * a.channels + d] = total;
   } else if (slot >= 0 && a.state_out && t1 == r.end) {
-    store_vals<NS>(a.state_out + at, h.v, left, rows_of_four(a.state_out, a.states), false);
+    store_states(a.state_out + in_state, h, rows_of_four(a.state_out, a.states));
   }
 }
 
@@ -413,7 +438,7 @@ __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
 #pragma unroll
     for (int i = 0; i < NS; ++i) {
       h[q].v[i] = fmaf(__builtin_amdgcn_exp2f(step * (la.v[i] * kLog2e)), h[q].v[i], du * b[q].v[i]);
-      y = fmaf(c[q].v[i], h[q].v[i], y);
+      y = i < left ? fmaf(c[q].v[i], h[q].v[i], y) : y;  // past the last state h may be NaN
     }
     y = fmaf(skip, u[q], add_lanes<P>(y));
     if (a.z) y *= silu_f32(z[q]);
@@ -473,7 +498,10 @@ ScanPlan plan_scan(const ct_scan_op& op, const ct_sequences& s) {
   p.chunk = (int)chunk;
   // Up to eight chunks of a sequence: folding saves 2.7 us. Of 16 it takes as long as the
   // carries (1 x 512 tokens of 2048 channels 24 and 27 us, 8 x 512 81 and 76), of more longer.
-  p.fold = most <= 8 * chunk;
+  // Where lanes of eight or 16 states have some to spare, the repeated ones' ends would cost
+  // the outputs a wave of four on a SIMD.
+  const int lanes_states = p.narrow || op.states > 8 ? (p.narrow ? 4 : 16) * prompt_parts(op.states, p.narrow) : 8;
+  p.fold = most <= 8 * chunk && (p.narrow || op.states == lanes_states);
   p.chunks = s.offsets ? s.tokens / chunk + s.count : (int64_t)s.count * ((most + chunk - 1) / chunk);
   p.ws_floats = p.chunks * op.channels * (op.states + 1);
   return p;

@@ -1,0 +1,70 @@
+"""The sequence-block operators where values are infinite or zero and sizes take each kernel, against
+their formulas in 64 bits."""
+import pytest
+import torch
+
+from paper_2008_03602_amd import _lib as L
+from gpu_util import device_ready, note
+from test_gpu_sequence import B, CODE, F, layout, scan64, scan_inputs, stream
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _device():
+    device_ready()
+    yield
+
+
+def scan(s, off, slots, dtype, uniform, softplus=True):
+    """y and the new states of scan_inputs `s`."""
+    channels, states, tokens = s["u"].shape[1], s["a"].shape[1], s["u"].shape[0]
+    op = L.make_scan(channels, states, s["groups"], CODE[dtype], softplus)
+    seqs = L.make_sequences(tokens, len(slots), s["state"].shape[0], 0, None if uniform else off.cuda(), slots.cuda())
+    c = {k: v.cuda() if torch.is_tensor(v) else v for k, v in s.items()}
+    y, out = torch.empty_like(c["u"]), c["state"].clone()
+    ws = torch.full((max(1, L.ct_scan_workspace(op, seqs)),), 255, dtype=torch.uint8, device="cuda")
+    L.ct_scan_run(op, seqs, c["u"], c["delta"], c["dt_bias"], c["a"], c["b"], c["c"], c["d"], c["z"], c["state"], out, y,
+                  ws, stream())
+    torch.cuda.synchronize()
+    return y, out
+
+
+def same_kinds(got, ref, bound, what):
+    """NaN, infinities (with their signs) and finite values in the same places, and these within their bound."""
+    got = got.detach().cpu().double()
+    assert torch.equal(torch.isnan(got), torch.isnan(ref)), what + ": NaN in other places"
+    inf = torch.isinf(ref)
+    assert torch.equal(torch.isinf(got), inf), what + ": infinities in other places"
+    assert torch.equal(got[inf], ref[inf]), what + ": signs of infinities"
+    fine = torch.isfinite(ref)
+    worst = ((got - ref).abs()[fine] / (bound[fine] + 1e-38)).max().item()
+    assert worst <= 1.0, "%s: error %.2f times the bound" % (what, worst)
+
+
+SPARE = [1, 3, 4, 5, 7, 8, 9, 13, 16, 17, 24, 33, 40, 64, 100, 132, 200]
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("states,lens,channels", [
+    (n, lens, 70) for n in SPARE for lens in ([1] * 5, [12, 0, 5], [190, 0, 70])] + [
+    (n, [40] * 30, 1100) for n in SPARE if n <= 40])  # enough for lanes of eight and 16 states
+def test_scan_infinities_are_the_same_of_any_number_of_states(states, lens, channels, dtype):
+    """An infinite input, step, state and coefficient: what the formula makes of them, whether or not a
+    lane has states to spare. b, c, d and the inputs are positive, so that no infinities cancel."""
+    uniform = len(set(lens)) == 1
+    off, slots, n, tokens = layout(lens, seed=states)
+    s = scan_inputs(tokens, channels, states, 1, dtype, n, states)
+    for k in ("u", "b", "c", "d", "z"):
+        s[k] = s[k].abs() + 0.1
+    s["a"], s["state"] = -0.05 - 0.1 * torch.rand(s["a"].shape), s["state"].abs()
+    inf = float("inf")
+    s["u"][1, 3], s["delta"][0, 11], s["u"][tokens - 1, 5] = inf, inf, inf
+    s["state"][int(slots[0]), 17, states - 1] = inf
+    s["z"][2, 23] = inf
+    note("scan of infinities: %s ch%d n%d %s" % (lens, channels, states, dtype))
+    y, out = scan(s, off, slots, dtype, uniform)
+    y64, new, ybound, nbound = scan64(s, off, slots, True, dtype)
+    assert torch.isinf(y64).sum() >= 3 and torch.isfinite(y64).any()
+    same_kinds(out, new, nbound, "state")
+    same_kinds(y, y64, ybound, "y")
