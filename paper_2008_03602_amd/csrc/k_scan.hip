@@ -99,6 +99,14 @@ __device__ __forceinline__ float add_lanes(float v) {
   return v;
 }
 
+// A state over a whole chunk: exp2(x) h + end, as it comes token by token. The factor is that of
+// half of x, twice, so that it does not leave fp32 where its product with h would not, and kept
+// finite and above 0, so that a state of 0 stays 0 and an infinite one infinite.
+__device__ __forceinline__ float over_chunk(float half_x, float h, float end) {
+  const float f = __builtin_amdgcn_fmed3f(__builtin_amdgcn_exp2f(half_x), 0x1p-126f, 0x1p127f);
+  return fmaf(f * h, f, end);  // where x is NaN, so is the end
+}
+
 // ------------------------------------------------------------------ prompts
 enum ScanMode { SCAN_WHOLE, SCAN_SUM, SCAN_OUT };
 
@@ -143,7 +151,7 @@ __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
   const bool spare = a.states < NP;
   const float inv = spare ? 1.f / (float)a.states : 0.f;
   // Arrays of channels x states from uniform addresses on, which leaves the lanes one offset: at
-  // most 2^31 bytes, for rows of u hold fewer than 2^21 channels.
+  // most 2^31 bytes, for rows of u hold 2^21 channels at most.
   const unsigned at = ((unsigned)d * (unsigned)a.states + (unsigned)n0) * 4u;
   auto load_states = [&](const float* all, bool vec) __attribute__((always_inline)) {
     if (!spare) return load_vals<NS>((const float*)((const char*)all + at), NS, vec);
@@ -185,13 +193,13 @@ __global__ void __launch_bounds__(256) scan_kernel(ScanArgs a) {
         // lanes of more than four states have none to spare here (plan_scan)
         if constexpr (NS <= 4) e[i] = load_states(end + c * per_chunk, vec_ws);
         else e[i] = load_vals<NS>((const float*)((const char*)(end + c * per_chunk) + at), NS, vec_ws);
-        dt[i] = sum[(int64_t)c * a.channels];
+        dt[i] = 0.5f * sum[(int64_t)c * a.channels];
       }
 #pragma unroll
       for (int i = 0; i < F; ++i)
         if (k + i < before)
 #pragma unroll
-          for (int n = 0; n < NS; ++n) h.v[n] = fmaf(__builtin_amdgcn_exp2f(dt[i] * la.v[n]), h.v[n], e[i].v[n]);
+          for (int n = 0; n < NS; ++n) h.v[n] = over_chunk(dt[i] * la.v[n], h.v[n], e[i].v[n]);
     }
   }
   const float bias = a.dt_bias ? a.dt_bias[d] : 0.f, skip = a.d_skip ? a.d_skip[d] : 0.f;
@@ -336,7 +344,7 @@ __global__ void __launch_bounds__(64) scan_carry_kernel(ScanArgs a) {
     if (slot >= 0 && a.state_out) a.state_out[(int64_t)slot * per_seq + e] = h;
     return;
   }
-  const float la = a.a[e] * kLog2e;
+  const float half_la = a.a[e] * (0.5f * kLog2e);
   float* p = a.ws + id * per_seq + e;
   const float* dt = a.ws_dt + id * a.channels + d;
   constexpr int F = 8;
@@ -354,7 +362,7 @@ __global__ void __launch_bounds__(64) scan_carry_kernel(ScanArgs a) {
     for (int i = 0; i < F; ++i)
       if (c + i < n - 1) {
         p[(int64_t)(c + i) * per_seq] = h;
-        h = fmaf(__builtin_amdgcn_exp2f(la * sum[u][i]), h, end[u][i]);
+        h = over_chunk(half_la * sum[u][i], h, end[u][i]);
       }
   };
   if (n > 1) {

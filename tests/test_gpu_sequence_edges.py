@@ -68,3 +68,41 @@ def test_scan_infinities_are_the_same_of_any_number_of_states(states, lens, chan
     assert torch.isinf(y64).sum() >= 3 and torch.isfinite(y64).any()
     same_kinds(out, new, nbound, "state")
     same_kinds(y, y64, ybound, "y")
+
+
+@pytest.mark.parametrize("states,channels", [(16, 66), (13, 66), (40, 66), (16, 4100)])
+@pytest.mark.parametrize("lens", [[50, 190], [50, 350], [400]])  # 240 rows are a few chunks
+def test_scan_of_cut_sequences_neither_over_nor_underflows_on_its_own(lens, states, channels):
+    """Decays of a whole chunk leave fp32 where those of its tokens and the states do not."""
+    off, slots, n, tokens = layout(lens, seed=1)
+    inf, ln2 = float("inf"), 0.6931471805599453
+    s = scan_inputs(tokens, channels, states, 1, F, n, 7)
+    for k in ("b", "c", "d", "z"):
+        s[k] = s[k].abs() + 0.1
+    s["dt_bias"].zero_()
+    s["a"] = -0.01 - 0.02 * torch.rand(channels, states)
+    s["delta"] = 0.1 * torch.rand(tokens, channels)
+    # channel 1: the states grow by 4.1 bits a token, but there is nothing to grow until the last eight
+    s["a"][1], s["delta"][:, 1] = 4.1 * ln2, 1.0
+    s["u"][:, 1] = 0.0
+    for e in off[1:].tolist():
+        s["u"][e - 8:e, 1] = 0.5
+    s["state"][:, 1] = 0.0
+    # channel 2: infinite states that are forgotten by 6 bits a token
+    s["a"][2], s["delta"][:, 2] = -6.0 * ln2, 1.0
+    s["state"][:, 2] = inf
+    # channel 3: states of 2^-120 that grow by 4.1 bits a token, 45 tokens long
+    s["a"][3], s["delta"][:, 3], s["u"][:, 3] = 4.1 * ln2, 0.0, 0.0
+    for b in off[:-1].tolist():
+        s["delta"][b:b + 45, 3] = 1.0
+    s["state"][:, 3] = 2.0 ** -120
+    note("scan over chunks: %s ch%d n%d" % (lens, channels, states))
+    y, out = scan(s, off, slots, F, False, softplus=False)
+    few = torch.cat([torch.arange(40), torch.arange(channels - 20, channels)])  # the reference's channels
+    part = {k: v[..., few] if k in ("u", "delta", "z") else v[few] if k in ("dt_bias", "a", "d") else
+            v[:, few] if k == "state" else v for k, v in s.items()}
+    y64, new, ybound, nbound = scan64(part, off, slots, False, F)
+    used = slots.long()
+    assert torch.isinf(new[used][:, 2]).all() and torch.isfinite(new[used][:, [1, 3]]).all()
+    same_kinds(out[:, few], new, nbound, "state")
+    same_kinds(y[:, few], y64, ybound, "y")
