@@ -203,7 +203,7 @@ def _arr(a, ctype):
 
 def _ptr(t) -> int:
     """Device address of a torch tensor (or an int address)."""
-    return t if t is None or t.__class__ is int else t.data_ptr()
+    return t if t is None or isinstance(t, int) else t.data_ptr()
 
 
 # ---------------------------------------------------------------- structs
@@ -609,7 +609,7 @@ def ct_linear_workspace(op: ct_linear_op) -> int:
 
 def _ws(ws, nbytes):
     """(address, bytes) of a workspace tensor, or of an address with its size."""
-    if ws is None or ws.__class__ is int:
+    if ws is None or isinstance(ws, int):
         return ws, nbytes
     return ws.data_ptr(), ws.numel() * ws.element_size()
 

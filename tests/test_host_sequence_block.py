@@ -40,3 +40,14 @@ def test_a_plan_keeps_its_workspace_when_a_larger_one_is_made(monkeypatch):
     del step, prompt, again
     gc.collect()
     assert made[0][1]() is not None and made[1][1]() is not None
+
+
+def test_addresses_may_be_of_any_kind_of_int():
+    class Address(int):
+        pass
+
+    a = Address(0x1000)
+    assert L._ptr(a) == 0x1000 and L._ptr(None) is None and L._ptr(torch.empty(1)) > 0
+    assert L._ws(a, 64) == (0x1000, 64)
+    none = L.make_linear(0, 24, 16, L.DT_BF16, L.DT_F32)
+    L.ct_linear_run(none, a, a, a, a, a, a, 0, 64)
