@@ -5,7 +5,7 @@ import torch
 
 from paper_2008_03602_amd import _lib as L
 from gpu_util import device_ready, note
-from test_gpu_sequence import B, CODE, F, layout, scan64, scan_inputs, stream
+from test_gpu_sequence import B, CODE, F, check_conv, check_scan, layout, scan64, scan_inputs, stream, within
 
 pytestmark = pytest.mark.gpu
 
@@ -106,3 +106,53 @@ def test_scan_of_cut_sequences_neither_over_nor_underflows_on_its_own(lens, stat
     assert torch.isinf(new[used][:, 2]).all() and torch.isfinite(new[used][:, [1, 3]]).all()
     same_kinds(out[:, few], new, nbound, "state")
     same_kinds(y[:, few], y64, ybound, "y")
+
+
+# ------------------------------------------------------------------ sizes that take each kernel
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("states,groups,channels", [(16, 1, 2050), (13, 2, 2052), (32, 2, 1030), (20, 1, 1030), (64, 1, 516),
+                                                    (40, 2, 516), (100, 1, 260), (128, 2, 520), (200, 1, 520), (256, 2, 260)])
+def test_scan_of_single_tokens_two_sequences_a_wave(states, groups, channels, dtype):
+    """As many waves as that takes (16 for each SIMD), and an odd number of sequences."""
+    lanes = 4 if states <= 16 else 8 if states <= 32 else 16
+    count = 16 * 1024 * 64 // (lanes * channels) + 1
+    count += 1 - count % 2
+    check_scan([1] * count, channels, states, groups, dtype, uniform=True, seed=states, unused=(0, 3))
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("states", [4, 8, 12, 20, 24, 28, 36, 60, 68, 132, 252])
+def test_scan_of_single_tokens_with_lanes_to_spare(states, dtype):
+    """States of whole quads that leave whole lanes without any."""
+    check_scan([1] * 3, 36, states, 2, dtype, uniform=True, seed=states)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("width", range(2, 9))
+def test_conv_of_an_odd_number_of_channels(width, dtype):
+    """An element a lane, every width."""
+    check_conv([0, 1, width - 1, width, 16, 17, 33], 41, width, dtype, seed=width)
+    check_conv([1] * 5, 41, width, dtype, uniform=True, seed=width + 1, unused=(2,))
+    check_conv([21] * 3, 41, width, dtype, uniform=True, in_place=True, seed=width + 2)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("lens,channels,states,chunk", [([9001, 0, 4530], 2050, 16, 64), ([13600], 2048, 13, 64),
+                                                        ([5000, 1, 3333], 6000, 16, 96), ([4000, 3000], 2049, 40, 96)])
+def test_scan_chunks_of_several_stages(lens, channels, states, chunk, dtype):
+    """Chunks that are longer than what is staged at a time, the last of them ragged."""
+    uniform = len(set(lens)) == 1 and len(lens) > 1
+    off, slots, n, tokens = layout(lens, seed=3)
+    s = scan_inputs(tokens, channels, states, 1, dtype, n, 9)
+    chunks = sum(-(-l // chunk) for l in lens) if uniform else tokens // chunk + len(lens)
+    op = L.make_scan(channels, states, 1, CODE[dtype])
+    seqs = L.make_sequences(tokens, len(lens), n, 0, None if uniform else off.cuda())
+    assert L.ct_scan_workspace(op, seqs) == chunks * channels * (states + 1) * 4
+    note("scan of long chunks: %s ch%d n%d %s" % (lens, channels, states, dtype))
+    y, out = scan(s, off, slots, dtype, uniform)
+    few = torch.tensor([0, 1, 63, 64, 257, channels // 2, channels - 2, channels - 1])  # the reference's channels
+    part = {k: v[..., few] if k in ("u", "delta", "z") else v[few] if k in ("dt_bias", "a", "d") else
+            v[:, few] if k == "state" else v for k, v in s.items()}
+    y64, new, ybound, nbound = scan64(part, off, slots, True, dtype)
+    within(out[:, few], new, nbound, "state")
+    within(y[:, few], y64, ybound, "y")

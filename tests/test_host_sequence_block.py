@@ -51,3 +51,9 @@ def test_addresses_may_be_of_any_kind_of_int():
     assert L._ws(a, 64) == (0x1000, 64)
     none = L.make_linear(0, 24, 16, L.DT_BF16, L.DT_F32)
     L.ct_linear_run(none, a, a, a, a, a, a, 0, 64)
+
+
+def test_long_reductions_and_long_prompts_need_their_workspaces():
+    """What the refusals of a wrong workspace are tested on."""
+    assert L.ct_linear_workspace(L.make_linear(96, 64, 16384, L.DT_BF16, L.DT_F32)) > 0
+    assert L.ct_scan_workspace(L.make_scan(256, 16, 1, 1), L.make_sequences(8192, 1, 1)) > 0
