@@ -43,7 +43,6 @@ struct ScanArgs {
   int vec_bc;         // rows of b and c take accesses of four values
   int per, chunk;     // chunks of a sequence where all are equal, tokens of a chunk
   int fold;           // a chunk's outputs fold the chunks before it; no carries
-  int64_t chunks;
   FastDiv dtiles, dgroup;  // channel tiles in all, and of one group
 };
 
@@ -531,7 +530,6 @@ static int scan_prompt(ScanArgs a, const ScanPlan& p, hipStream_t st) {
   if (!p.chunk) return scan_launch<T, NS, P, SCAN_WHOLE>(a, a.s.count, st);
   a.chunk = p.chunk;
   a.fold = p.fold;
-  a.chunks = p.chunks;
   a.per = a.s.offsets ? 0 : tiles_in(a.s.len, p.chunk);
   a.ws_dt = a.ws + p.chunks * a.channels * a.states;
   int rc = scan_launch<T, NS, P, SCAN_SUM>(a, p.chunks, st);
