@@ -257,14 +257,12 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearAr
     char* dst = lds + stage * STAGE + team * ROWS * ROWB + wave * BYTES;
     auto go = [&](auto tail) __attribute__((always_inline)) {
       const unsigned k = (unsigned)(k0 * (int)sizeof(T));
-      const SliceView sw = slice_view(vw.bytes, k, tail.value), sx = slice_view(vx.bytes, k, tail.value);
-      const __amdgpu_buffer_rsrc_t tw = tail.value ? make_rsrc((const char*)vw.base + sw.base, sw.bytes) : rw,
-                                   tx = tail.value ? make_rsrc((const char*)vx.base + sx.base, sx.bytes) : rx;
+      const int kw = tail.value ? uniform_part(k, vw.bytes) : (int)k, kx = tail.value ? uniform_part(k, vx.bytes) : (int)k;
 #pragma unroll
       for (int i = 0; i < NC; ++i) {
         const bool out = tail.value && k0 + first(i) >= k_end;
         if constexpr (COPY > 0) {
-          copy_lds<COPY>(i < NW ? tw : tx, dst + i * WAVES * BYTES, out ? kOobGroup : off[i], sw.uniform);
+          copy_lds<COPY>(i < NW ? rw : rx, dst + i * WAVES * BYTES, out ? kOobGroup : off[i], i < NW ? kw : kx);
         } else {
           held[stage][i].load(i < NW ? rw : rx, off[i] == kOobGroup || out ? kOobGroup : off[i] + k);
         }

@@ -126,19 +126,11 @@ __device__ __forceinline__ void store_elem(__amdgpu_buffer_rsrc_t r, unsigned of
 // ---- 16-byte groups, or words, of an operand's rows ----
 // Byte offset past every operand tile: reads as 0.
 constexpr unsigned kOobGroup = 0xFFFFFFF0u;
-// What the copies of a slice, k bytes into the rows of a buffer, are relative to. The range
-// check need not count a copy's uniform offset, and where it subtracts it from the buffer's
-// size the difference must not pass below 0: a slice of which every row has all bytes keeps k
-// there, less than any row holds; the last one, and those past the end, have a buffer that
-// starts with them.
-struct SliceView {
-  unsigned base, bytes;
-  int uniform;
-};
-constexpr SliceView slice_view(unsigned bytes, unsigned k, bool tail) {
-  if (!tail) return {0, bytes, (int)k};
-  return {k, k < bytes ? bytes - k : 0, 0};
-}
+// The uniform offset of copies k bytes into the rows of a buffer. The range check need not count
+// it, and where it subtracts it from the buffer's size the difference must not pass below 0,
+// which a slice past the end of a single row's would bring about: it stops at the buffer's end,
+// where no lane has anything to copy.
+constexpr int uniform_part(unsigned k, unsigned bytes) { return (int)(k < bytes ? k : bytes); }
 
 // ---- scalar functions in fp32 ----
 constexpr float kLog2e = 1.4426950408889634f;

@@ -67,12 +67,11 @@ constexpr bool sound(unsigned row, unsigned pitch, unsigned have, unsigned each)
     for (unsigned r = 0; r < have + 2; ++r)
       for (unsigned first = 0; first < 128; first += each) {
         const bool exists = k + first < row, mine = r < have;
-        const ct::SliceView v = ct::slice_view(bytes, k, k + 128 > row);
-        const unsigned lane = mine && exists ? r * pitch + first : ct::kOobGroup, u = (unsigned)v.uniform;
-        const bool alone = lane < v.bytes, subtracted = lane < v.bytes - u;
+        const unsigned lane = mine && exists ? r * pitch + first : ct::kOobGroup;
+        const unsigned u = (unsigned)ct::uniform_part(k, bytes);
+        const bool alone = lane < bytes, subtracted = lane < bytes - u;
         if (mine && exists) {
-          if (!alone || !subtracted || v.base + lane + u != r * pitch + k + first ||
-              v.base + v.bytes > bytes || lane + u + each > v.bytes) return false;
+          if (!alone || !subtracted || lane + u != r * pitch + k + first || lane + u + each > bytes) return false;
         } else if (alone || subtracted) {
           return false;
         }
