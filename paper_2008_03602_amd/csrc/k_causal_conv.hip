@@ -155,8 +155,7 @@ static int conv_launch(ConvArgs a, hipStream_t st) {
   const int64_t blocks = (n.total + 3) / 4 * a.dblocks.d;
   a.tiles = (int)n.total;
   if (n.total > 0x7FFFFFF0 || !fits_launch(blocks, 256)) return refuse_size("ct_causal_conv_run");
-  hipLaunchKernelGGL((causal_conv_kernel<T, W, VEC, U>), dim3((unsigned)blocks), dim3(256), 0, st, a);
-  return hipGetLastError() == hipSuccess ? 0 : -1;
+  return launch(causal_conv_kernel<T, W, VEC, U>, dim3((unsigned)blocks), 256, 0, st, a);
 }
 template <typename T, int W>
 static int conv_pick(const ConvArgs& a, bool wide, hipStream_t st) {

@@ -491,10 +491,8 @@ static int launch_tile(LinearArgs a, hipStream_t st) {
     return refuse_size("ct_linear_run");
   a.dgroup = make_fastdiv(4 * (int64_t)a.tiles_m);
   a.dlast = make_fastdiv(a.tiles_n % 4 ? a.tiles_n % 4 : 4);
-  hipLaunchKernelGGL((linear_tile_kernel<T, t.bm, t.bn, t.wm, t.wn, t.wk, S, COPY>),
-                     dim3((unsigned)tiles, (unsigned)a.split), dim3(64 * t.wm * t.wn * t.wk),
-                     S * t.wk * (t.bm + t.bn) * 128, st, a);
-  return hipGetLastError() == hipSuccess ? 0 : -1;
+  return launch(linear_tile_kernel<T, t.bm, t.bn, t.wm, t.wn, t.wk, S, COPY>, dim3((unsigned)tiles, (unsigned)a.split),
+                64 * t.wm * t.wn * t.wk, S * t.wk * (t.bm + t.bn) * 128, st, a);
 }
 template <typename T, int COPY>
 static int linear_pick(const LinearArgs& a, int kind, hipStream_t st) {
@@ -547,8 +545,7 @@ int launch_linear(const ct_linear_op& op, const LinearPlan& p, const void* x, co
                        : linear_pick_odd(a, p.kind, st);
   if (rc || p.split == 1) return rc;
   const int64_t quads = (int64_t)op.m * ((op.n + 3) / 4);
-  hipLaunchKernelGGL(linear_join_kernel, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, st, a);
-  return hipGetLastError() == hipSuccess ? 0 : -1;
+  return launch(linear_join_kernel, dim3((unsigned)((quads + 255) / 256)), 256, 0, st, a);
 }
 
 }  // namespace ct

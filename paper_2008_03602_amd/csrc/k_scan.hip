@@ -522,8 +522,7 @@ static int scan_launch(ScanArgs a, int64_t pieces, hipStream_t st) {
   if (!fits_launch(blocks, 256)) return refuse_size("ct_scan_run");
   a.dgroup = make_fastdiv(per);
   a.dtiles = make_fastdiv(tiles);
-  hipLaunchKernelGGL((scan_kernel<T, NS, P, MODE>), dim3((unsigned)blocks), dim3(256), 0, st, a);
-  return hipGetLastError() == hipSuccess ? 0 : -1;
+  return launch(scan_kernel<T, NS, P, MODE>, dim3((unsigned)blocks), 256, 0, st, a);
 }
 template <typename T, int NS, int P>
 static int scan_prompt(ScanArgs a, const ScanPlan& p, hipStream_t st) {
@@ -537,8 +536,7 @@ static int scan_prompt(ScanArgs a, const ScanPlan& p, hipStream_t st) {
   if (!p.fold) {
     const int64_t blocks = (((int64_t)a.channels * a.states + 63) / 64) * a.s.count;
     if (!fits_launch(blocks, 64)) return refuse_size("ct_scan_run");
-    hipLaunchKernelGGL(scan_carry_kernel, dim3((unsigned)blocks), dim3(64), 0, st, a);
-    if (hipGetLastError() != hipSuccess) return -1;
+    if ((rc = launch(scan_carry_kernel, dim3((unsigned)blocks), 64, 0, st, a))) return rc;
   }
   return scan_launch<T, NS, P, SCAN_OUT>(a, p.chunks, st);
 }
@@ -550,8 +548,7 @@ static int step_launch(ScanArgs a, hipStream_t st) {
   if (waves > 0x7FFFFFF0 || !fits_launch((waves + 3) / 4, 256)) return refuse_size("ct_scan_run");
   a.dgroup = make_fastdiv(per);
   a.dtiles = make_fastdiv(tiles);
-  hipLaunchKernelGGL((scan_step_kernel<T, NS, P, SEQ>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, st, a);
-  return hipGetLastError() == hipSuccess ? 0 : -1;
+  return launch(scan_step_kernel<T, NS, P, SEQ>, dim3((unsigned)((waves + 3) / 4)), 256, 0, st, a);
 }
 template <typename T, int NS, int P>
 static int scan_step(const ScanArgs& a, hipStream_t st) {

@@ -22,6 +22,13 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 inline bool fits_launch(int64_t blocks, int threads) {
   return blocks <= 0x7FFFFFFF && blocks * threads <= 0xFFFFFFFFll;
 }
+// 0, or -1 with the reason left in hipGetLastError. An error that another call left there is
+// none of this launch's.
+template <typename A>
+inline int launch(void (*kernel)(A), dim3 blocks, int threads, size_t lds, hipStream_t st, A a) {
+  void* args[] = {&a};
+  return hipLaunchKernel((const void*)kernel, blocks, dim3((unsigned)threads), args, lds, st) == hipSuccess ? 0 : -1;
+}
 inline int refuse_size(const char* who) {
   set_error(std::string(who) + ": too large for one launch");
   return -2;

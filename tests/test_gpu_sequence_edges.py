@@ -156,3 +156,25 @@ def test_scan_chunks_of_several_stages(lens, channels, states, chunk, dtype):
     y64, new, ybound, nbound = scan64(part, off, slots, True, dtype)
     within(out[:, few], new, nbound, "state")
     within(y[:, few], y64, ybound, "y")
+
+
+def test_errors_that_other_calls_left_are_not_the_operators():
+    """An earlier HIP error that nobody took makes no later call fail."""
+    hip = L.lib()  # its own runtime, through which the symbols are found
+    x, w = torch.ones(4, 8, device="cuda"), torch.ones(16, 8, device="cuda")
+    y, conv, out = torch.zeros(4, 16, device="cuda"), torch.zeros(4, 8, device="cuda"), torch.zeros(4, 8, device="cuda")
+    seqs = L.make_sequences(4, 1, 1)
+    one, taps, a = torch.ones(8, device="cuda"), torch.ones(8, 2, device="cuda"), -torch.ones(8, 4, device="cuda")
+    op = L.make_scan(8, 4, 2, L.DT_F32)
+    ws = torch.empty(max(1, L.ct_scan_workspace(op, seqs)), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    st = stream()
+    try:
+        for call in (lambda: L.ct_linear_run(L.make_linear(4, 16, 8, L.DT_F32, L.DT_F32), x, w, None, None, y, None, st),
+                     lambda: L.ct_causal_conv_run(L.make_causal_conv(8, 2, L.DT_F32), seqs, x, taps, None, None, None, conv, st),
+                     lambda: L.ct_scan_run(op, seqs, x, x, one, a, x, x, None, None, None, None, out, ws, st)):
+            assert hip.hipSetDevice(1 << 20) != 0  # refused on the host
+            call()
+    finally:
+        hip.hipGetLastError()
+    assert (y == 8).all() and (conv[1:] == 2).all() and torch.isfinite(out).all() and (out > 0).all()
