@@ -13,14 +13,14 @@
 //           h(end) = exp(a * sum of steps) h(start) + h(end from 0);
 //   out:    the outputs of each chunk from h at its start.
 // That is nearly twice the exponentials, but as many chunks at once as fill the device: the
-// 16384 tokens take 233 us (kernels: sum 95, carry 22, out 129), whole sequences alone 4 ms. The
-// vector ALU is busy 84-88 % of sum and out, with 112 instructions a token in out, 80 of them
-// the states'. b and c through scalar registers instead of LDS lost 5 % (no room to have the
-// next token's on their way), five waves on a SIMD instead of four spill, and the products
-// dt u b as rank-one updates on the matrix cores, 12 vector instructions a token fewer, lost
-// 3-4 %.
-// Of a few chunks, outputs fold the ends before them and carry is left out: sum then leaves
-// the state from state_in in the place of the last chunk's end, which nothing needs.
+// 16384 tokens take 235 us (kernels at their fastest: sum 95, carry 23, out 133), whole sequences
+// alone 4 ms. The vector ALU is busy 89 % of sum and 85 % of out, with 112 instructions a token
+// in out, 80 of them the states'. b and c through scalar registers instead of LDS lost 5 % (no
+// room to have the next token's on their way), five waves on a SIMD instead of four spill, and
+// the products dt u b as rank-one updates on the matrix cores, 12 vector instructions a token
+// fewer, lost 3-4 %.
+// Of a few chunks, outputs fold the ends before them and carry is left out: sum then leaves the
+// state from state_in in the place of the last chunk's end, which nothing needs.
 // Either way state_in is read before any chunk's outputs write state_out, so that both may be
 // one array.
 #include <hip/hip_runtime.h>
@@ -380,7 +380,7 @@ __global__ void __launch_bounds__(64) scan_carry_kernel(ScanArgs a) {
 // One token of each sequence: a wave updates 64 / P channels of SEQ sequences, whose loads are
 // all on their way together; a, the bias and the skip weight are read once for them. Four
 // states a lane make every access to the states one of 1 KB: 256 sequences of 4096 channels
-// of 16 states (67 MB read, 67 MB written) 25.3 us, 5.6 TB/s; one sequence a wave 30 us, 16
+// of 16 states (67 MB read, 67 MB written) 25.4 us, 5.6 TB/s; one sequence a wave 30 us, 16
 // states a lane 45 (of which the stores through the caches are 10).
 template <typename T, int NS, int P, int SEQ>
 __global__ void __launch_bounds__(256) scan_step_kernel(ScanArgs a) {
@@ -475,7 +475,8 @@ ScanPlan plan_scan(const ct_scan_op& op, const ct_sequences& s) {
   };
   // 16 states a lane (8 where a channel has no more) or four, cut or whole: what takes the
   // fewest us by fits to bf16 (1 to 128 sequences of 32 to 2048 tokens and 300 to 4096 channels
-  // of 8 to 64 states; the choice is the fastest or within 5 % of it). A SIMD with n waves gives
+  // of 8 to 64 states; the choice is the fastest or within 5 % of it), which decide for fp32 and
+  // for more states too, where nothing was fitted. A SIMD with n waves gives
   // each a token in token + wave n, its vector ALU one in full, and the longest sequence takes
   // as many; cut, all tokens are walked twice at the full rate, by three kernels. whole / cut of
   // 16 states: 32 x 512 tokens of 4096 channels 287 / 444, in fours 483 / 495; 8 x 128 of 2048:

@@ -4,9 +4,9 @@
       -> project to (low rank step, b, c) -> project the step up -> selective scan, gated by z
       -> project out, plus x
 
-Seven calls on one stream (``ct_linear_run`` four times, ``ct_causal_conv_run``, ``ct_scan_run``,
-and nothing between them): the halves and slices are read in place through row pitches, and the
-residual is added in the last product's epilogue. Histories and states live in slots that the
+Six calls on one stream (``ct_linear_run`` four times, ``ct_causal_conv_run``, ``ct_scan_run``), and
+where offsets may leave rows out a clear of the scan's output before it: the halves and slices are
+read in place through row pitches, and the residual is added in the last product's epilogue. Histories and states live in slots that the
 caller hands out, so prompts of unequal lengths, single tokens of many sequences and rows that
 belong to no sequence go through the same code. Buffers are made once for the most rows that a
 call may bring, workspaces with the plans, and a call allocates nothing: it may be captured into
