@@ -625,6 +625,117 @@ int ct_scan_run(const ct_scan_op *op, const ct_sequences *seqs, const void *u, c
                 const void *z, const float *state_in, float *state_out, void *y, void *ws, int64_t ws_bytes,
                 void *stream);
 
+/* ---- operators of a linear-attention block ----
+ *
+ * What such a block takes to be served next to the calls above: the norm, rows
+ * of 8 and 4 bits with the product that reads them, and linear attention with a
+ * decay for each head. The conventions are those of the sequence block: the
+ * caller's stream, workspaces and slots, no allocation, nothing but kernels
+ * recorded, the same inputs give the same bits.
+ *
+ * Microscaled rows. A row of `cols` values is stored as (cols + 31) / 32 blocks
+ * of 32, a value being its element's times its block's scale:
+ *   CT_MX_E4M3  8 bits an element, 32 bytes a block: sign, 4 bits of exponent
+ *               (bias 7), 3 of fraction; up to 448; 0x7F is NaN
+ *   CT_MX_E2M1  4 bits an element, 16 bytes a block, element 2i in the low half
+ *               of byte i: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign
+ * and a byte s a block for the scale 2^(s - 127), 255 being NaN. Rows of
+ * elements lie ld bytes apart, a multiple of 16, and rows of scales lds bytes
+ * apart, a multiple of 4; their addresses are such multiples too. Elements of the
+ * last block behind the row's last value are 0, as every call that writes rows
+ * leaves them (and readers rely on it); it also writes 0 to the scales behind the
+ * last block up to the next multiple of 4, which are not read as scales.
+ *
+ * A row is quantised block by block: with m the largest magnitude of the block,
+ * s - 127 = floor(log2 m) less 8 (e4m3) or 2 (e2m1), at least -127, and elements
+ * are the values over the scale, rounded to nearest even, at most the largest
+ * element. A block with an infinity or a NaN gets the scale NaN. */
+#define CT_MX_E4M3 2
+#define CT_MX_E2M1 3
+
+typedef struct ct_mx_op {
+    int32_t rows, cols;
+    int32_t dtype;   /* CT_DT_*: the values */
+    int32_t format;  /* CT_MX_*             */
+    int64_t ldx;     /* elements            */
+    int64_t ldq, lds;/* bytes               */
+} ct_mx_op;
+
+/* x (rows x cols in `dtype`) to elements q and scales. */
+int ct_mx_quantise_run(const ct_mx_op *op, const void *x, void *q, void *scales, void *stream);
+/* The values that q and scales stand for, rounded to `dtype`, to x. */
+int ct_mx_values_run(const ct_mx_op *op, const void *q, const void *scales, void *x, void *stream);
+
+/* ct_linear on microscaled rows: y = act(x w^T + bias) with the residual. Where
+ * y is fp32, products are exact and sums are in fp32. Where it is bf16 the matrix
+ * cores take the 8- and 4-bit elements themselves: of each eight products they
+ * add, bits below 2^-13 of the largest are dropped. Rows of x and w are at most
+ * 4 MiB apart. */
+typedef struct ct_mx_linear_op {
+    int32_t m, n, k;
+    int32_t x_format, w_format;  /* CT_MX_*                       */
+    int32_t out_dtype;           /* CT_DT_*: r and y; bias is fp32 */
+    int32_t act, res;            /* CT_ACT_*, CT_RES_*            */
+    int64_t ldx, ldxs, ldw, ldws;/* bytes: x, its scales, w, its scales */
+    int64_t ldr, ldy;            /* elements */
+} ct_mx_linear_op;
+
+int ct_mx_linear_workspace(const ct_mx_linear_op *op, int64_t *bytes);
+/* bias may be NULL; res is read only where op->res asks for it, and may be y
+ * itself (with ldr = ldy). */
+int ct_mx_linear_run(const ct_mx_linear_op *op, const void *x, const void *x_scales, const void *w,
+                     const void *w_scales, const float *bias, const void *res, void *y, void *ws, int64_t ws_bytes,
+                     void *stream);
+
+/* Root-mean-square norm of rows, or of each of `groups` equal parts of a row:
+ *   h = x + res,   y = h / sqrt(mean of h^2 over the part + eps) * w * z / (1 + exp(-z)).
+ * x, res and z (rows x cols) in `dtype`, w (cols) fp32; res, w and z may be NULL.
+ * sum (optional) takes h, rounded to `dtype`; y is of type `out`, a CT_DT_* or
+ * microscaled rows (CT_MX_*, ldy then in bytes; parts are whole blocks of 32
+ * where there are several), and comes from h before it is rounded. h^2 is summed
+ * in fp32, and a part whose sum is past its range counts as infinite. An output
+ * may be an input itself where type and pitch are the same. */
+typedef struct ct_norm_op {
+    int32_t rows, cols, groups;
+    int32_t dtype;  /* CT_DT_*             */
+    int32_t out;    /* CT_DT_* or CT_MX_*  */
+    float eps;      /* 0 or more           */
+    int64_t ldx, ldres, ldsum, ldz;
+    int64_t ldy;    /* elements, or bytes of microscaled rows */
+    int64_t lds;    /* bytes: scales       */
+} ct_norm_op;
+
+int ct_norm_run(const ct_norm_op *op, const void *x, const void *res, void *sum, const float *w, const void *z,
+                void *y, void *scales, void *stream);
+
+/* Linear attention with a decay for each head, along each sequence. For head h
+ * with its state S (key_dim x value_dim) and group g = h / (heads / groups):
+ *   dt_t = delta[t,h] + dt_bias[h], through softplus if asked for; 1 without delta;
+ *   S_t = exp(min(dt_t a[h], 0)) S_{t-1} + k[t,g]^T v[t,h]   (times dt_t with step_input);
+ *   o[t,h] = scale * q[t,g] S_t.
+ * q and k (tokens x groups x key_dim), v and o (tokens x heads x value_dim) in
+ * `dtype`, delta (tokens x heads) in `delta_dtype`; dt_bias, a (heads) and the
+ * states (slots x heads x key_dim x value_dim) fp32. delta, dt_bias, state_in
+ * (zeros) and state_out may be NULL; state_out may be state_in itself. key_dim
+ * and value_dim 1..256; groups divides heads. Rows of q, k, v and o are at most
+ * 4 MiB apart. What no infinity or NaN reaches by the formula is as if there were
+ * none; what one reaches is not finite, but may be the other of the two. */
+typedef struct ct_decay_attention_op {
+    int32_t heads, groups, key_dim, value_dim;
+    int32_t dtype, delta_dtype;  /* CT_DT_* */
+    int32_t softplus;            /* 0 or 1  */
+    int32_t step_input;          /* 0 or 1  */
+    float scale;
+    int32_t reserved;            /* 0       */
+    int64_t ldq, ldk, ldv, lddelta, ldo;
+} ct_decay_attention_op;
+
+int ct_decay_attention_workspace(const ct_decay_attention_op *op, const ct_sequences *seqs, int64_t *bytes);
+int ct_decay_attention_run(const ct_decay_attention_op *op, const ct_sequences *seqs, const void *q, const void *k,
+                           const void *v, const void *delta, const float *dt_bias, const float *a,
+                           const float *state_in, float *state_out, void *o, void *ws, int64_t ws_bytes,
+                           void *stream);
+
 #ifdef __cplusplus
 }
 #endif

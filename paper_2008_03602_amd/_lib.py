@@ -23,6 +23,7 @@ CT_E_TIMEOUT, CT_E_CLIENT, CT_E_STOPPED = -6, -7, -8
 S_OK, S_INVALID, S_LAUNCH, S_TIMEOUT, S_WRONG_ANSWER = 0, 1, 2, 3, 4
 STATUS_NAMES = {0: "ok", 1: "invalid", 2: "launch_error", 3: "timeout", 4: "wrong_answer"}
 DT_F32, DT_BF16 = 0, 1
+MX_E4M3, MX_E2M1 = 2, 3
 ACT_NONE, ACT_RELU, ACT_RELU6, ACT_SILU, ACT_GELU = 0, 1, 2, 3, 4
 RES_NONE, RES_ADD, RES_ADD_ACT = 0, 1, 2
 MASK_WORDS = 8
@@ -106,6 +107,26 @@ class ct_scan_op(ctypes.Structure):
                [(n, c_i64) for n in ("ldu", "lddelta", "ldb", "ldc", "ldz", "ldy")]
 
 
+class ct_mx_op(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("rows", "cols", "dtype", "format")] + [(n, c_i64) for n in ("ldx", "ldq", "lds")]
+
+
+class ct_mx_linear_op(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("m", "n", "k", "x_format", "w_format", "out_dtype", "act", "res")] + \
+               [(n, c_i64) for n in ("ldx", "ldxs", "ldw", "ldws", "ldr", "ldy")]
+
+
+class ct_norm_op(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("rows", "cols", "groups", "dtype", "out")] + [("eps", c_f32)] + \
+               [(n, c_i64) for n in ("ldx", "ldres", "ldsum", "ldz", "ldy", "lds")]
+
+
+class ct_decay_attention_op(ctypes.Structure):
+    _fields_ = [(n, c_i32) for n in ("heads", "groups", "key_dim", "value_dim", "dtype", "delta_dtype", "softplus",
+                                     "step_input")] + [("scale", c_f32), ("reserved", c_i32)] + \
+               [(n, c_i64) for n in ("ldq", "ldk", "ldv", "lddelta", "ldo")]
+
+
 _VP = ctypes.c_void_p
 _SIGS = {
     "ct_init": (c_i32, [c_i32]),
@@ -163,6 +184,13 @@ _SIGS = {
     "ct_causal_conv_run": (c_i32, [P(ct_causal_conv_op), P(ct_sequences)] + [_VP] * 7),
     "ct_scan_workspace": (c_i32, [P(ct_scan_op), P(ct_sequences), P(c_i64)]),
     "ct_scan_run": (c_i32, [P(ct_scan_op), P(ct_sequences)] + [_VP] * 12 + [c_i64, _VP]),
+    "ct_mx_quantise_run": (c_i32, [P(ct_mx_op)] + [_VP] * 4),
+    "ct_mx_values_run": (c_i32, [P(ct_mx_op)] + [_VP] * 4),
+    "ct_mx_linear_workspace": (c_i32, [P(ct_mx_linear_op), P(c_i64)]),
+    "ct_mx_linear_run": (c_i32, [P(ct_mx_linear_op)] + [_VP] * 8 + [c_i64, _VP]),
+    "ct_norm_run": (c_i32, [P(ct_norm_op)] + [_VP] * 8),
+    "ct_decay_attention_workspace": (c_i32, [P(ct_decay_attention_op), P(ct_sequences), P(c_i64)]),
+    "ct_decay_attention_run": (c_i32, [P(ct_decay_attention_op), P(ct_sequences)] + [_VP] * 10 + [c_i64, _VP]),
 }
 
 _lock = threading.Lock()
@@ -659,6 +687,107 @@ def ct_scan_run(op: ct_scan_op, seqs: ct_sequences, u, delta, dt_bias, a, b, c, 
     except AttributeError:
         rc = f(op, seqs, *map(_ptr, (u, delta, dt_bias, a, b, c, d_skip, z, state_in, state_out, y)), ws, nbytes,
                stream or None)
+    if rc:
+        _check(rc)
+
+
+# ---------------------------------------------------------------- operators of a linear-attention block
+def _addresses(*tensors):
+    """Device addresses of tensors, or of addresses among them."""
+    try:  # tensors, without a call for each: a decode step is as long as its calls
+        return [None if t is None else t.data_ptr() for t in tensors]
+    except AttributeError:
+        return [_ptr(t) for t in tensors]
+
+
+def mx_row_bytes(cols: int, format: int) -> int:
+    """Bytes of a microscaled row's elements: whole blocks of 32."""
+    return (cols + 31) // 32 * (32 if format == MX_E4M3 else 16)
+
+
+def mx_scale_bytes(cols: int) -> int:
+    """Bytes of a microscaled row's scales: one a block, whole groups of four."""
+    return (cols + 127) // 128 * 4
+
+
+def make_mx(rows, cols, dtype, format, ldx=0, ldq=0, lds=0) -> ct_mx_op:
+    """Rows of `cols` values in `dtype` and their microscaled form; a pitch of 0 is that of a contiguous array."""
+    return ct_mx_op(int(rows), int(cols), int(dtype), int(format), int(ldx) or cols,
+                    int(ldq) or mx_row_bytes(cols, format), int(lds) or mx_scale_bytes(cols))
+
+
+def make_mx_linear(m, n, k, x_format, w_format, out_dtype, act=ACT_NONE, res=RES_NONE, ldx=0, ldxs=0, ldw=0, ldws=0,
+                   ldr=0, ldy=0) -> ct_mx_linear_op:
+    """y[m, n] = act(x w^T + bias) with a residual, of microscaled x and w (pitches in bytes)."""
+    return ct_mx_linear_op(int(m), int(n), int(k), int(x_format), int(w_format), int(out_dtype), int(act), int(res),
+                           int(ldx) or mx_row_bytes(k, x_format), int(ldxs) or mx_scale_bytes(k),
+                           int(ldw) or mx_row_bytes(k, w_format), int(ldws) or mx_scale_bytes(k), int(ldr) or n,
+                           int(ldy) or n)
+
+
+def make_norm(rows, cols, dtype, out, groups=1, eps=1e-5, ldx=0, ldres=0, ldsum=0, ldz=0, ldy=0, lds=0) -> ct_norm_op:
+    """The norm of rows, or of `groups` parts of each; `out` is a DT_* or an MX_* (ldy then in bytes)."""
+    y = mx_row_bytes(cols, out) if out in (MX_E4M3, MX_E2M1) else cols
+    return ct_norm_op(int(rows), int(cols), int(groups), int(dtype), int(out), float(eps), int(ldx) or cols,
+                      int(ldres) or cols, int(ldsum) or cols, int(ldz) or cols, int(ldy) or y,
+                      int(lds) or mx_scale_bytes(cols))
+
+
+def make_decay_attention(heads, groups, key_dim, value_dim, dtype, delta_dtype=None, softplus=True, step_input=False,
+                         scale=1.0, ldq=0, ldk=0, ldv=0, lddelta=0, ldo=0) -> ct_decay_attention_op:
+    gk, hv = groups * key_dim, heads * value_dim
+    return ct_decay_attention_op(int(heads), int(groups), int(key_dim), int(value_dim), int(dtype),
+                                 int(dtype if delta_dtype is None else delta_dtype), int(softplus), int(step_input),
+                                 float(scale), 0, int(ldq) or gk, int(ldk) or gk, int(ldv) or hv, int(lddelta) or heads,
+                                 int(ldo) or hv)
+
+
+def ct_mx_quantise_run(op: ct_mx_op, x, q, scales, stream: int = 0) -> None:
+    rc = (_lib or lib()).ct_mx_quantise_run(op, *_addresses(x, q, scales), stream or None)
+    if rc:
+        _check(rc)
+
+
+def ct_mx_values_run(op: ct_mx_op, q, scales, x, stream: int = 0) -> None:
+    rc = (_lib or lib()).ct_mx_values_run(op, *_addresses(q, scales, x), stream or None)
+    if rc:
+        _check(rc)
+
+
+def ct_mx_linear_workspace(op: ct_mx_linear_op) -> int:
+    """Bytes of scratch memory that ct_mx_linear_run needs for op."""
+    n = c_i64()
+    _check(lib().ct_mx_linear_workspace(ctypes.byref(op), ctypes.byref(n)))
+    return n.value
+
+
+def ct_mx_linear_run(op: ct_mx_linear_op, x, x_scales, w, w_scales, bias, res, y, ws=None, stream: int = 0,
+                     ws_bytes: int = 0) -> None:
+    ws, nbytes = _ws(ws, ws_bytes)
+    rc = (_lib or lib()).ct_mx_linear_run(op, *_addresses(x, x_scales, w, w_scales, bias, res, y), ws, nbytes,
+                                          stream or None)
+    if rc:
+        _check(rc)
+
+
+def ct_norm_run(op: ct_norm_op, x, res, sum, w, z, y, scales=None, stream: int = 0) -> None:
+    rc = (_lib or lib()).ct_norm_run(op, *_addresses(x, res, sum, w, z, y, scales), stream or None)
+    if rc:
+        _check(rc)
+
+
+def ct_decay_attention_workspace(op: ct_decay_attention_op, seqs: ct_sequences) -> int:
+    """Bytes of scratch memory that ct_decay_attention_run needs for op and seqs."""
+    n = c_i64()
+    _check(lib().ct_decay_attention_workspace(ctypes.byref(op), ctypes.byref(seqs), ctypes.byref(n)))
+    return n.value
+
+
+def ct_decay_attention_run(op: ct_decay_attention_op, seqs: ct_sequences, q, k, v, delta, dt_bias, a, state_in,
+                           state_out, o, ws=None, stream: int = 0, ws_bytes: int = 0) -> None:
+    ws, nbytes = _ws(ws, ws_bytes)
+    rc = (_lib or lib()).ct_decay_attention_run(op, seqs, *_addresses(q, k, v, delta, dt_bias, a, state_in, state_out,
+                                                                      o), ws, nbytes, stream or None)
     if rc:
         _check(rc)
 

@@ -27,24 +27,17 @@
 #include <type_traits>
 #include <utility>
 
-#include "k_seq.h"
+#include "k_linear.h"
 
 namespace ct {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-struct LinearArgs {
-  const void *x, *w, *res;
-  const float* bias;
-  void* y;
-  float* ws;
-  int m, n, k;
-  int64_t ldx, ldw, ldr, ldy;
-  int act, res_mode, out_bf16;
-  int stream;           // y goes past the caches
-  int tiles_m, tiles_n;
-  int split, per_split; // slices of the reduction, elements in each (whole 128-byte chunks)
-  FastDiv dgroup, dlast;
+struct LinearArgs : OutArgs {
+  const void *x, *w;
+  int k;
+  int per_split;  // elements in a slice of the reduction (whole 128-byte chunks)
+  int64_t ldx, ldw;
 };
 
 // acc += A B for one 16-byte group per lane: row lane % 16 of each operand, group lane / 16
@@ -66,73 +59,8 @@ __device__ __forceinline__ f32x4 mma16(u32x4 a, u32x4 b, f32x4 acc) {
   }
 }
 
-// ------------------------------------------------------------------ epilogue
-// Four columns of the bias, and of a row of the residual, from column j on: 0 where there
-// are none.
-__device__ __forceinline__ Quad load_bias(const LinearArgs& a, int j) {
-  Quad q = {};
-  if (!a.bias || j >= a.n) return q;
-  if (j + 4 <= a.n) return load_quad4(a.bias + j);
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (j + e < a.n) q.v[e] = a.bias[j + e];
-  return q;
-}
-__device__ __forceinline__ Quad load_res(const LinearArgs& a, int i, int j) {
-  Quad q = {};
-  if (!a.res_mode || i >= a.m || j >= a.n) return q;
-  const int64_t at = i * a.ldr + j;
-  if (j + 4 <= a.n)
-    return a.out_bf16 ? load_quad4((const bf16_t*)a.res + at) : load_quad4((const float*)a.res + at);
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (j + e < a.n) q.v[e] = a.out_bf16 ? (float)((const bf16_t*)a.res)[at + e] : ((const float*)a.res)[at + e];
-  return q;
-}
-// N quads of outputs from their sums, one choice of the activation for all of them.
-template <int N>
-__device__ __forceinline__ void finish(const LinearArgs& a, float (&v)[N][4], const Quad& bias, const Quad (&res)[N]) {
-  auto each = [&](auto f) __attribute__((always_inline)) {
-#pragma unroll
-    for (int q = 0; q < N; ++q)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[q][e] = f(v[q][e], q, e);
-  };
-  each([&](float x, int, int e) { return x + bias.v[e]; });
-  if (a.res_mode == CT_RES_ADD_ACT) each([&](float x, int q, int e) { return x + res[q].v[e]; });
-  switch (a.act) {
-    case CT_ACT_RELU: each([](float x, int, int) { return activate(x, CT_ACT_RELU); }); break;
-    case CT_ACT_RELU6: each([](float x, int, int) { return activate(x, CT_ACT_RELU6); }); break;
-    case CT_ACT_SILU: each([](float x, int, int) { return activate(x, CT_ACT_SILU); }); break;
-    case CT_ACT_GELU: each([](float x, int, int) { return activate(x, CT_ACT_GELU); }); break;
-  }
-  if (a.res_mode == CT_RES_ADD) each([&](float x, int q, int e) { return x + res[q].v[e]; });
-}
-// Outputs (i, j .. j+3), those of them that exist.
-__device__ __forceinline__ void store4(const LinearArgs& a, int i, int j, f32x4 acc, const Quad& bias, const Quad& r) {
-  float v[1][4] = {{acc.x, acc.y, acc.z, acc.w}};
-  const Quad res[1] = {r};
-  finish(a, v, bias, res);
-  const int64_t at = i * a.ldy + j;
-  if (j + 4 <= a.n) {
-    if (a.out_bf16) store_quad4((bf16_t*)a.y + at, v[0], false);
-    else store_quad4((float*)a.y + at, v[0], false);
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (j + e >= a.n) break;
-    if (a.out_bf16) ((bf16_t*)a.y)[at + e] = (bf16_t)v[0][e];
-    else ((float*)a.y)[at + e] = v[0][e];
-  }
-}
-// Partial sums of slice sp: rows of n rounded up to four.
-__device__ __forceinline__ void store_part(const LinearArgs& a, int sp, int i, int j, f32x4 acc) {
-  const int64_t n4 = (a.n + 3) / 4 * 4;
-  *(f32x4*)(a.ws + ((int64_t)sp * a.m + i) * n4 + j) = acc;
-}
 // Adds the slices in their order and finishes the outputs.
-__global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs a) {
+__global__ void __launch_bounds__(256) linear_join_kernel(OutArgs a) {
   const int n4 = (a.n + 3) / 4;
   const int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (q >= (int64_t)a.m * n4) return;
@@ -148,6 +76,11 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs a) {
       if (s + e < a.split) v += part[e];
   }
   store4(a, i, j, v, bias, res);
+}
+
+int launch_join(const OutArgs& a, hipStream_t st) {
+  const int64_t quads = (int64_t)a.m * ((a.n + 3) / 4);
+  return launch(linear_join_kernel, dim3((unsigned)((quads + 255) / 256)), 256, 0, st, a);
 }
 
 // ------------------------------------------------------------------ 16-byte groups of rows
@@ -187,13 +120,6 @@ __device__ __forceinline__ RowsView rows_view(const void* p, int64_t ld, int r0,
   return {(const void*)(at - odd), (unsigned)bytes, odd};
 }
 
-// One wave instruction: lane i copies BYTES bytes at byte offset off + k of r to lds + BYTES i.
-template <int BYTES>
-__device__ __forceinline__ void copy_lds(__amdgpu_buffer_rsrc_t r, char* lds, unsigned off, int k) {
-  if constexpr (BYTES == 4) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)lds, 4, (int)off, k, 0, 0);
-  else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)lds, 16, (int)off, k, 0, 0);
-}
-
 // ------------------------------------------------------------------ tiles
 // A block computes BM x BN outputs with WK teams of WM x WN waves, each team every WK-th
 // slice of 128 bytes of each operand row: where the tile is small, a slice's products take
@@ -212,19 +138,8 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearAr
   static_assert(BN % (RPC * WAVES) == 0 && BM % (RPC * WAVES) == 0, "every wave copies as many rows");
   extern __shared__ __align__(16) char lds[];
 
-  // Each XCD takes one band of tiles, in columns four tiles wide: the tiles at work on it
-  // share a few panels of x and four of w in its L2.
-  const int idx = xcd_band_tile((int)blockIdx.x, a.tiles_m * a.tiles_n);
-  const int grp = fdiv(idx, a.dgroup), in = idx - grp * a.dgroup.d;
-  int mi, ni;
-  if (grp * 4 + 4 <= a.tiles_n) {
-    mi = in >> 2;
-    ni = grp * 4 + (in & 3);
-  } else {
-    mi = fdiv(in, a.dlast);
-    ni = grp * 4 + in - mi * a.dlast.d;
-  }
-  const int m0 = mi * BM, n0 = ni * BN, sp = (int)blockIdx.y;
+  const TileAt at = tile_of_block(a, (int)blockIdx.x);
+  const int m0 = at.mi * BM, n0 = at.ni * BN, sp = (int)blockIdx.y;
   const int lane = (int)threadIdx.x & 63, team = wave_id() / WAVES, wave = wave_id() % WAVES;
   const int k_begin = sp * a.per_split, k_end = min(a.k, k_begin + a.per_split);
   const int chunks = (k_end - k_begin + WK * KC - 1) / (WK * KC);  // slices of a team
@@ -337,87 +252,7 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) linear_tile_kernel(LinearAr
     }
   }
 
-  // The sums go through the wave's share of LDS, as many rows of its tile at a time as it
-  // holds, so that each access to y and r takes whole rows of the tile.
-  constexpr int RM = BM / WM, RN = BN / WN, SLOTS = RN / 4;  // 16-byte slots of a row
-  constexpr int FIT = STAGES * STAGE / WK / WAVES / (RN * 4) / 16 * 16, H = FIT < RM ? FIT : RM;
-  constexpr int STEP = 64 / SLOTS;  // rows of one access
-  static_assert(RM % H == 0, "");
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // slices past the end, too
-  __syncthreads();
-  if constexpr (WK > 1) {  // the teams' sums, added in their order by the first
-    constexpr int SUMS = BM * BN * 4;
-    static_assert(WK * SUMS <= STAGES * STAGE && H == RM, "");
-    if (team > 0) {
-#pragma unroll
-      for (int i = 0; i < TN; ++i)
-#pragma unroll
-        for (int j = 0; j < TM; ++j)
-          *(f32x4*)(lds + team * SUMS + ((wave * TN + i) * TM + j) * 1024 + lane * 16) = acc[i][j];
-    }
-    __syncthreads();
-    if (team > 0) return;
-#pragma unroll
-    for (int t = 1; t < WK; ++t)
-#pragma unroll
-      for (int i = 0; i < TN; ++i)
-#pragma unroll
-        for (int j = 0; j < TM; ++j)
-          acc[i][j] += *(const f32x4*)(lds + t * SUMS + ((wave * TN + i) * TM + j) * 1024 + lane * 16);
-  }
-  char* mine = lds + wave * (H * RN * 4);
-  auto slot = [](int r, int s) { return (s ^ ((SLOTS >= 16 ? r : r >> 1) & (SLOTS - 1))) * 16; };
-  const int sl = lane % SLOTS, col = n0 + wn + sl * 4, r0 = lane / SLOTS;
-  const bool whole = m0 + BM <= a.m && n0 + BN <= a.n;  // no output of the tile is missing
-  const Quad bias = a.split > 1 ? Quad{} : load_bias(a, col);
-  constexpr int ROWS_EACH = H / STEP, Q = ROWS_EACH % 4 ? ROWS_EACH : 4;  // rows of a lane, and at a time
-  auto take = [&](int r) { return *(const f32x4*)(mine + r * RN * 4 + slot(r, sl)); };
-  auto finish_rows = [&](int h, auto zero) __attribute__((always_inline)) {
-    using O = decltype(zero);
-    const int64_t row = m0 + wm + h + r0;
-    O* y = (O*)a.y + row * a.ldy + col;
-    const O* rp = (const O*)a.res + row * a.ldr + col;
-#pragma unroll 1
-    for (int r = r0; r < H; r += Q * STEP) {
-      Quad res[Q] = {};
-      if (a.res_mode) {
-#pragma unroll
-        for (int q = 0; q < Q; ++q) res[q] = load_quad4(rp + q * STEP * a.ldr);
-        rp += Q * STEP * a.ldr;
-      }
-      float v[Q][4];
-#pragma unroll
-      for (int q = 0; q < Q; ++q) {
-        const f32x4 s = take(r + q * STEP);
-        v[q][0] = s.x; v[q][1] = s.y; v[q][2] = s.z; v[q][3] = s.w;
-      }
-      finish(a, v, bias, res);
-#pragma unroll
-      for (int q = 0; q < Q; ++q) store_quad4(y + q * STEP * a.ldy, v[q], a.stream);
-      y += Q * STEP * a.ldy;
-    }
-  };
-#pragma unroll
-  for (int h = 0; h < RM; h += H) {
-#pragma unroll
-    for (int j = 0; j < H / 16; ++j)
-#pragma unroll
-      for (int i = 0; i < TN; ++i)
-        *(f32x4*)(mine + (j * 16 + lrow) * RN * 4 + slot(j * 16 + lrow, i * 4 + kg)) = acc[i][h / 16 + j];
-    if (a.split > 1) {
-      for (int r = r0; r < H; r += STEP)
-        if (m0 + wm + h + r < a.m && col < a.n) store_part(a, sp, m0 + wm + h + r, col, take(r));
-    } else if (whole) {
-      if (a.out_bf16) finish_rows(h, bf16_t());
-      else finish_rows(h, 0.f);
-    } else {
-#pragma unroll 1
-      for (int r = r0; r < H; r += STEP) {
-        const int row = m0 + wm + h + r;
-        if (row < a.m && col < a.n) store4(a, row, col, take(r), bias, load_res(a, row, col));
-      }
-    }
-  }
+  write_tile<BM, BN, WM, WN, WK, STAGES * STAGE>(a, lds, acc, m0, n0, sp);
 }
 
 // ------------------------------------------------------------------ plans and launches
@@ -484,14 +319,9 @@ template <typename T, int COPY, int KIND>
 static int launch_tile(LinearArgs a, hipStream_t st) {
   constexpr TileShape t = kTiles[KIND];
   constexpr int S = COPY ? t.stages : 2;
-  a.tiles_m = (a.m + t.bm - 1) / t.bm;
-  a.tiles_n = (a.n + t.bn - 1) / t.bn;
-  const int64_t tiles = (int64_t)a.tiles_m * a.tiles_n;
-  if (!fits_launch(tiles, 64 * t.wm * t.wn * t.wk) || 4 * (int64_t)a.tiles_m > 0x7FFFFFFF)
-    return refuse_size("ct_linear_run");
-  a.dgroup = make_fastdiv(4 * (int64_t)a.tiles_m);
-  a.dlast = make_fastdiv(a.tiles_n % 4 ? a.tiles_n % 4 : 4);
-  return launch(linear_tile_kernel<T, t.bm, t.bn, t.wm, t.wn, t.wk, S, COPY>, dim3((unsigned)tiles, (unsigned)a.split),
+  if (!set_tiles(a, t.bm, t.bn, 64 * t.wm * t.wn * t.wk)) return refuse_size("ct_linear_run");
+  return launch(linear_tile_kernel<T, t.bm, t.bn, t.wm, t.wn, t.wk, S, COPY>,
+                dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)a.split),
                 64 * t.wm * t.wn * t.wk, S * t.wk * (t.bm + t.bn) * 128, st, a);
 }
 template <typename T, int COPY>
@@ -544,8 +374,7 @@ int launch_linear(const ct_linear_op& op, const LinearPlan& p, const void* x, co
          : on % 4 == 0 ? linear_pick<bf16_t, 4>(a, p.kind, st)
                        : linear_pick_odd(a, p.kind, st);
   if (rc || p.split == 1) return rc;
-  const int64_t quads = (int64_t)op.m * ((op.n + 3) / 4);
-  return launch(linear_join_kernel, dim3((unsigned)((quads + 255) / 256)), 256, 0, st, a);
+  return launch_join(a, st);
 }
 
 }  // namespace ct

@@ -1,0 +1,332 @@
+// Product of microscaled rows with its epilogue: y = act(x w^T + bias) + r, or act(x w^T + bias + r),
+// x and w of e4m3 or e2m1 elements in blocks of 32 with a power of two as their scale.
+//
+// The matrix instruction takes 128 elements of a row, a lane's 32 of them and the scale of one
+// block: of e2m1 lane group g holds elements 32 g to 32 g + 31, of e4m3 16 g to 16 g + 15 and the
+// same 64 further on, and either way its scale is the one of block g. Fragments and scales are
+// read from LDS as they lie in memory. The weights are the first operand: a lane's four
+// consecutive accumulators are then four consecutive outputs of one row of y.
+//
+// Sums. Of each eight consecutive products the instruction drops what lies below 2^-13 of the
+// largest (measured: 2^-13 of it survives beside it and 2^-14 does not, across eights all 23 bits
+// do), 1.5e-5 of the result for two operands of normal values in e4m3, which an output of bf16
+// (2^-9) does not show. For fp32 outputs the elements are turned into bf16, which holds each with
+// its scale exactly, and multiplied by the 16-bit instruction: products exact, sums in fp32.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+#include <utility>
+
+#include "k_linear.h"
+#include "k_mx.h"
+
+namespace ct {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+struct MxLinearArgs : OutArgs {
+  const char *x, *w;
+  const unsigned char *xs, *wsc;
+  int blocks;     // of a row
+  int per_split;  // steps of 128 elements in a slice of the reduction
+  int64_t ldx, ldxs, ldw, ldws;
+};
+
+constexpr int mx_step_bytes(int format) { return format == CT_MX_E4M3 ? 128 : 64; }  // of 128 elements
+
+// A lane's 32 elements of a row.
+template <int FORMAT>
+struct MxFrag {
+  u32x4 lo, hi;  // e2m1: hi is not used
+};
+// Four words of eight bf16 each from 32 elements with their scale.
+template <int FORMAT>
+__device__ __forceinline__ bf16x8 mx_bf16(const MxFrag<FORMAT>& f, int c, unsigned scale) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const float s = __builtin_bit_cast(float, scale << 23);  // the conversion takes the exponent's bits as they are
+  bf16x2 p[4];
+  if constexpr (FORMAT == CT_MX_E4M3) {
+    const u32x4 q = c < 2 ? f.lo : f.hi;
+    const unsigned w0 = q[c % 2 * 2], w1 = q[c % 2 * 2 + 1];
+    p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s, false);
+    p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s, true);
+    p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, false);
+    p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, true);
+  } else {
+    const unsigned w = f.lo[c];
+    p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0);
+    p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1);
+    p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2);
+    p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3);
+  }
+  bf16x8 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r[2 * i] = p[i].x;
+    r[2 * i + 1] = p[i].y;
+  }
+  return r;
+}
+template <int FORMAT>
+__device__ __forceinline__ i32x8 mx_operand(const MxFrag<FORMAT>& f) {
+  if constexpr (FORMAT == CT_MX_E4M3)
+    return __builtin_bit_cast(i32x8, __builtin_shufflevector(f.lo, f.hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  else
+    return __builtin_bit_cast(i32x8, __builtin_shufflevector(f.lo, f.lo, 0, 1, 2, 3, -1, -1, -1, -1));
+}
+constexpr int mx_code(int format) { return format == CT_MX_E4M3 ? 0 : 4; }  // of the instruction
+
+// The rows of an operand, or of its scales, from row r0 on (at most `most` of `rows`).
+struct MxRows {
+  const void* base;
+  unsigned bytes;
+};
+__device__ __forceinline__ MxRows mx_rows(const void* p, int64_t ld, int r0, int rows, int most, int row_bytes) {
+  const int have = min(rows - r0, most);
+  return {(const char*)p + r0 * ld, have > 0 && row_bytes > 0 ? (unsigned)((have - 1) * ld + row_bytes) : 0};
+}
+
+// A block computes BM x BN outputs with WK teams of WM x WN waves, each team every WK-th step of
+// 128 elements. Steps go through STAGES buffers in LDS, copied straight into it, the later ones in
+// flight while one is multiplied; the 16-byte groups of a row are permuted by its number, so that
+// the 16 rows of a fragment lie in distinct banks. Every address is in bounds: rows are a buffer
+// that ends with the last of the tile's, and rows, groups and scales past the end have an offset
+// past it, and read 0.
+template <int FW, int FX, bool EXACT, int BM, int BN, int WM, int WN, int WK, int STAGES>
+__global__ void __launch_bounds__(64 * WM * WN * WK) mx_linear_kernel(MxLinearArgs a) {
+  constexpr int WAVES = WM * WN, RBW = mx_step_bytes(FW), RBX = mx_step_bytes(FX);
+  constexpr int RPCW = 1024 / RBW, RPCX = 1024 / RBX;  // rows of one copy
+  constexpr int NCW = BN / RPCW / WAVES, NCX = BM / RPCX / WAVES;  // copies of a wave
+  constexpr int SW = BN / WAVES, SX = BM / WAVES;  // rows whose scales a wave copies
+  constexpr int TM = BM / WM / 16, TN = BN / WN / 16;
+  constexpr int AT_X = BN * RBW, AT_SW = AT_X + BM * RBX, AT_SX = AT_SW + BN * 4, TEAM = AT_SX + BM * 4;
+  constexpr int STAGE = WK * TEAM;
+  static_assert(BN % (RPCW * WAVES) == 0 && BM % (RPCX * WAVES) == 0 && SW <= 64 && SX <= 64, "every wave copies as many rows");
+  static_assert((RPCW * WAVES >> 1) % (RBW / 16) == 0 && (RPCX * WAVES >> 1) % (RBX / 16) == 0, "one permutation for every copy");
+  extern __shared__ __align__(16) char lds[];
+
+  const TileAt tile = tile_of_block(a, (int)blockIdx.x);
+  const int m0 = tile.mi * BM, n0 = tile.ni * BN, sp = (int)blockIdx.y;
+  const int lane = (int)threadIdx.x & 63, team = wave_id() / WAVES, wave = wave_id() % WAVES;
+  const int steps = (a.blocks + 3) / 4, begin = sp * a.per_split, end = min(steps, begin + a.per_split);
+  const int rounds = (end - begin + WK - 1) / WK;  // steps of a team
+
+  const int row_w = a.blocks * (RBW / 4), row_x = a.blocks * (RBX / 4), row_s = steps * 4;  // bytes
+  const MxRows vw = mx_rows(a.w, a.ldw, n0, a.n, BN, row_w), vx = mx_rows(a.x, a.ldx, m0, a.m, BM, row_x);
+  const MxRows vsw = mx_rows(a.wsc, a.ldws, n0, a.n, BN, row_s), vsx = mx_rows(a.xs, a.ldxs, m0, a.m, BM, row_s);
+  const __amdgpu_buffer_rsrc_t rw = make_rsrc(vw.base, vw.bytes), rx = make_rsrc(vx.base, vx.bytes);
+  const __amdgpu_buffer_rsrc_t rsw = make_rsrc(vsw.base, vsw.bytes), rsx = make_rsrc(vsx.base, vsx.bytes);
+
+  // Byte of a row that a lane copies in each step: whole rows to a copy, lane by lane in LDS, so
+  // that the permutation of a row's groups is one of the addresses that its lanes read.
+  const auto first = [&](int rb) {
+    const int lpr = rb / 16, row = wave * (64 / lpr) + lane / lpr;
+    return ((lane % lpr) ^ ((row >> 1) & (lpr - 1))) * 16;
+  };
+  const int first_w = first(RBW), first_x = first(RBX);
+  unsigned off_w[NCW], off_x[NCX];
+#pragma unroll
+  for (int i = 0; i < NCW; ++i) {
+    const int r = (i * WAVES + wave) * RPCW + lane / (RBW / 16);
+    off_w[i] = n0 + r < a.n ? (unsigned)(r * (int)a.ldw + first_w) : kOobGroup;
+  }
+#pragma unroll
+  for (int i = 0; i < NCX; ++i) {
+    const int r = (i * WAVES + wave) * RPCX + lane / (RBX / 16);
+    off_x[i] = m0 + r < a.m ? (unsigned)(r * (int)a.ldx + first_x) : kOobGroup;
+  }
+  const unsigned off_sw = n0 + wave * SW + lane < a.n ? (unsigned)((wave * SW + lane) * (int)a.ldws) : kOobGroup;
+  const unsigned off_sx = m0 + wave * SX + lane < a.m ? (unsigned)((wave * SX + lane) * (int)a.ldxs) : kOobGroup;
+
+  auto fetch = [&](int c, int stage) __attribute__((always_inline)) {
+    const int step = begin + c * WK + team;
+    char* dst = lds + stage * STAGE + team * TEAM;
+    auto go = [&](auto tail) __attribute__((always_inline)) {
+      const bool none = tail.value && step >= end;
+      const auto at = [&](int rb, unsigned bytes) {
+        const unsigned k = (unsigned)step * (unsigned)rb;
+        return tail.value ? uniform_part(k, bytes) : (int)k;
+      };
+      const int kw = at(RBW, vw.bytes), kx = at(RBX, vx.bytes), ksw = at(4, vsw.bytes), ksx = at(4, vsx.bytes);
+      const bool out_w = none || (tail.value && step * RBW + first_w >= row_w);
+      const bool out_x = none || (tail.value && step * RBX + first_x >= row_x);
+#pragma unroll
+      for (int i = 0; i < NCW; ++i) copy_lds<16>(rw, dst + (i * WAVES + wave) * 1024, out_w ? kOobGroup : off_w[i], kw);
+#pragma unroll
+      for (int i = 0; i < NCX; ++i)
+        copy_lds<16>(rx, dst + AT_X + (i * WAVES + wave) * 1024, out_x ? kOobGroup : off_x[i], kx);
+      // some lane of every wave copies, so that the copies on their way are as many in each
+      if (lane < SW) copy_lds<4>(rsw, dst + AT_SW + wave * SW * 4, none ? kOobGroup : off_sw, ksw);
+      if (lane < SX) copy_lds<4>(rsx, dst + AT_SX + wave * SX * 4, none ? kOobGroup : off_sx, ksx);
+    };
+    if (step * 4 + 4 <= a.blocks && step < end) go(std::false_type{});
+    else go(std::true_type{});
+  };
+
+  const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+  const int lrow = lane & 15, kg = lane >> 4;
+  // Where a lane's 32 elements of row lrow lie: e2m1 one group, e4m3 two.
+  const auto place = [&](int rb, int half) {
+    const int g = rb == 64 ? kg : EXACT ? 2 * kg + half : kg + 4 * half;
+    return lrow * rb + ((g ^ (lrow >> 1)) & (rb / 16 - 1)) * 16;
+  };
+  const int pw0 = place(RBW, 0), pw1 = place(RBW, 1), px0 = place(RBX, 0), px1 = place(RBX, 1);
+  f32x4 acc[TN][TM] = {};
+  auto multiply = [&](int c, int stage) __attribute__((always_inline)) {
+    const char* base = lds + stage * STAGE + team * TEAM;
+    const char *sw = base + wn * RBW, *sx = base + AT_X + wm * RBX;
+    const unsigned char *cw = (const unsigned char*)base + AT_SW + (wn + lrow) * 4 + kg,
+                        *cx = (const unsigned char*)base + AT_SX + (wm + lrow) * 4 + kg;
+    // scales behind a row's last block are not read as such: their elements are 0
+    const bool real = (begin + c * WK + team) * 4 + kg < a.blocks;
+    MxFrag<FW> fw[TN];
+    MxFrag<FX> fx[TM];
+    int ew[TN], ex[TM];
+#pragma unroll
+    for (int i = 0; i < TN; ++i) {
+      fw[i].lo = *(const u32x4*)(sw + i * 16 * RBW + pw0);
+      if constexpr (FW == CT_MX_E4M3) fw[i].hi = *(const u32x4*)(sw + i * 16 * RBW + pw1);
+      ew[i] = cw[i * 64];
+    }
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      fx[j].lo = *(const u32x4*)(sx + j * 16 * RBX + px0);
+      if constexpr (FX == CT_MX_E4M3) fx[j].hi = *(const u32x4*)(sx + j * 16 * RBX + px1);
+      ex[j] = cx[j * 64];
+    }
+    if (!real) {
+#pragma unroll
+      for (int i = 0; i < TN; ++i) ew[i] = 127;
+#pragma unroll
+      for (int j = 0; j < TM; ++j) ex[j] = 127;
+    }
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int c4 = 0; c4 < 4; ++c4) {
+        bf16x8 bw[TN];
+#pragma unroll
+        for (int i = 0; i < TN; ++i) bw[i] = mx_bf16<FW>(fw[i], c4, (unsigned)ew[i]);
+#pragma unroll
+        for (int j = 0; j < TM; ++j) {
+          const bf16x8 bx = mx_bf16<FX>(fx[j], c4, (unsigned)ex[j]);
+#pragma unroll
+          for (int i = 0; i < TN; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[i], bx, acc[i][j], 0, 0, 0);
+        }
+      }
+    } else {
+      constexpr int CW = mx_code(FW), CX = mx_code(FX);
+#pragma unroll
+      for (int j = 0; j < TM; ++j)
+#pragma unroll
+        for (int i = 0; i < TN; ++i)
+          acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(mx_operand<FW>(fw[i]), mx_operand<FX>(fx[j]), acc[i][j],
+                                                                       CW, CX, 0, ew[i], 0, ex[j]);
+    }
+  };
+
+  // Steps past the end read 0, so that STAGES - 1 of them are in flight at every wait. The
+  // barrier also says that every wave has read the stage that is filled next.
+  static_assert((NCW + NCX + 2) * (STAGES - 2) <= 63, "the counter of loads on their way has six bits");
+  if (rounds > 0) {
+#pragma unroll
+    for (int c = 0; c < STAGES - 1; ++c) fetch(c, c);
+    int stage = 0;
+    for (int c = 0; c < rounds; ++c) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NCW + NCX + 2) * (STAGES - 2)) : "memory");
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      fetch(c + STAGES - 1, stage ? stage - 1 : STAGES - 1);
+      multiply(c, stage);
+      stage = stage == STAGES - 1 ? 0 : stage + 1;
+    }
+  }
+  // The compiler counts the waits behind this instruction's results by the passes of 4-bit
+  // operands on some paths, four too few of e4m3.
+  asm volatile("s_nop 15" ::: "memory");
+  write_tile<BM, BN, WM, WN, WK, STAGES * STAGE>(a, lds, acc, m0, n0, sp);
+}
+
+// ------------------------------------------------------------------ plans and launches
+enum { MXL_32, MXL_64, MXL_128X64, MXL_128, MXL_256, MXL_KINDS };
+struct MxShape {
+  int bm, bn, wm, wn, wk, stages;
+};
+constexpr MxShape kMxTiles[MXL_KINDS] = {{32, 32, 1, 2, 4, 3}, {64, 64, 2, 2, 2, 3}, {128, 64, 2, 2, 1, 3},
+                                         {128, 128, 2, 2, 1, 2}, {256, 256, 4, 2, 1, 2}};
+
+static int64_t tiles_of(const ct_mx_linear_op& op, int kind) {
+  const MxShape t = kMxTiles[kind];
+  return (((int64_t)op.m + t.bm - 1) / t.bm) * (((int64_t)op.n + t.bn - 1) / t.bn);
+}
+
+MxLinearPlan plan_mx_linear(const ct_mx_linear_op& op) {
+  MxLinearPlan p = {};
+  const int steps = (int)(((int64_t)op.k + 127) / 128);
+  auto rounds = [&](int kind) { return (double)((tiles_of(op, kind) + kPlanCus - 1) / kPlanCus); };
+  const std::pair<int, double> costs[] = {{MXL_64, 0.5 * rounds(MXL_64)},
+                                          {MXL_128X64, 0.8 * rounds(MXL_128X64)},
+                                          {MXL_128, 1.3 * rounds(MXL_128)},
+                                          {MXL_256, op.out_dtype == CT_DT_F32 ? 1e299 : 4.0 * rounds(MXL_256)}};
+  double least = 1e300;
+  for (auto [kind, cost] : costs)
+    if (cost < least) {
+      least = cost;
+      p.kind = kind;
+    }
+  if (op.m <= 32 || (p.kind == MXL_64 && tiles_of(op, MXL_64) < kPlanCus * 3 / 4)) p.kind = MXL_32;
+  // A long reduction over few tiles: slices of it, of 32 steps at least, so that they save more
+  // than the second kernel takes
+  const int64_t blocks = tiles_of(op, p.kind);
+  int split = 1;
+  if (blocks <= kPlanCus / 4 && steps >= 64) split = (int)(kPlanCus / blocks < steps / 32 ? kPlanCus / blocks : steps / 32);
+  const int per = steps ? (steps + split - 1) / split : 1;
+  p.split = steps ? (steps + per - 1) / per : 1;
+  p.per_split = per;
+  p.ws_floats = p.split > 1 ? (int64_t)p.split * op.m * ((op.n + 3) / 4 * 4) : 0;
+  return p;
+}
+
+template <int FW, int FX, bool EXACT, int KIND>
+static int mxl_launch(MxLinearArgs a, hipStream_t st) {
+  constexpr MxShape t = kMxTiles[KIND];
+  constexpr int stage = t.wk * (t.bn * (mx_step_bytes(FW) + 4) + t.bm * (mx_step_bytes(FX) + 4));
+  if (!set_tiles(a, t.bm, t.bn, 64 * t.wm * t.wn * t.wk)) return refuse_size("ct_mx_linear_run");
+  return launch(mx_linear_kernel<FW, FX, EXACT, t.bm, t.bn, t.wm, t.wn, t.wk, t.stages>,
+                dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)a.split), 64 * t.wm * t.wn * t.wk, t.stages * stage, st, a);
+}
+template <int FW, int FX, bool EXACT>
+static int mxl_pick(const MxLinearArgs& a, int kind, hipStream_t st) {
+  switch (kind) {
+    case MXL_32: return mxl_launch<FW, FX, EXACT, MXL_32>(a, st);
+    case MXL_64: return mxl_launch<FW, FX, EXACT, MXL_64>(a, st);
+    case MXL_128X64: return mxl_launch<FW, FX, EXACT, MXL_128X64>(a, st);
+    case MXL_128: return mxl_launch<FW, FX, EXACT, MXL_128>(a, st);
+    default:
+      if constexpr (!EXACT) return mxl_launch<FW, FX, EXACT, MXL_256>(a, st);
+      return mxl_launch<FW, FX, EXACT, MXL_128>(a, st);  // with the elements in bf16 it leaves no registers
+  }
+}
+template <int FW, int FX>
+static int mxl_sums(const MxLinearArgs& a, int kind, hipStream_t st) {
+  return a.out_bf16 ? mxl_pick<FW, FX, false>(a, kind, st) : mxl_pick<FW, FX, true>(a, kind, st);
+}
+
+int launch_mx_linear(const ct_mx_linear_op& op, const MxLinearPlan& p, const MxLinearArrays& v, void* stream) {
+  MxLinearArgs a = {};
+  a.x = (const char*)v.x; a.xs = (const unsigned char*)v.xs;
+  a.w = (const char*)v.w; a.wsc = (const unsigned char*)v.ws;
+  a.bias = v.bias; a.res = v.res; a.y = v.y; a.ws = v.scratch;
+  a.m = op.m; a.n = op.n; a.blocks = mx_blocks(op.k);
+  a.ldx = op.ldx; a.ldxs = op.ldxs; a.ldw = op.ldw; a.ldws = op.ldws; a.ldr = op.ldr; a.ldy = op.ldy;
+  a.act = op.act; a.res_mode = op.res; a.out_bf16 = op.out_dtype == CT_DT_BF16;
+  a.split = p.split; a.per_split = p.per_split;
+  a.stream = (int64_t)op.m * op.n * elem_bytes(op.out_dtype) >= kStreamBytes;
+  hipStream_t st = (hipStream_t)stream;
+  const bool w8 = op.w_format == CT_MX_E4M3, x8 = op.x_format == CT_MX_E4M3;
+  const int rc = w8 ? x8 ? mxl_sums<CT_MX_E4M3, CT_MX_E4M3>(a, p.kind, st) : mxl_sums<CT_MX_E4M3, CT_MX_E2M1>(a, p.kind, st)
+                    : x8 ? mxl_sums<CT_MX_E2M1, CT_MX_E4M3>(a, p.kind, st) : mxl_sums<CT_MX_E2M1, CT_MX_E2M1>(a, p.kind, st);
+  return rc || p.split == 1 ? rc : launch_join(a, st);
+}
+
+}  // namespace ct

@@ -1,5 +1,5 @@
-// Internal declarations of the sequence-block operators (ct_linear, ct_causal_conv,
-// ct_scan): the plans that the workspace functions and the launchers both take, so that a
+// Internal declarations of the sequence- and linear-attention-block operators (ct_linear,
+// ct_causal_conv, ct_scan, ct_norm, ct_mx, ct_decay_attention): the plans that the workspace functions and the launchers both take, so that a
 // call is launched as its workspace was sized.
 #pragma once
 
@@ -60,5 +60,45 @@ struct ScanArrays {
   float* ws;
 };
 int launch_scan(const ct_scan_op& op, const ScanPlan& p, const SeqView& s, const ScanArrays& v, void* stream);
+
+// ---- ct_norm, ct_mx ----
+int launch_norm(const ct_norm_op& op, const void* x, const void* res, void* sum, const float* w, const void* z, void* y,
+                void* scales, void* stream);
+// x to q and scales, or with `values` back.
+int launch_mx(const ct_mx_op& op, void* x, void* q, void* scales, bool values, void* stream);
+
+// ---- ct_mx_linear ----
+struct MxLinearPlan {
+  int kind;           // the kernel (k_mx_linear.hip)
+  int split;          // slices of the reduction, each with partial sums of its own
+  int per_split;      // steps of 128 elements in a slice
+  int64_t ws_floats;  // split * m * n where the reduction is split
+};
+MxLinearPlan plan_mx_linear(const ct_mx_linear_op& op);
+struct MxLinearArrays {
+  const void *x, *xs, *w, *ws;
+  const float* bias;
+  const void* res;
+  void* y;
+  float* scratch;
+};
+int launch_mx_linear(const ct_mx_linear_op& op, const MxLinearPlan& p, const MxLinearArrays& v, void* stream);
+
+// ---- ct_decay_attention ----
+struct DecayPlan {
+  int piece;          // tokens of a piece (0: every sequence in one)
+  int64_t pieces;     // pieces in all, an upper bound
+  int64_t ws_floats;
+};
+DecayPlan plan_decay(const ct_decay_attention_op& op, const ct_sequences& s);
+struct DecayArrays {
+  const void *q, *k, *v, *delta;
+  const float *dt_bias, *a, *state_in;
+  float* state_out;
+  void* o;
+  float* ws;
+};
+int launch_decay(const ct_decay_attention_op& op, const DecayPlan& p, const SeqView& s, const DecayArrays& v,
+                 int max_len, void* stream);
 
 }  // namespace ct

@@ -1,0 +1,795 @@
+"""The linear-attention-block operators against their formulas in 64 bits on the CPU.
+
+Tolerances are error bounds worked out beside each reference, elementwise: u = 2^-24 for every
+fp32 operation on what it adds up, a few units for exp, log and reciprocals, and the output's own
+rounding (2^-8 relative for bf16, 2^-24 for fp32). Microscaled rows are compared element for
+element where their values are given, else through what rounding allows."""
+import math
+
+import pytest
+import torch
+
+from paper_2008_03602_amd import _lib as L
+from gpu_util import device_ready, note
+from test_gpu_sequence import act64, gen, normal, placed, stream, within
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+F, B, D = torch.float32, torch.bfloat16, torch.float64
+CODE = {F: L.DT_F32, B: L.DT_BF16}
+ROUND = {F: U, B: 2.0 ** -8}
+NAN, INF = float("nan"), float("inf")
+FORMATS = (L.MX_E4M3, L.MX_E2M1)
+TOP = {L.MX_E4M3: 448.0, L.MX_E2M1: 6.0}
+TOP_E = {L.MX_E4M3: 8, L.MX_E2M1: 2}
+LOW_E = {L.MX_E4M3: -6, L.MX_E2M1: 0}
+BITS = {L.MX_E4M3: 3, L.MX_E2M1: 1}
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _device():
+    device_ready()
+    yield
+
+
+# ------------------------------------------------------------------ microscaled rows in plain Python
+def table(fmt):
+    """Values of all codes, in 64 bits."""
+    if fmt == L.MX_E2M1:
+        pos = [0, 0.5, 1, 1.5, 2, 3, 4, 6]
+    else:
+        pos = [(1 + (c & 7) / 8) * 2.0 ** ((c >> 3) - 7) if c >> 3 else (c & 7) * 2.0 ** -9 for c in range(127)] + [NAN]
+    return torch.tensor(pos + [-v for v in pos], dtype=D)
+
+
+def codes_of(q, cols, fmt):
+    """[rows, whole blocks of columns] codes of stored rows."""
+    blocks = (cols + 31) // 32
+    if fmt == L.MX_E4M3:
+        return q[:, :blocks * 32].long()
+    b = q[:, :blocks * 16].long()
+    return torch.stack([b & 15, b >> 4], 2).reshape(b.shape[0], -1)
+
+
+def values_of(q, scales, cols, fmt):
+    """What stored rows stand for, in 64 bits."""
+    v = table(fmt)[codes_of(q, cols, fmt)]
+    s = scales[:, :(cols + 31) // 32].long()
+    p = torch.where(s == 255, NAN, torch.pow(torch.tensor(2.0, dtype=D), (s - 127).double()))
+    return (v * p.repeat_interleave(32, 1))[:, :cols]
+
+
+def exponent(v):
+    """floor(log2 v) of positive v."""
+    return torch.frexp(v)[1].double() - 1
+
+
+def two_to(e):
+    return torch.ldexp(torch.ones_like(e, dtype=D), e.long())
+
+
+def quantise64(x, fmt):
+    """(codes over whole blocks, scale bytes over whole groups) of x, by the definition."""
+    rows, cols = x.shape
+    blocks = (cols + 31) // 32
+    v = torch.zeros(rows, blocks * 32, dtype=D)
+    v[:, :cols] = x.double()
+    v = v.reshape(rows, blocks, 32)
+    m = v.abs().amax(2)
+    bad = ~torch.isfinite(v).all(2)
+    e = torch.where(m > 0, exponent(m.clamp(min=1e-300)) - TOP_E[fmt], -127.0).clamp(min=-127)
+    e = torch.where(bad, 0.0, e)
+    t = (v / two_to(e)[..., None]).abs().clamp(max=TOP[fmt])
+    step = two_to(torch.where(t > 0, exponent(t.clamp(min=1e-300)), -300.0).clamp(min=LOW_E[fmt]) - BITS[fmt])
+    r = (torch.round(t / step) * step).clamp(max=TOP[fmt])
+    pos = table(fmt)[:128 if fmt == L.MX_E4M3 else 8]
+    order = torch.where(torch.isnan(pos), INF, pos)
+    code = torch.searchsorted(order, torch.where(torch.isnan(r), 0.0, r))
+    code = code + torch.signbit(v).long() * len(pos)
+    s = torch.zeros(rows, (blocks + 3) // 4 * 4, dtype=torch.long)
+    s[:, :blocks] = torch.where(bad, 255, (e + 127).long())
+    return code.reshape(rows, -1), s, bad
+
+
+def mx_buffers(rows, cols, fmt, pitch=0, spitch=0, fill=0xA5):
+    q = torch.full((rows, pitch or L.mx_row_bytes(cols, fmt)), fill, dtype=torch.uint8, device="cuda")
+    s = torch.full((rows, spitch or L.mx_scale_bytes(cols)), fill, dtype=torch.uint8, device="cuda")
+    return q, s
+
+
+def check_quantise(x, fmt, pitch=0, shift=0, qpitch=0, spitch=0, what=""):
+    rows, cols = x.shape
+    what = what or "quantise %dx%d %s format %d" % (rows, cols, x.dtype, fmt)
+    note(what)
+    xd = placed(x, pitch, shift)
+    q, s = mx_buffers(rows, cols, fmt, qpitch, spitch)
+    op = L.make_mx(rows, cols, CODE[x.dtype], fmt, ldx=pitch, ldq=qpitch, lds=spitch)
+    L.ct_mx_quantise_run(op, xd, q, s, stream())
+    torch.cuda.synchronize()
+    code, scale, bad = quantise64(x, fmt)
+    got, gots = codes_of(q.cpu(), cols, fmt), s.cpu().long()
+    n = scale.shape[1]
+    assert torch.equal(gots[:, :n], scale), what + ": scales"
+    fine = ~bad.repeat_interleave(32, 1)
+    assert torch.equal(got[fine], code[fine]), what + ": elements"
+    assert (got[:, cols:] % (128 if fmt == L.MX_E4M3 else 8) == 0).all(), what + ": behind the row"
+    assert (gots[:, n:] == 0xA5).all() and (q.cpu()[:, L.mx_row_bytes(cols, fmt):] == 0xA5).all(), what + ": between rows"
+    y = placed(torch.full((rows, cols), NAN, dtype=x.dtype), pitch, shift, fill=7.0)
+    L.ct_mx_values_run(op, q, s, y, stream())
+    torch.cuda.synchronize()
+    want = values_of(q.cpu(), s.cpu(), cols, fmt)
+    assert torch.equal(torch.isnan(y.cpu()), torch.isnan(want)), what + ": NaN"
+    keep = ~torch.isnan(want)
+    assert torch.equal(y.cpu()[keep], want.to(x.dtype)[keep]), what + ": values"
+    if pitch > cols:
+        assert (y.as_strided((rows, pitch - cols), (pitch, 1), y.storage_offset() + cols) == 7.0).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 8), (2, 31), (5, 32), (4, 33), (7, 100), (3, 129), (33, 515), (2, 4096)])
+def test_quantise_sizes(rows, cols, dtype, fmt):
+    check_quantise(normal(gen(rows * cols), rows, cols, dtype=dtype), fmt)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [B, F])
+def test_quantise_strides_and_alignment(dtype, fmt):
+    for shift, pitch, qp, sp in ((0, 107, 256, 12), (1, 104, 128, 4), (3, 131, 0, 0), (8, 128, 144, 8)):
+        check_quantise(normal(gen(shift), 6, 100, dtype=dtype), fmt, pitch, shift, qp, sp)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [B, F])
+def test_quantise_ties_borders_and_extremes(dtype, fmt):
+    t = table(fmt)[:len(table(fmt)) // 2]
+    t = t[~torch.isnan(t)]
+    ties = (t[1:] + t[:-1]) / 2  # between two elements: to the even one
+    rows = []
+    for scale in (0, -20, 60, -118, 118 if fmt == L.MX_E4M3 else 124):
+        for v in (t, ties, ties * (1 + 2.0 ** -7), ties * (1 - 2.0 ** -7)):
+            v = torch.cat([v, torch.zeros(-len(v) % 31, dtype=D)]).reshape(-1, 31)
+            v = torch.cat([v, torch.full((v.shape[0], 1), 2.0 ** TOP_E[fmt], dtype=D)], 1)
+            rows.append(torch.ldexp(v, torch.tensor(scale)))
+    check_quantise(torch.cat(rows).to(dtype), fmt, what="quantise ties")
+    border = torch.zeros(12, 32, dtype=D)
+    top = 2.0 ** TOP_E[fmt]
+    for i, m in enumerate((top, top * 2, top * 1.99, top * 1.5, 2.0 ** -126, 2.0 ** -127, 2.0 ** -133, 2.0 ** -119, 0.0,
+                           2.0 ** 127, 1.5 * 2.0 ** 127, 1.99 * 2.0 ** 127)):
+        border[i] = torch.linspace(-1, 1, 32, dtype=D) * m
+    check_quantise(border.to(dtype), fmt, what="quantise borders")
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [B, F])
+def test_quantise_keeps_infinities_and_nan_to_their_blocks(dtype, fmt):
+    x = normal(gen(3), 6, 160, dtype=dtype)
+    x[0, 3], x[1, 40], x[2, 159], x[3, 64:96], x[4, 0] = NAN, INF, -INF, NAN, -NAN
+    check_quantise(x, fmt)
+
+
+# ------------------------------------------------------------------ product
+def random_rows(g, rows, cols, fmt, low=118, high=136, pitch=0, spitch=0):
+    """Stored rows of any codes but NaN, and their values."""
+    blocks = (cols + 31) // 32
+    n = 256 if fmt == L.MX_E4M3 else 16
+    code = torch.randint(0, n, (rows, blocks * 32), generator=g)
+    if fmt == L.MX_E4M3:
+        code[code % 128 == 127] -= 1
+    code[:, cols:] = 0
+    stored = code if fmt == L.MX_E4M3 else code[:, ::2] | code[:, 1::2] << 4
+    q = torch.full((rows, pitch or L.mx_row_bytes(cols, fmt)), 0x7F, dtype=torch.uint8)
+    q[:, :stored.shape[1]] = stored.to(torch.uint8)
+    s = torch.full((rows, spitch or L.mx_scale_bytes(cols)), 255, dtype=torch.uint8)  # NaN behind the blocks
+    s[:, :blocks] = torch.randint(low, high, (rows, blocks), generator=g).to(torch.uint8)
+    return q.cuda(), s.cuda(), values_of(q, s, cols, fmt)
+
+
+def dropped(x, w):
+    """What the matrix cores may drop: of each eight products seven times 2^-13 of the largest."""
+    m, k = x.shape
+    pad = -k % 8
+    xa = torch.nn.functional.pad(x.abs(), (0, pad)).reshape(m, -1, 8)
+    wa = torch.nn.functional.pad(w.abs(), (0, pad)).reshape(w.shape[0], -1, 8)
+    out = torch.zeros(m, w.shape[0], dtype=D)
+    for i in range(m):
+        out[i] = (xa[i][None] * wa).amax(2).sum(1)
+    return 7 * 2.0 ** -13 * out
+
+
+def check_product(m, n, k, fx, fw, out, act=0, res=0, bias=True, seed=0, xp=0, wp=0, sp=0, yp=0, shift=0, in_place=False,
+                  low=118, high=136):
+    g = gen(seed)
+    what = "mx product m%d n%d k%d formats %d %d -> %s act%d res%d" % (m, n, k, fx, fw, out, act, res)
+    note(what)
+    xq, xs, x = random_rows(g, m, k, fx, low, high, xp, sp)
+    wq, wsc, w = random_rows(g, n, k, fw, low, high, wp, sp)
+    size = float((x.abs().mean() * w.abs().mean() * k).item()) if k else 1.0
+    b = normal(g, n, std=size) if bias else None
+    r = normal(g, m, n, std=size, dtype=out) if res else None
+    rd = placed(r, yp, shift) if res else None
+    yd = rd if in_place else placed(torch.full((m, n), NAN, dtype=out), yp, shift, fill=7.0)
+    op = L.make_mx_linear(m, n, k, fx, fw, CODE[out], act, res, xp, sp, wp, sp, yp, yp)
+    ws = torch.full((max(16, L.ct_mx_linear_workspace(op)),), 255, dtype=torch.uint8, device="cuda")
+    L.ct_mx_linear_run(op, xq, xs, wq, wsc, b.cuda() if bias else None, rd, yd, ws, stream())
+    torch.cuda.synchronize()
+    v, mag = x @ w.t(), x.abs() @ w.abs().t()
+    bound = dropped(x, w) if out == B else torch.zeros_like(v)
+    if bias:
+        v, mag = v + b.double(), mag + b.double().abs()
+    if res == L.RES_ADD_ACT:
+        v, mag = v + r.double(), mag + r.double().abs()
+    y = act64(v, act)
+    # the activations' slopes are at most 1.13, their own errors a few units of what goes in
+    bound = 1.13 * (bound + (k + 4) * U * mag) + 8 * U * v.abs()
+    if res == L.RES_ADD:
+        y = y + r.double()
+        bound = bound + U * y.abs()
+    bound = bound + ROUND[out] * (y.abs() + bound)
+    within(yd, y, bound, what)
+    if yp > n and not in_place:
+        assert (yd.as_strided((m, yp - n), (yp, 1), yd.storage_offset() + n) == 7.0).all(), what
+
+
+PAIRS = [(x, w) for x in FORMATS for w in FORMATS]
+
+
+@pytest.mark.parametrize("out", [B, F])
+@pytest.mark.parametrize("fx,fw", PAIRS)
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 16, 32), (2, 17, 40), (5, 33, 129), (16, 64, 128), (33, 48, 1000),
+                                   (65, 129, 96), (130, 70, 515), (257, 255, 160)])
+def test_product_sizes_and_formats(m, n, k, fx, fw, out):
+    check_product(m, n, k, fx, fw, out, act=(m + n) % 5, res=k % 3, seed=m * n + k)
+
+
+@pytest.mark.parametrize("out", [B, F])
+@pytest.mark.parametrize("m,n,k", [(1300, 1100, 96), (700, 900, 128), (2100, 2080, 64), (40, 2500, 288), (3, 70, 9000)])
+def test_product_tiles(m, n, k, out):
+    for fx, fw in ((L.MX_E4M3, L.MX_E2M1), (L.MX_E2M1, L.MX_E4M3)):
+        check_product(m, n, k, fx, fw, out, act=3, res=1, seed=k)
+
+
+@pytest.mark.parametrize("fx,fw", PAIRS)
+def test_product_strides(fx, fw):
+    for m, n, k in ((3, 24, 50), (24, 200, 77), (130, 70, 264)):
+        row = L.mx_row_bytes(k, L.MX_E4M3)
+        check_product(m, n, k, fx, fw, B, act=3, res=1, seed=1, xp=row + 16, wp=row + 48, sp=L.mx_scale_bytes(k) + 4, yp=n + 5, shift=1)
+        check_product(m, n, k, fx, fw, F, act=1, res=2, seed=2, xp=row + 64, wp=row, sp=L.mx_scale_bytes(k) + 16, yp=n + 3, shift=3)
+        check_product(m, n, k, fx, fw, F, act=0, res=1, seed=3, yp=n + 1, in_place=True)
+
+
+@pytest.mark.parametrize("act", range(5))
+@pytest.mark.parametrize("res", range(3))
+def test_product_epilogues(act, res):
+    for out in (B, F):
+        check_product(70, 132, 64, L.MX_E4M3, L.MX_E2M1, out, act, res, bias=bool(act % 2), seed=act)
+
+
+def test_product_of_split_reductions():
+    for fx, fw in PAIRS:
+        for out in (B, F):
+            op = L.make_mx_linear(20, 24, 16500, fx, fw, CODE[out])
+            assert L.ct_mx_linear_workspace(op) > 0
+            check_product(20, 24, 16500, fx, fw, out, act=2, res=2, seed=5)
+
+
+def test_product_without_a_reduction_is_its_epilogue():
+    for out in (B, F):
+        b, r = normal(gen(1), 40), normal(gen(2), 9, 40, dtype=out)
+        y = torch.empty(9, 40, dtype=out, device="cuda")
+        op = L.make_mx_linear(9, 40, 0, L.MX_E4M3, L.MX_E4M3, CODE[out], L.ACT_RELU, L.RES_ADD)
+        L.ct_mx_linear_run(op, None, None, None, None, b.cuda(), r.cuda(), y, None, stream())
+        assert torch.equal(y.cpu(), (b.clamp(min=0) + r.float()).to(out))
+
+
+def test_product_with_scales_at_the_ends():
+    """The least scale, the largest ones, and NaN: only the row or column of a block is NaN."""
+    for fx, fw in PAIRS:
+        for out in (B, F):
+            check_product(20, 40, 96, fx, fw, out, seed=7, low=0, high=3, bias=False)
+            g = gen(9)
+            xq, xs, x = random_rows(g, 40, 200, fx, 240, 247)
+            wq, wsc, w = random_rows(g, 48, 200, fw, 1, 8)
+            xs[5, 2], wsc[7, 6] = 255, 255
+            y = torch.empty(40, 48, dtype=out, device="cuda")
+            L.ct_mx_linear_run(L.make_mx_linear(40, 48, 200, fx, fw, CODE[out]), xq, xs, wq, wsc, None, None, y, None, stream())
+            want = x @ w.t()
+            want[5], want[:, 7] = NAN, NAN
+            bound = dropped(x, w) + 204 * U * (x.abs() @ w.abs().t())
+            within(y, want, bound + ROUND[out] * (want.abs() + bound), "scales at the ends")
+
+
+# ------------------------------------------------------------------ norm
+def check_norm(rows, cols, dtype, out, groups=1, residual=True, gate=True, weight=True, keep=True, seed=0, pitch=0, shift=0,
+               eps=1e-5, in_place=False, std=1.0):
+    g = gen(seed)
+    what = "norm %dx%d/%d %s -> %s res%d gate%d" % (rows, cols, groups, dtype, out, residual, gate)
+    note(what)
+    x, res, z = (normal(g, rows, cols, std=std, dtype=dtype) for _ in range(3))
+    w = normal(g, cols, mean=1.0, std=0.3)
+    p = pitch or cols
+    xd, rd, zd = (placed(t, pitch, shift) for t in (x, res, z / std))
+    z = (z / std).to(dtype)
+    h = x.double() + res.double() * residual
+    sd = (xd if in_place else placed(torch.full((rows, cols), NAN, dtype=dtype), pitch, shift, fill=7.0)) if keep else None
+    mx = out in FORMATS
+    if mx:
+        y, s = mx_buffers(rows, cols, out, L.mx_row_bytes(cols, out) + 16, L.mx_scale_bytes(cols) + 4)
+    else:
+        y, s = placed(torch.full((rows, cols), NAN, dtype=out), pitch, shift, fill=7.0), None
+    op = L.make_norm(rows, cols, CODE[dtype], out if mx else CODE[out], groups, eps, p, p, p, p, y.stride(0),
+                     s.stride(0) if mx else 0)
+    L.ct_norm_run(op, xd, rd if residual else None, sd, w.cuda() if weight else None, zd if gate else None, y, s, stream())
+    torch.cuda.synchronize()
+    n = cols // groups
+    v = h.reshape(rows, groups, n)
+    ref = (v / torch.sqrt((v * v).mean(2, keepdim=True) + eps)).reshape(rows, cols)
+    # half the relative error of the sum of n squares, and a few units; the gate's exponential
+    # takes the rounding of z log2(e) with it
+    rel = (n / 2 + 12) * U * torch.ones_like(ref)
+    if weight:
+        ref = ref * w.double()
+    if gate:
+        zz = z.double()
+        ref = ref * zz / (1 + torch.exp(-zz))
+        rel = rel + (2 * zz.abs() + 8) * U
+    bound = rel * ref.abs()
+    if keep:
+        within(sd, h, (U if residual else 0.0) * h.abs() + ROUND[dtype] * h.abs() * (1 + U), what + " sum")
+    if not mx:
+        within(y, ref, bound + ROUND[out] * (ref.abs() + bound), what)
+        if pitch > cols:
+            assert (y.as_strided((rows, pitch - cols), (pitch, 1), y.storage_offset() + cols) == 7.0).all()
+        return
+    q, s = y.cpu(), s.cpu()
+    blocks, row = (cols + 31) // 32, L.mx_row_bytes(cols, out)
+    assert (q[:, row:] == 0xA5).all() and (s[:, L.mx_scale_bytes(cols):] == 0xA5).all()
+    assert (s[:, blocks:L.mx_scale_bytes(cols)] == 0).all()
+    assert (codes_of(q, cols, out)[:, cols:] == 0).all()
+    full, fb = torch.zeros(rows, blocks * 32, dtype=D), torch.zeros(rows, blocks * 32, dtype=D)
+    full[:, :cols], fb[:, :cols] = ref, bound
+    m, i = full.abs().reshape(rows, blocks, 32).max(2)
+    mb = fb.reshape(rows, blocks, 32).amax(2)
+    e = s[:, :blocks].double() - 127
+    lo, hi = ((exponent((m + k * mb).clamp(min=1e-300)) - TOP_E[out]).clamp(min=-127) for k in (-1, 1))
+    assert ((e >= lo) & (e <= hi)).all(), what + ": scales"
+    t, scale = full, two_to(e).repeat_interleave(32, 1)
+    got = values_of(q, s, blocks * 32, out)
+    reach = (t.abs() + fb) / scale
+    step = two_to(exponent(reach.clamp(min=1e-300)).clamp(min=LOW_E[out]) - BITS[out])
+    near = (got - t).abs() <= (step / 2 * scale + fb) * (1 + 1e-12)
+    full_scale = (reach >= TOP[out]) & (got == torch.sign(t) * TOP[out] * scale)
+    assert (near | full_scale).all(), what + ": elements"
+
+
+@pytest.mark.parametrize("out", [B, F, *FORMATS])
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("rows,cols", [(1, 1), (3, 7), (2, 40), (5, 64), (9, 100), (4, 257), (3, 512), (2, 515), (3, 2048),
+                                       (2, 4100), (2, 8192), (1, 16384), (2, 20000)])
+def test_norm_sizes_and_types(rows, cols, dtype, out):
+    check_norm(rows, cols, dtype, out, residual=bool(cols % 2) or cols == 2048, gate=cols % 3 != 0, seed=cols)
+
+
+@pytest.mark.parametrize("out", [B, F, *FORMATS])
+@pytest.mark.parametrize("groups,part", [(4, 32), (3, 64), (32, 128), (2, 288), (5, 1024), (2, 16416)])
+def test_norm_of_parts(groups, part, out):
+    check_norm(5, groups * part, B, out, groups, residual=False, seed=part)
+    check_norm(3, groups * part, F, out, groups, weight=False, gate=False, seed=part)
+    if out in (B, F):
+        check_norm(4, groups * 21, B, out, groups, seed=part)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("pitch,shift", [(107, 1), (104, 8), (131, 3)])
+def test_norm_strides_alignment_and_sums_in_place(pitch, shift, dtype):
+    for out in (B, F, *FORMATS):
+        check_norm(6, 100, dtype, out, pitch=pitch, shift=shift, seed=shift)
+        check_norm(6, 100, dtype, out, pitch=pitch, shift=shift, in_place=True, seed=shift + 1)
+    check_norm(2, 20000, dtype, B, in_place=True, seed=4)
+    check_norm(3, 96, dtype, B, keep=False, residual=False, gate=False, seed=5)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+def test_norm_of_zeros_small_and_large_values(dtype):
+    for std in (0.0, 1e-12, 1e15):
+        if std:
+            check_norm(3, 200, dtype, F, std=std, eps=1e-30, seed=1)
+    x = torch.zeros(2, 96, dtype=dtype, device="cuda")
+    for out in (L.DT_F32, *FORMATS):
+        y, s = (torch.empty(2, 96, device="cuda"), None) if out == L.DT_F32 else mx_buffers(2, 96, out)
+        L.ct_norm_run(L.make_norm(2, 96, CODE[dtype], out, eps=1e-5), x, None, None, None, None, y, s, stream())
+        torch.cuda.synchronize()
+        assert (y == 0).all() and (s is None or (s == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+def test_norm_keeps_nan_to_its_part(dtype):
+    x = normal(gen(2), 4, 256, dtype=dtype)
+    bad = x.clone()
+    bad[1, 70], bad[2, 255], bad[3, 0] = NAN, INF, -INF
+    for out in (F, *FORMATS):
+        ys = []
+        for t in (x, bad):
+            y, s = (torch.empty(4, 256, device="cuda"), None) if out == F else mx_buffers(4, 256, out)
+            L.ct_norm_run(L.make_norm(4, 256, CODE[dtype], CODE.get(out, out), groups=4), t.cuda(), None, None, None, None, y, s,
+                          stream())
+            ys.append(y.cpu().double() if out == F else values_of(y.cpu(), s.cpu(), 256, out))
+        touched = torch.zeros(4, 4, 64, dtype=torch.bool)
+        touched[1, 1] = touched[2, 3] = touched[3, 0] = True
+        touched = touched.reshape(4, 256)
+        assert torch.equal(ys[0][~touched], ys[1][~touched])
+        if out == F:  # an infinite sum of squares: finite values over it are 0, the infinite one NaN
+            assert torch.isnan(ys[1][1, 64:128]).all() and torch.isnan(ys[1][2, 255]) and (ys[1][2, 192:255] == 0).all()
+        else:
+            assert torch.isnan(ys[1][1, 64:128]).all() and torch.isnan(ys[1][2, 224:]).all()
+
+
+# ------------------------------------------------------------------ attention
+def layout(lens, seed=0, unused=(), lead=0, tail=0, spare=3):
+    """offsets, slots (in no order, -1 for the unused ones), slot count, token rows"""
+    n = len(lens) + spare
+    slots = torch.randperm(n, generator=gen(seed + 1000))[:len(lens)].to(torch.int32)
+    for i in unused:
+        slots[i] = -1
+    off = torch.tensor([lead + sum(lens[:i]) for i in range(len(lens) + 1)], dtype=torch.int32)
+    return off, slots, n, lead + sum(lens) + tail
+
+
+def attention64(s, off, slots, scale, step_input, softplus, dtype):
+    """o, new states and the bounds of both, in 64 bits."""
+    q, k, v = (s[n].double() for n in ("q", "k", "v"))
+    heads, key, value = s["state"].shape[1:]
+    T, groups = q.shape[0], q.shape[1] // key
+    head = torch.arange(heads) // (heads // groups)
+    o, obound = torch.full((T, heads, value), NAN, dtype=D), torch.zeros(T, heads, value, dtype=D)
+    new, nbound = s["state"].double(), torch.zeros(s["state"].shape, dtype=D)
+    for i, slot in enumerate(slots.tolist()):
+        b, e = int(off[i]), int(off[i + 1])
+        has = 0 <= slot < new.shape[0]
+        h = s["state"][slot].double() if has else torch.zeros(heads, key, value, dtype=D)
+        mag, err = h.abs(), torch.zeros_like(h)
+        for t in range(b, e):
+            dt = torch.ones(heads, dtype=D)
+            if s["delta"] is not None:
+                dt = s["delta"][t].double() + s["dt_bias"].double()
+                dt = torch.nn.functional.softplus(dt, threshold=700.0) if softplus else dt
+            l = (dt * s["a"].double()).clamp(max=0)
+            a = torch.exp(l)[:, None, None]
+            # the step within 8 units, its product, the base-2 logarithm and the exponential with it
+            r = (12 * l.abs() + 6)[:, None, None] * U
+            kv = (k[t].reshape(groups, key)[head][:, :, None] * v[t].reshape(heads, value)[:, None, :])
+            kv = kv * dt[:, None, None] if step_input else kv
+            err = a * (err + r * mag) + 12 * U * kv.abs()
+            h, mag = a * h + kv, a * mag + kv.abs()
+            err = err + 2 * U * mag
+            qt = q[t].reshape(groups, key)[head][:, :, None]
+            o[t] = (qt * h).sum(1) * scale
+            # prompts round weights and states to twice the fraction of bf16 before the matrix cores take them
+            prod = (qt.abs() * mag).sum(1) * abs(scale)
+            obound[t] = (qt.abs() * err).sum(1) * abs(scale) + ((key + 70) * U + (2.0 ** -15 if dtype == B else 0.0)) * prod
+        if has:
+            new[slot], nbound[slot] = h, err + 70 * U * mag
+    obound = obound + ROUND[dtype] * (torch.nan_to_num(o).abs() + obound)
+    return o.reshape(T, heads * value), obound.reshape(T, heads * value), new, nbound
+
+
+def attention_inputs(g, tokens, heads, groups, key, value, slots, dtype, delta_dtype, delta=True, strong=False):
+    s = {"q": normal(g, tokens, groups * key, dtype=dtype), "k": normal(g, tokens, groups * key, dtype=dtype),
+         "v": normal(g, tokens, heads * value, dtype=dtype), "state": normal(g, slots, heads, key, value)}
+    if delta:
+        s["delta"] = normal(g, tokens, heads, std=3.0 if strong else 1.0, dtype=delta_dtype)
+        s["dt_bias"] = normal(g, heads, mean=0.0 if strong else -3.0)
+        s["a"] = -torch.exp(normal(g, heads, mean=2.0 if strong else 0.5))
+    else:
+        s["delta"] = s["dt_bias"] = None
+        s["a"] = torch.log1p(-torch.exp2(-2 - 5 * torch.rand(heads, generator=g)))
+    return s
+
+
+def check_attention(lens, heads, groups, key, value, dtype, delta=True, delta_dtype=None, step_input=False, softplus=True,
+                    uniform=False, pad=0, shift=0, in_place=False, unused=(), lead=0, tail=0, seed=0, strong=False, hint=None,
+                    state_in=True, spare=3):
+    what = "attention %s heads%d/%d %dx%d %s delta%d step%d uniform%d pad%d shift%d" % (
+        lens if len(lens) < 12 else len(lens), heads, groups, key, value, dtype, delta, step_input, uniform, pad, shift)
+    note(what)
+    delta_dtype = delta_dtype or dtype
+    off, slots, n, tokens = layout(lens, seed, unused, lead, tail, spare)
+    s = attention_inputs(gen(seed), tokens, heads, groups, key, value, n, dtype, delta_dtype, delta, strong)
+    inside = torch.zeros(tokens, dtype=torch.bool)
+    inside[int(off[0]):int(off[-1])] = True
+    for name in ("q", "k", "v"):
+        s[name][~inside] = NAN
+    if not state_in:
+        s["state"].zero_()
+    scale = key ** -0.5
+    dev = {m: placed(s[m], pad and s[m].shape[1] + pad, shift) for m in ("q", "k", "v")}
+    dd = placed(s["delta"], pad and heads + pad, shift) if delta else None
+    o = placed(torch.full((tokens, heads * value), NAN, dtype=dtype), pad and heads * value + pad, shift, fill=7.0)
+    sd = s["state"].cuda()
+    out = sd if in_place else torch.full_like(sd, 3.0)
+    op = L.make_decay_attention(heads, groups, key, value, CODE[dtype], CODE[delta_dtype], softplus, step_input, scale,
+                                dev["q"].stride(0), dev["k"].stride(0), dev["v"].stride(0), dd.stride(0) if delta else 0,
+                                o.stride(0))
+    most = max(lens + [0])
+    seqs = L.make_sequences(tokens, len(lens), n, most if hint is None else hint, None if uniform else off.cuda(), slots.cuda())
+    need = L.ct_decay_attention_workspace(op, seqs)
+    ws = torch.full((max(16, need),), 255, dtype=torch.uint8, device="cuda")
+    before = sd.clone()
+    L.ct_decay_attention_run(op, seqs, dev["q"], dev["k"], dev["v"], dd, s["dt_bias"].cuda() if delta else None, s["a"].cuda(),
+                             sd if state_in else None, out, o, ws, stream())
+    torch.cuda.synchronize()
+    ref, obound, new, nbound = attention64(s, off, slots, scale, step_input, softplus, dtype)
+    used = torch.zeros(n, dtype=torch.bool)
+    used[[v for v in slots.tolist() if v >= 0]] = True
+    rest = out.cpu()[~used]
+    assert torch.equal(rest, before.cpu()[~used] if in_place else torch.full_like(rest, 3.0)), what + ": other slots"
+    if used.any():
+        within(out[used.cuda()], new[used], nbound[used], what + " state")
+    got = o.cpu()
+    assert torch.isnan(got[~inside]).all(), what + ": rows of no sequence"
+    within(got[inside], ref[inside], obound[inside], what)
+    if pad:
+        c = heads * value
+        assert (o.as_strided((tokens, pad), (c + pad, 1), o.storage_offset() + c) == 7.0).all(), what
+    return need
+
+
+DIMS = [(1, 1), (5, 3), (16, 16), (24, 40), (64, 64), (40, 72), (128, 64), (128, 128), (96, 250), (256, 128), (250, 130), (7, 256)]
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("key,value", DIMS)
+def test_attention_dimensions(key, value, dtype):
+    check_attention([1] * 5, 4, 2, key, value, dtype, uniform=True, seed=key + value, unused=(2,))
+    check_attention([0, 1, 70, 3, 64, 33, 0, 130], 3, 3, key, value, dtype, seed=key, unused=(4,))
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("lens", [[1], [2], [0], [15, 16, 17], [31, 32, 33], [63, 64, 65], [127, 128, 129], [300], [0, 0, 5, 0]])
+def test_attention_lengths(lens, dtype):
+    for hint in (None, 0):
+        check_attention(lens, 2, 1, 32, 48, dtype, seed=sum(lens), hint=hint)
+    check_attention(lens, 2, 2, 64, 32, dtype, delta=False, seed=sum(lens), lead=3, tail=2)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("heads,groups", [(1, 1), (8, 1), (6, 3), (16, 16)])
+def test_attention_heads_that_share_queries_and_keys(heads, groups, dtype):
+    check_attention([40, 1, 90], heads, groups, 32, 32, dtype, seed=heads, step_input=True)
+    check_attention([1] * 9, heads, groups, 32, 32, dtype, seed=heads, step_input=True, uniform=True)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("pad,shift", [(8, 0), (3, 1), (16, 8), (1, 3)])
+def test_attention_strides_and_alignment(pad, shift, dtype):
+    check_attention([70, 0, 1, 100], 4, 2, 40, 24, dtype, pad=pad, shift=shift, seed=pad)
+    check_attention([1] * 6, 4, 2, 40, 24, dtype, pad=pad, shift=shift, uniform=True, seed=pad)
+    check_attention([70, 33], 4, 2, 64, 64, dtype, pad=pad, shift=shift, seed=pad)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+def test_attention_steps(dtype):
+    other = F if dtype == B else B
+    check_attention([90, 7], 4, 4, 32, 32, dtype, delta_dtype=other, seed=1)
+    check_attention([1] * 4, 4, 4, 32, 32, dtype, delta_dtype=other, uniform=True, seed=1)
+    # steps below 0 without the softplus: decays of 1, and inputs with a sign
+    check_attention([90, 7], 4, 4, 32, 32, dtype, delta_dtype=F, softplus=False, step_input=True, seed=2)
+    check_attention([1] * 4, 4, 4, 32, 32, dtype, delta_dtype=F, softplus=False, step_input=True, uniform=True, seed=2)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+def test_attention_strong_and_uneven_decays(dtype):
+    for seed in range(3):
+        check_attention([200, 65], 8, 8, 32, 32, dtype, delta_dtype=F, strong=True, seed=seed)
+        check_attention([1] * 8, 8, 8, 32, 32, dtype, delta_dtype=F, strong=True, uniform=True, seed=seed)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+def test_attention_states_in_place_and_from_zeros(dtype):
+    for lens, uniform in (([40, 3, 0, 2, 129], False), ([1] * 7, True), ([65] * 3, True)):
+        check_attention(lens, 2, 2, 64, 64, dtype, in_place=True, uniform=uniform, seed=3)
+        check_attention(lens, 2, 2, 64, 64, dtype, state_in=False, uniform=uniform, seed=4)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+def test_attention_of_many_sequences(dtype):
+    lens = [int(v) for v in torch.randint(0, 6, (700,), generator=gen(5))]
+    check_attention(lens, 2, 1, 8, 8, dtype, seed=8, unused=tuple(range(0, 700, 7)), lead=5, tail=11)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+def test_attention_of_one_long_prompt(dtype):
+    check_attention([2500], 2, 1, 32, 32, dtype, seed=1)
+    check_attention([1100, 0, 1500], 2, 2, 64, 64, dtype, seed=2, unused=(0,))
+    check_attention([1200, 1300], 1, 1, 128, 40, dtype, delta=False, seed=3, hint=0)
+
+
+def run_plain(s, lens, heads, groups, key, value, dtype, state=None, hint=None):
+    off = torch.tensor([sum(lens[:i]) for i in range(len(lens) + 1)], dtype=torch.int32).cuda()
+    op = L.make_decay_attention(heads, groups, key, value, CODE[dtype], L.DT_F32, scale=1.0)
+    seqs = L.make_sequences(sum(lens), len(lens), len(lens), max(lens) if hint is None else hint, off)
+    ws = torch.full((max(16, L.ct_decay_attention_workspace(op, seqs)),), 255, dtype=torch.uint8, device="cuda")
+    o = torch.empty(sum(lens), heads * value, dtype=dtype, device="cuda")
+    out = torch.empty(len(lens), heads, key, value, device="cuda")
+    t = {n: s[n].cuda() for n in ("q", "k", "v", "delta", "dt_bias", "a")}
+    L.ct_decay_attention_run(op, seqs, t["q"], t["k"], t["v"], t["delta"], t["dt_bias"], t["a"],
+                             None if state is None else state.cuda(), out, o, ws, stream())
+    torch.cuda.synchronize()
+    return o.cpu().double(), out.cpu().double()
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("name,bad", [("v", NAN), ("v", INF), ("k", NAN), ("k", -INF), ("q", NAN), ("delta", NAN)])
+def test_attention_keeps_infinities_and_nan_behind_their_token(name, bad, dtype):
+    """Nothing of a token reaches those before it, other heads or other sequences."""
+    heads, key, value, lens = 3, 32, 40, [70, 150, 40]
+    s = attention_inputs(gen(4), sum(lens), heads, heads, key, value, 3, dtype, F)
+    state = s["state"]
+    clean, cs = run_plain(s, lens, heads, heads, key, value, dtype, state)
+    for t in (70, 75, 133, 134, 219):  # of the second sequence: its first, one early, at a tile's end, its last
+        d = {k: v.clone() if v is not None else None for k, v in s.items()}
+        col = {"v": value, "delta": 1}.get(name, key) + {"v": 7, "delta": 0}.get(name, 5)
+        d[name][t, col] = bad  # of the second head
+        got, gs = run_plain(d, lens, heads, heads, key, value, dtype, state)
+        reached = torch.zeros(sum(lens), heads, value, dtype=torch.bool)
+        rstate = torch.zeros(3, heads, key, value, dtype=torch.bool)
+        if name == "q":
+            reached[t, 1] = True
+        else:
+            reached[t:220, 1] = True
+            rstate[1, 1] = True
+            if name == "v":
+                reached[:] = False
+                reached[t:220, 1, 7] = True
+                rstate[:] = False
+                rstate[1, 1, :, 7] = True
+            if name == "k":
+                rstate[:] = False
+                rstate[1, 1, 5] = True
+        flat = reached.reshape(sum(lens), -1)
+        assert torch.equal(got[~flat], clean[~flat]) and torch.equal(gs[~rstate], cs[~rstate]), (name, bad, t)
+        assert not torch.isfinite(got[flat]).any() and not torch.isfinite(gs[rstate]).any(), (name, bad, t)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+def test_attention_an_infinite_rate_forgets_everything_before(dtype):
+    heads, key, value, lens = 2, 32, 32, [100]
+    s = attention_inputs(gen(6), 100, heads, heads, key, value, 1, dtype, F)
+    s["delta"][[0, 37, 64, 65], 1] = INF  # a decay of exp(-inf) = 0
+    o, st = run_plain(s, lens, heads, heads, key, value, dtype, s["state"])
+    ref, bound, new, nbound = attention64({**s, "delta": s["delta"].clamp(max=1e4)}, torch.tensor([0, 100]), torch.tensor([0]), 1.0,
+                                          False, True, dtype)
+    within(o, ref, bound, "forgetting")
+    within(st, new, nbound, "forgetting: state")
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+def test_attention_repeats_its_bits_and_a_split_prompt_goes_on(dtype):
+    heads, key, value = 4, 64, 64
+    s = attention_inputs(gen(7), 600, heads, heads, key, value, 1, dtype, F)
+    a = run_plain(s, [600], heads, heads, key, value, dtype, s["state"])
+    for _ in range(3):
+        b = run_plain(s, [600], heads, heads, key, value, dtype, s["state"])
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+    first = {k: v[:301] if v is not None and k in ("q", "k", "v", "delta") else v for k, v in s.items()}
+    second = {k: v[301:] if v is not None and k in ("q", "k", "v", "delta") else v for k, v in s.items()}
+    o1, s1 = run_plain(first, [301], heads, heads, key, value, dtype, s["state"])
+    o2, s2 = run_plain(second, [299], heads, heads, key, value, dtype, s1.float())
+    _, bound, _, nbound = attention64(s, torch.tensor([0, 600]), torch.tensor([0]), 1.0, False, True, dtype)
+    within(torch.cat([o1, o2]), a[0], 2 * bound, "a prompt in two calls")
+    within(s2, a[1], 2 * nbound, "a prompt in two calls: state")
+
+
+# ------------------------------------------------------------------ streams, graphs, offsets
+def calls(seed, dtype=B):
+    """One call of each operator with its outputs and fresh inputs: [(call(stream), outputs)]."""
+    g = gen(seed)
+    out = []
+    x, z = normal(g, 70, 256, dtype=dtype).cuda(), normal(g, 70, 256, dtype=dtype).cuda()
+    q, sc = mx_buffers(70, 256, L.MX_E4M3)
+    norm = L.make_norm(70, 256, CODE[dtype], L.MX_E4M3)
+    total = torch.empty_like(x)
+    out.append((lambda st: L.ct_norm_run(norm, x, z, total, None, z, q, sc, st), [q, sc, total]))
+    w = normal(g, 96, 256, dtype=dtype).cuda()
+    wq, wsc = mx_buffers(96, 256, L.MX_E2M1)
+    mx = L.make_mx(96, 256, CODE[dtype], L.MX_E2M1)
+    out.append((lambda st: L.ct_mx_quantise_run(mx, w, wq, wsc, st), [wq, wsc]))
+    y = torch.empty(70, 96, dtype=B, device="cuda")
+    lin = L.make_mx_linear(70, 96, 256, L.MX_E4M3, L.MX_E2M1, L.DT_BF16)
+    out.append((lambda st: L.ct_mx_linear_run(lin, q, sc, wq, wsc, None, None, y, None, st), [y]))
+    back = torch.empty_like(w)
+    out.append((lambda st: L.ct_mx_values_run(mx, wq, wsc, back, st), [back]))
+    s = attention_inputs(g, 1500, 2, 2, 64, 64, 1, dtype, F)
+    t = {k: v.cuda() for k, v in s.items()}
+    op = L.make_decay_attention(2, 2, 64, 64, CODE[dtype], L.DT_F32)
+    seqs = L.make_sequences(1500, 1, 1)
+    ws = torch.empty(max(16, L.ct_decay_attention_workspace(op, seqs)), dtype=torch.uint8, device="cuda")
+    o, state = torch.empty_like(t["v"]), torch.empty_like(t["state"])
+    out.append((lambda st: L.ct_decay_attention_run(op, seqs, t["q"], t["k"], t["v"], t["delta"], t["dt_bias"], t["a"],
+                                                    t["state"], state, o, ws, st), [o, state]))
+    tok = L.make_decay_attention(2, 2, 64, 64, CODE[dtype], L.DT_F32)
+    one = L.make_sequences(1, 1, 1, 1)
+    o1, state1 = torch.empty(1, 128, dtype=dtype, device="cuda"), torch.empty_like(t["state"])
+    out.append((lambda st: L.ct_decay_attention_run(tok, one, t["q"], t["k"], t["v"], t["delta"], t["dt_bias"], t["a"],
+                                                    state, state1, o1, None, st), [o1, state1]))
+    return out
+
+
+def test_calls_on_other_streams_and_from_graphs_give_the_same_bits():
+    sets = [calls(1), calls(2, F)]
+    note("operators on streams and in graphs")
+    want = []
+    for cs in sets:
+        for c, _ in cs:
+            c(stream())
+        torch.cuda.synchronize()
+        want.append([t.clone() for _, outs in cs for t in outs])
+
+    def scrub():
+        for cs in sets:
+            for _, outs in cs:
+                for t in outs:
+                    t.zero_()
+        torch.cuda.synchronize()
+
+    def same():
+        torch.cuda.synchronize()
+        for cs, w in zip(sets, want):
+            for t, r in zip([t for _, outs in cs for t in outs], w):
+                assert torch.equal(t, r)
+
+    scrub()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for cs, st in zip(sets, streams):
+        for c, _ in cs:
+            c(st.cuda_stream)
+    same()
+    graphs = []
+    for cs in sets:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            for c, _ in cs:
+                c(stream())
+        graphs.append(graph)
+    for i in range(4):
+        scrub()
+        for graph, st in zip(graphs, streams):
+            with torch.cuda.stream(st if i % 2 else torch.cuda.current_stream()):
+                graph.replay()
+        same()
+        torch.randn(1000, device="cuda").sum().item()
+
+
+def test_offsets_past_32_bits():
+    """Rows so far apart that the last ones lie past 2^31 elements, and past 2^32 bytes."""
+    rows, pitch = 2100, 1 << 20
+    flat = torch.zeros(rows * pitch + 4096, dtype=B, device="cuda")
+    x = flat[:rows * pitch].view(rows, pitch)
+    g = gen(1)
+    v = normal(g, rows, 64, dtype=B)
+    x[:, :64] = v.cuda()
+    note("norm and quantise of rows past 2^31 elements")
+    y = torch.empty(rows, 64, dtype=B, device="cuda")
+    L.ct_norm_run(L.make_norm(rows, 64, L.DT_BF16, L.DT_BF16, ldx=pitch), x, None, None, None, None, y, None, stream())
+    z = torch.empty_like(y)
+    L.ct_norm_run(L.make_norm(rows, 64, L.DT_BF16, L.DT_BF16), v.cuda(), None, None, None, None, z, None, stream())
+    assert torch.equal(y, z)
+    q, s = mx_buffers(rows, 64, L.MX_E4M3)
+    q2, s2 = mx_buffers(rows, 64, L.MX_E4M3)
+    L.ct_mx_quantise_run(L.make_mx(rows, 64, L.DT_BF16, L.MX_E4M3, ldx=pitch), x, q, s, stream())
+    L.ct_mx_quantise_run(L.make_mx(rows, 64, L.DT_BF16, L.MX_E4M3), v.cuda(), q2, s2, stream())
+    assert torch.equal(q, q2) and torch.equal(s, s2)
+    note("attention over rows past 2^31 elements")
+    for lens in ([rows], [1] * rows):
+        key = value = 16
+        outs = []
+        for t, p in ((x, pitch), (v.cuda(), 64)):
+            op = L.make_decay_attention(1, 1, key, value, L.DT_BF16, scale=1.0, softplus=True, ldq=p, ldk=p, ldv=p, lddelta=p)
+            seqs = L.make_sequences(rows, len(lens), len(lens), max(lens))
+            ws = torch.empty(max(16, L.ct_decay_attention_workspace(op, seqs)), dtype=torch.uint8, device="cuda")
+            o, st = torch.empty(rows, value, dtype=B, device="cuda"), torch.empty(len(lens), 1, key, value, device="cuda")
+            L.ct_decay_attention_run(op, seqs, t, t[:, 16:], t[:, 32:], t[:, 48:], None, -torch.ones(1, device="cuda"), None, st,
+                                     o, ws, stream())
+            outs.append((o, st))
+        assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
