@@ -6,6 +6,9 @@
 
 namespace ct {
 
+// Sequences of at most this many tokens go token by token.
+constexpr int kDecayStepTokens = 4;
+
 struct DecayArgs {
   const void *q, *k, *v, *delta;
   const float *dt_bias, *a, *state_in;
@@ -18,24 +21,34 @@ struct DecayArgs {
   float scale;
   int64_t ldq, ldk, ldv, lddelta, ldo;
   FastDiv dheads, dper;  // by heads, by heads to a group
+  // pieces of a sequence (0 tokens: whole sequences): their numbering, what each leaves to the next
+  int piece, per;
+  f32x4* ends;    // pieces x heads x frames
+  float* decays;  // pieces x heads
+  int frames;     // quads of a state in the order of the matrix cores' results
 };
 
-// Step and log2 of the decay of a head at a token. A step or rate that is NaN stays one; below
-// 2^-150 the decay is 0 in fp32, and a sum of many such logarithms would lose the small ones.
+// Step and logarithm of the decay of a head at a token. A step or rate that is NaN stays one; below
+// e^-104 the decay is 0 in fp32, and a sum of many such logarithms would lose the small ones.
 struct Step {
   float dt, l;
 };
-__device__ __forceinline__ Step step_of(const DecayArgs& a, int row, int head, float bias, float rate) {
+// What `delta` holds for a token (0 without): asked for early, looked at late.
+__device__ __forceinline__ float delta_of(const DecayArgs& a, int row, int head) {
+  if (!a.delta) return 0.f;
+  const int64_t at = row * a.lddelta + head;
+  return a.delta_bf16 ? (float)((const bf16_t*)a.delta)[at] : ((const float*)a.delta)[at];
+}
+__device__ __forceinline__ Step step_of(const DecayArgs& a, float delta, float bias, float rate) {
   float dt = 1.f;
   if (a.delta) {
-    const int64_t at = row * a.lddelta + head;
-    dt = (a.delta_bf16 ? (float)((const bf16_t*)a.delta)[at] : ((const float*)a.delta)[at]) + bias;
+    dt = delta + bias;
     if (a.softplus) dt = softplus_f32(dt);
   }
   float l = dt * rate;
   l = l > 0.f ? 0.f : l;
   l = l < -104.f ? -104.f : l;
-  return {dt, l * kLog2e};
+  return {dt, l};
 }
 
 // ------------------------------------------------------------------ token by token
@@ -75,7 +88,7 @@ __global__ void __launch_bounds__(256) decay_step_kernel(DecayArgs a) {
       now[0][tid] = (float)((const T*)a.q)[t * a.ldq + (int64_t)group * a.key + tid];
       now[1][tid] = (float)((const T*)a.k)[t * a.ldk + (int64_t)group * a.key + tid];
     }
-    const Step step = step_of(a, t, head, bias, rate);
+    const Step step = step_of(a, delta_of(a, t, head), bias, rate);
     f32x4 v = {};
     const T* vp = (const T*)a.v + t * a.ldv + (int64_t)head * a.value + c0;
     if (left >= 4) {
@@ -87,7 +100,7 @@ __global__ void __launch_bounds__(256) decay_step_kernel(DecayArgs a) {
         if (e < left) v[e] = (float)vp[e];
     }
     if (a.step_input) v *= step.dt;
-    const float decay = __builtin_amdgcn_exp2f(step.l);
+    const float decay = __builtin_amdgcn_exp2f(step.l * kLog2e);
     __syncthreads();  // q and k are there, and the sums of the token before have been read
     f32x4 acc = {};
 #pragma unroll
@@ -149,9 +162,545 @@ static int decay_step(const DecayArgs& a, hipStream_t st) {
                        : decay_step_rows<T, 32>(a, grid, st);
 }
 
-DecayPlan plan_decay(const ct_decay_attention_op&, const ct_sequences&) { return {}; }
+// ------------------------------------------------------------------ chunks of a prompt
+// With G_i the sum of l over the tokens of a chunk up to i, and S the state before it,
+//   o_i = e^{G_i} q_i S + sum_{j <= i} e^{G_i - G_j} (q_i k_j) dt_j v_j,
+//   S'  = e^{G_C} S + sum_j k_j^T e^{G_C - G_j} dt_j v_j.
+// A block takes a head of a sequence, or of a piece of one, and up to 64 NC columns of v, chunk by
+// chunk. Its four waves have 16 NC columns each: their part of the state stays in the matrix
+// cores' accumulators, whose layout is also that of an operand, so the state goes through no
+// memory. Operands in rows are read from LDS as they lie there, those in columns transposed.
+//
+// Precision. In bf16 the inputs are exact, and what is computed from them is taken apart into bf16
+// terms before it meets a matrix core: the state (for o) and the weights q k e^{..} into two, 2^-17
+// of each, below the output's rounding; the weighted v, which the fp32 state is summed from, into
+// three, 2^-25. fp32 takes fp32 products. G is summed in fp64 and kept as two fp32, so that weak
+// decays keep their digits behind strong ones.
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
 
-int launch_decay(const ct_decay_attention_op& op, const DecayPlan&, const SeqView& s, const DecayArrays& v, int,
+template <typename T>
+struct Mat;
+template <>
+struct Mat<bf16_t> {
+  typedef bf16x8 Frag;  // row or column lane % 16, steps 8 (lane / 16) on, of 32
+  static constexpr int CHUNK = 64, KS = 32, STATE_TERMS = 2, P_TERMS = 2, V_TERMS = 3;
+  static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Mat<float> {
+  typedef f32x4 Frag;  // row or column lane % 16, steps 4 (lane / 16) on, of 16
+  static constexpr int CHUNK = 32, KS = 16, STATE_TERMS = 1, P_TERMS = 1, V_TERMS = 1;
+  static __device__ __forceinline__ f32x4 mma(Frag a, Frag b, f32x4 c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float x = a[e], y = b[e];
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(x, y, c, 0, 0, 0);
+    }
+    return c;
+  }
+};
+// Eight values as TERMS fragments whose sum they are, but for what the last one drops.
+template <int TERMS>
+__device__ __forceinline__ void split8(float (&v)[8], bf16x8 (&f)[TERMS]) {
+#pragma unroll
+  for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      f[t][i] = (__bf16)v[i];
+      v[i] -= (float)f[t][i];
+    }
+}
+
+// A tile in LDS: rows of BYTES, their 16-byte groups permuted by the row's number so that eight
+// rows' groups, and the halves of four rows, lie in distinct banks.
+template <int BYTES>
+__device__ __forceinline__ int tile_at(int row, int group) {
+  const int key = ((row & 3) << 1 | (row >> 2 & 1)) & (BYTES / 16 - 1);
+  return row * BYTES + (group ^ key) * 16;
+}
+// Row r0 + lane % 16, steps of number k.
+template <typename T, int BYTES>
+__device__ __forceinline__ typename Mat<T>::Frag read_rows(const char* tile, int r0, int k) {
+  const int lane = (int)threadIdx.x & 63;
+  return *(const typename Mat<T>::Frag*)(tile + tile_at<BYTES>(r0 + (lane & 15), k * 4 + (lane >> 4)));
+}
+// Column of lane % 16, steps (rows) of number k: fp32 column c0 + lane % 16, bf16 the lane's of four
+// runs of four columns, `run` columns apart.
+template <typename T, int BYTES>
+__device__ __forceinline__ typename Mat<T>::Frag read_cols(const char* tile, int k, int c0, int run) {
+  const int lane = (int)threadIdx.x & 63, g = lane >> 4, l = lane & 15;
+  if constexpr (sizeof(T) == 2) {
+    typedef i16x4 __attribute__((address_space(3))) * lds_i16x4;
+    i16x4 part[2];
+    const int col = c0 + (l & 3) * run;  // this lane's run for the transposed read, of row l / 4
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const char* p = tile + tile_at<BYTES>(k * 32 + g * 8 + h * 4 + (l >> 2), col / 8) + (col & 4) * 2;
+      part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(__attribute__((address_space(3))) char*)p);
+    }
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+  } else {
+    const int col = c0 + l;
+    f32x4 f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f[e] = *(const float*)(tile + tile_at<BYTES>(k * 16 + g * 4 + e, col / 4) + (col & 3) * 4);
+    return f;
+  }
+}
+
+// ROWS rows of a tile of BYTES each from memory, 16 bytes a lane straight into LDS where the rows
+// lie on 16 bytes (wait_copies() and a barrier before they are read), else element by element
+// through registers. Elements past `cols` and rows past `rows` read 0.
+template <typename T, int BYTES, int ROWS, bool ALIGNED>
+__device__ __forceinline__ void fill_tile(char* tile, const T* base, int64_t ld, int rows, int cols) {
+  constexpr int GROUPS = BYTES / 16, N = ROWS * GROUPS / 256, E = 16 / (int)sizeof(T);
+  static_assert(ROWS * GROUPS % 256 == 0, "");
+  const __amdgpu_buffer_rsrc_t r = make_rsrc(base, rows > 0 ? ((rows - 1) * ld + cols) * (int64_t)sizeof(T) : 0);
+  // Where a thread's group i is from: whose place its slot is (the permutation is its own inverse)
+  const auto offset = [&](int i, int* col) {
+    const int at = i * 256 + (int)threadIdx.x, row = at / GROUPS;
+    *col = (tile_at<BYTES>(row, at % GROUPS) - row * BYTES) / 16 * E;
+    if (row >= rows) *col = cols;
+    return (unsigned)(row * (int)ld + *col) * (unsigned)sizeof(T);
+  };
+  if constexpr (ALIGNED) {
+    char* mine = tile + wave_id() * 1024;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int col;
+      const unsigned off = offset(i, &col);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)(mine + i * 4096), 16, (int)(col < cols ? off : kOobGroup), 0, 0, 0);
+    }
+  } else {
+#pragma unroll 1
+    for (int i = 0; i < N; ++i) {
+      int col;
+      const unsigned off = offset(i, &col);
+      unsigned w[4] = {};
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const int o = (int)(col + e < cols ? off + e * (unsigned)sizeof(T) : kOobGroup);
+        if constexpr (sizeof(T) == 2) w[e / 2] |= (unsigned)__builtin_amdgcn_raw_buffer_load_b16(r, o, 0, 0) << (16 * (e & 1));
+        else w[e] = __builtin_amdgcn_raw_buffer_load_b32(r, o, 0, 0);
+      }
+      *(u32x4*)(tile + (i * 256 + (int)threadIdx.x) * 16) = (u32x4){w[0], w[1], w[2], w[3]};
+    }
+  }
+}
+
+// What the tokens of a chunk carry: G in two parts, e^G, the weights of the state's sum and the
+// steps (1 where they do not scale the input).
+template <int C>
+struct Steps {
+  float hi[C], lo[C], grown[C], weight[C], dt[C];
+  float end;  // e^{G_C}
+};
+
+// Whether one of a lane's values is infinite or NaN.
+template <typename F, int N>
+__device__ __forceinline__ bool any_wild(const F& f) {
+  bool any = false;
+#pragma unroll
+  for (int e = 0; e < N; ++e) any |= !(__builtin_fabsf((float)f[e]) < __builtin_inff());
+  return any;
+}
+
+template <typename T, int DK, int NC, bool OUT, bool ALIGNED>
+__global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 ? 1 : 2) decay_tile_kernel(DecayArgs a) {
+  typedef Mat<T> M;
+  typedef typename M::Frag Frag;
+  constexpr int C = M::CHUNK, KS = M::KS, IT = C / 16, DT = DK / 16, DKS = DK / KS, CKS = C / KS;
+  constexpr int DV = 64 * NC, KB = DK * (int)sizeof(T), VB = DV * (int)sizeof(T), PB = C * (int)sizeof(T);
+  constexpr int AT_K = OUT ? C * KB : 0, AT_V = AT_K + C * KB, AT_P = AT_V + C * VB;
+  extern __shared__ __align__(16) char lds[];
+  __shared__ Steps<C> steps[2];
+  const int lane = (int)threadIdx.x & 63, wave = wave_id(), g = lane >> 4, l16 = lane & 15;
+  char *tq = lds, *tk = lds + AT_K, *tv = lds + AT_V, *tp = lds + AT_P;
+
+  const int unit = fdiv((int)blockIdx.x, a.dheads), head = (int)blockIdx.x - unit * a.heads;
+  int begin, end;
+  SeqRange r;
+  if (a.piece) {
+    r = find_tile(a.seqs, a.per, a.piece, unit, &begin);
+    if (r.s < 0 || (begin >= r.end && r.end > r.begin)) return;  // a number that no piece has
+    end = tile_end(begin, r.end, a.piece);
+  } else {
+    r = seq_range(a.seqs, unit);
+    begin = r.begin;
+    end = r.end;
+  }
+  const bool first = begin == r.begin, last = end == r.end;
+  if (!OUT && last) return;  // nothing comes after it
+  const int slot = seq_slot(a.seqs, r.s), group = fdiv(head, a.dper);
+  const int c0 = (int)blockIdx.y * DV, cw = c0 + wave * 16 * NC;  // the block's columns, the wave's
+  const int cols = min(a.value - c0, DV);
+  const float bias = a.dt_bias ? a.dt_bias[head] : 0.f, rate = a.a[head];
+  const T* q = (const T*)a.q + (int64_t)group * a.key;
+  const T* k = (const T*)a.k + (int64_t)group * a.key;
+  const T* v = (const T*)a.v + (int64_t)head * a.value + c0;
+
+  const auto fill_q = [&](int t) __attribute__((always_inline)) {
+    fill_tile<T, KB, C, ALIGNED>(tq, q + t * a.ldq, a.ldq, min(end - t, C), a.key);
+  };
+  const auto fill_kv = [&](int t) __attribute__((always_inline)) {
+    fill_tile<T, KB, C, ALIGNED>(tk, k + t * a.ldk, a.ldk, min(end - t, C), a.key);
+    fill_tile<T, VB, C, ALIGNED>(tv, v + t * a.ldv, a.ldv, min(end - t, C), cols);
+  };
+  if (begin < end) {
+    if constexpr (OUT) fill_q(begin);
+    fill_kv(begin);
+  }
+
+  // The state: element e of S[t][c] is row row0 + row_of(t) + e, column cw + 16 c + l16, of a buffer
+  // that ends with its last row; columns past the last have an offset past it.
+  const int row0 = sizeof(T) == 2 ? g * 8 : g * 4;
+  const auto row_of = [](int t) { return sizeof(T) == 2 ? t / 2 * 32 + (t & 1) * 4 : t * 16; };
+  const int64_t state_at = ((int64_t)slot * a.heads + head) * a.key * a.value;
+  const unsigned state_bytes = (unsigned)(a.key * a.value) * 4;
+  unsigned state_off[NC];
+#pragma unroll
+  for (int c = 0; c < NC; ++c) {
+    const int col = cw + 16 * c + l16;
+    state_off[c] = col < a.value ? (unsigned)(row0 * a.value + col) * 4 : kOobGroup;
+  }
+  f32x4* frames = a.ends + ((int64_t)unit * a.heads + head) * a.frames + (((int)blockIdx.y * 4 + wave) * NC * DT) * 64 + lane;
+  f32x4 S[DT][NC];
+  if (OUT && !first) {
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) S[t][c] = frames[(t * NC + c) * 64];
+  } else {
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.state_in + state_at, first && slot >= 0 && a.state_in ? state_bytes : 0);
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          S[t][c][e] = load_elem<float>(rs, state_off[c] == kOobGroup ? kOobGroup : state_off[c] + (unsigned)((row_of(t) + e) * a.value) * 4, 0);
+  }
+
+  double total = 0;
+  // Wave 0: what `delta` holds for the chunk at t, a token to a lane, and the chunk's steps from it
+  const auto ask = [&](int t) { return lane < C && t + lane < end ? delta_of(a, t + lane, head) : 0.f; };
+  const auto make_steps = [&](int t, float delta, Steps<C>& to) __attribute__((always_inline)) {
+    const Step s = step_of(a, delta, bias, rate);
+    double G = lane < C && t + lane < end ? (double)s.l * 1.4426950408889634 : 0.;
+#pragma unroll
+    for (int o = 1; o < C; o <<= 1) {
+      const double up = __shfl_up(G, o);
+      if (lane >= o) G += up;
+    }
+    const double all = __shfl(G, C - 1);
+    if (lane < C) {
+      const float dt = a.step_input && t + lane < end ? s.dt : 1.f;
+      to.hi[lane] = (float)G;
+      to.lo[lane] = (float)(G - (double)(float)G);
+      to.grown[lane] = __builtin_amdgcn_exp2f((float)G);
+      to.weight[lane] = __builtin_amdgcn_exp2f((float)(all - G)) * dt;
+      to.dt[lane] = dt;
+      if (lane == 0) to.end = __builtin_amdgcn_exp2f((float)all);
+    }
+    total += all;
+  };
+  if (wave == 0 && begin < end) make_steps(begin, ask(begin), steps[0]);
+
+  int turn = 0;
+#pragma unroll 1
+  for (int t = begin; t < end; turn ^= 1) {
+    const Steps<C>& st = steps[turn];
+    const int next = tile_end(t, end, C);
+    wait_copies();
+    __syncthreads();
+    float delta = 0;
+    if (wave == 0 && next < end) delta = ask(next);
+
+    f32x4 O[IT][NC];
+    if constexpr (OUT) {
+      // Weights of tokens i = 16 wave + l16 (a wave to 16 of them), j = 16 jt + 4 g + e
+      if (wave < IT) {
+        f32x4 p[IT] = {};
+#pragma unroll
+        for (int s = 0; s < DKS; ++s) {
+          const Frag fq = read_rows<T, KB>(tq, wave * 16, s);
+#pragma unroll
+          for (int jt = 0; jt < IT; ++jt) p[jt] = M::mma(read_rows<T, KB>(tk, jt * 16, s), fq, p[jt]);
+        }
+        const int i = wave * 16 + l16;
+        const float hi = st.hi[i], lo = st.lo[i];
+#pragma unroll
+        for (int jt = 0; jt < IT; ++jt) {
+          const f32x4 hj = *(const f32x4*)&st.hi[jt * 16 + g * 4], lj = *(const f32x4*)&st.lo[jt * 16 + g * 4];
+          const f32x4 dj = *(const f32x4*)&st.dt[jt * 16 + g * 4];
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float w = __builtin_amdgcn_exp2f((hi - hj[e]) + (lo - lj[e])) * dj[e];
+            x[e] = jt * 16 + g * 4 + e <= i ? p[jt][e] * w : 0.f;
+          }
+          if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int n = 0; n < M::P_TERMS; ++n) {
+              const unsigned w0 = pack_bf16(x[0], x[1]), w1 = pack_bf16(x[2], x[3]);
+              *(u32x2*)(tp + n * C * PB + tile_at<PB>(i, jt * 2 + g / 2) + (g & 1) * 8) = (u32x2){w0, w1};
+              x[0] -= unpack<T>(w0, 0);
+              x[1] -= unpack<T>(w0, 1);
+              x[2] -= unpack<T>(w1, 0);
+              x[3] -= unpack<T>(w1, 1);
+            }
+          } else {
+            *(f32x4*)(tp + tile_at<PB>(i, jt * 4 + g)) = (f32x4){x[0], x[1], x[2], x[3]};
+          }
+        }
+      }
+      // What the state before the chunk gives: columns of the wave, all tokens
+#pragma unroll
+      for (int i = 0; i < IT; ++i)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) O[i][c] = f32x4{};
+#pragma unroll
+      for (int s = 0; s < DKS; ++s) {
+        Frag fs[NC][M::STATE_TERMS];
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          if constexpr (sizeof(T) == 2) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = S[2 * s + e / 4][c][e % 4];
+            split8(x, fs[c]);
+          } else {
+            fs[c][0] = S[s][c];
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < IT; ++i) {
+          const Frag fq = read_rows<T, KB>(tq, i * 16, s);
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int n = 0; n < M::STATE_TERMS; ++n) O[i][c] = M::mma(fs[c][n], fq, O[i][c]);
+        }
+        asm volatile("" ::: "memory");  // one step's operands at a time
+      }
+#pragma unroll
+      for (int i = 0; i < IT; ++i) {
+        const float grown = st.grown[i * 16 + l16];
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) O[i][c][e] *= grown;
+      }
+    }
+    if (wave == 0 && next < end) make_steps(next, delta, steps[turn ^ 1]);
+    if constexpr (OUT) {
+      __syncthreads();
+      if (next < end) fill_q(next);  // q has been read
+    }
+
+    // Tokens of the chunk: to the outputs behind them, and to the state
+    const float decay = st.end;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) S[d][c][e] *= decay;
+    bool odd = false;
+#pragma unroll
+    for (int s = 0; s < CKS; ++s) {
+      constexpr int E = KS / 4;
+      Frag fv[NC], fw[NC][M::V_TERMS];
+#pragma unroll
+      for (int c = 0; c < NC; ++c) {
+        fv[c] = read_cols<T, VB>(tv, s, wave * 16 * NC + 16 * c, 4);
+        float x[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = (float)fv[c][e] * st.weight[s * KS + g * E + e];
+        if constexpr (sizeof(T) == 2) split8(x, fw[c]);
+        else fw[c][0] = (f32x4){x[0], x[1], x[2], x[3]};
+        // What is infinite or NaN is added by itself, to the tokens from its own on: a product with
+        // the weight 0 of an earlier one would be NaN
+        if (OUT && __ballot(any_wild<Frag, E>(fv[c]))) {
+          odd = true;
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if (!(__builtin_fabsf((float)fv[c][e]) < __builtin_inff())) fv[c][e] = 0;
+        }
+      }
+      if constexpr (OUT) {
+#pragma unroll
+        for (int i = s * KS / 16; i < IT; ++i) {
+#pragma unroll
+          for (int n = 0; n < M::P_TERMS; ++n) {
+            const Frag fp = read_rows<T, PB>(tp + n * C * PB, i * 16, s);
+#pragma unroll
+            for (int c = 0; c < NC; ++c) O[i][c] = M::mma(fv[c], fp, O[i][c]);
+          }
+        }
+        asm volatile("" ::: "memory");
+      }
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const Frag fk = sizeof(T) == 2 ? read_cols<T, KB>(tk, s, d / 2 * 32 + (d & 1) * 4, 8) : read_cols<T, KB>(tk, s, d * 16, 4);
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int n = 0; n < M::V_TERMS; ++n) S[d][c] = M::mma(fk, fw[c][n], S[d][c]);
+        if (d % 2) asm volatile("" ::: "memory");
+      }
+    }
+    if constexpr (OUT) {
+      if (odd) {
+#pragma unroll
+        for (int i = 0; i < IT; ++i)
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll 1
+            for (int j = 0; j <= i * 16 + l16; ++j) {
+              const int row = i * 16 + l16;
+              float p = 0;
+#pragma unroll
+              for (int n = 0; n < M::P_TERMS; ++n)
+                p += (float)*(const T*)(tp + n * C * PB + tile_at<PB>(row, j * (int)sizeof(T) / 16) + j * (int)sizeof(T) % 16);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int col = (wave * NC + c) * 16 + g * 4 + e;
+                const float x = (float)*(const T*)(tv + tile_at<VB>(j, col * (int)sizeof(T) / 16) + col * (int)sizeof(T) % 16);
+                if (!(__builtin_fabsf(x) < __builtin_inff())) O[i][c][e] += p * x;
+              }
+            }
+      }
+#pragma unroll
+      for (int i = 0; i < IT; ++i) {
+        const int row = t + i * 16 + l16;
+        if (row >= end) continue;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+          const int col = cw + 16 * c + g * 4;
+          T* p = (T*)a.o + row * a.ldo + (int64_t)head * a.value + col;
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = O[i][c][e] * a.scale;
+          if (col + 4 <= a.value) store_quad4(p, x, false);
+          else
+#pragma unroll
+            for (int e = 0; e < 3; ++e)
+              if (col + e < a.value) p[e] = from_f32<T>(x[e]);
+        }
+      }
+    }
+    __syncthreads();
+    if (next < end) fill_kv(next);  // k and v have been read
+    t = next;
+  }
+
+  if constexpr (!OUT) {
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) frames[(t * NC + c) * 64] = S[t][c];
+    if (threadIdx.x == 0 && blockIdx.y == 0)
+      a.decays[(int64_t)unit * a.heads + head] = __builtin_amdgcn_exp2f((float)total);
+  } else if (last && slot >= 0 && a.state_out) {
+    const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.state_out + state_at, state_bytes);
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          store_elem<float>(rs, state_off[c] == kOobGroup ? kOobGroup : state_off[c] + (unsigned)((row_of(t) + e) * a.value) * 4, 0, S[t][c][e]);
+  }
+}
+
+// Every piece's state at its end, from zeros (a sequence's first: from its own state), to the state
+// before each piece but the first.
+__global__ void __launch_bounds__(256) decay_join_kernel(DecayArgs a) {
+  const int s = fdiv((int)blockIdx.x, a.dheads), head = (int)blockIdx.x - s * a.heads;
+  const int at = (int)blockIdx.y * 256 + (int)threadIdx.x;
+  const SeqRange r = seq_range(a.seqs, s);
+  const int pieces = tiles_in(r.end - r.begin, a.piece);
+  const int64_t unit = a.seqs.offsets ? r.begin / a.piece + (int64_t)s : (int64_t)s * a.per;
+  if (at >= a.frames || pieces < 2) return;
+  const int64_t step = (int64_t)a.heads * a.frames;
+  f32x4* p = a.ends + (unit * a.heads + head) * a.frames + at;
+  f32x4 run = *p, held = pieces > 2 ? p[step] : f32x4{};
+  for (int i = 1; i < pieces; ++i) {
+    const f32x4 end = held;
+    if (i + 2 < pieces) held = p[(i + 1) * step];
+    p[i * step] = run;
+    if (i + 1 < pieces) run = end + run * a.decays[(unit + i) * a.heads + head];
+  }
+}
+
+// Whether operands' rows can be read 16 bytes at a time.
+static bool decay_aligned(const DecayArgs& a, int e) {
+  const int64_t on = (int64_t)((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v) | a.ldq * e | a.ldk * e | a.ldv * e |
+                     (int64_t)a.key * e | (int64_t)a.value * e;
+  return on % 16 == 0;
+}
+struct DecayShape {
+  int dk, nc, slices, frames;
+};
+static DecayShape decay_shape(int key, int value) {
+  const int dk = key <= 64 ? 64 : key <= 128 ? 128 : 256, nc = value <= 64 || dk == 256 ? 1 : 2;
+  const int slices = (value + 64 * nc - 1) / (64 * nc);
+  return {dk, nc, slices, slices * 64 * nc * dk / 4};
+}
+template <typename T, int DK, int NC, bool OUT>
+static int decay_tiles(const DecayArgs& a, dim3 blocks, hipStream_t st) {
+  constexpr int C = Mat<T>::CHUNK, e = (int)sizeof(T);
+  constexpr size_t lds = C * ((OUT ? 2 : 1) * DK * e + 64 * NC * e + (OUT ? Mat<T>::P_TERMS * C * e : 0));
+  return decay_aligned(a, e) ? launch(decay_tile_kernel<T, DK, NC, OUT, true>, blocks, 256, lds, st, a)
+                             : launch(decay_tile_kernel<T, DK, NC, OUT, false>, blocks, 256, lds, st, a);
+}
+template <typename T, bool OUT>
+static int decay_tiles(const DecayArgs& a, const DecayShape& s, dim3 blocks, hipStream_t st) {
+  switch (s.dk) {
+    case 64: return s.nc == 1 ? decay_tiles<T, 64, 1, OUT>(a, blocks, st) : decay_tiles<T, 64, 2, OUT>(a, blocks, st);
+    case 128: return s.nc == 1 ? decay_tiles<T, 128, 1, OUT>(a, blocks, st) : decay_tiles<T, 128, 2, OUT>(a, blocks, st);
+    default: return decay_tiles<T, 256, 1, OUT>(a, blocks, st);
+  }
+}
+template <typename T>
+static int decay_prompt(const DecayArgs& a, int64_t units, hipStream_t st) {
+  const DecayShape s = decay_shape(a.key, a.value);
+  const int64_t blocks = units * a.heads;
+  if (!fits_launch(blocks, 256) || !fits_launch((int64_t)a.seqs.count * a.heads, 256)) return refuse_size("ct_decay_attention_run");
+  const dim3 grid((unsigned)blocks, (unsigned)s.slices);
+  if (a.piece) {
+    if (const int rc = decay_tiles<T, false>(a, s, grid, st)) return rc;
+    const dim3 join((unsigned)((int64_t)a.seqs.count * a.heads), (unsigned)((a.frames + 255) / 256));
+    if (const int rc = launch(decay_join_kernel, join, 256, 0, st, a)) return rc;
+  }
+  return decay_tiles<T, true>(a, s, grid, st);
+}
+
+DecayPlan plan_decay(const ct_decay_attention_op& op, const ct_sequences& s) {
+  DecayPlan p = {};
+  const int longest = !s.offsets ? (s.count ? s.tokens / s.count : 0) : s.max_len ? (s.max_len < s.tokens ? s.max_len : s.tokens) : s.tokens;
+  p.step = longest <= kDecayStepTokens;
+  if (p.step) return p;
+  const DecayShape shape = decay_shape(op.key_dim, op.value_dim);
+  // Pieces, so that two blocks are at work on every compute unit, of 256 tokens at least: a piece's
+  // state is as many bytes as some 64 of its tokens
+  const int64_t rows = (int64_t)s.tokens * op.heads * shape.slices;
+  const int64_t piece = (rows / (2 * kPlanCus) + 63) / 64 * 64;
+  p.piece = (int)(piece < 256 ? 256 : piece);
+  if (longest <= p.piece + p.piece / 2) p.piece = 0;
+  if (!p.piece) return p;
+  const SeqView v = {s.offsets, s.slots, s.tokens, s.count, s.num_slots, !s.offsets && s.count ? s.tokens / s.count : 0};
+  p.pieces = seq_tiles(v, p.piece).total;
+  p.ws_floats = p.pieces * op.heads * ((int64_t)shape.frames * 4 + 1);
+  return p;
+}
+
+int launch_decay(const ct_decay_attention_op& op, const DecayPlan& p, const SeqView& s, const DecayArrays& v,
                  void* stream) {
   DecayArgs a = {};
   a.q = v.q; a.k = v.k; a.v = v.v; a.delta = v.delta; a.dt_bias = v.dt_bias; a.a = v.a;
@@ -163,7 +712,15 @@ int launch_decay(const ct_decay_attention_op& op, const DecayPlan&, const SeqVie
   a.dheads = make_fastdiv(op.heads);
   a.dper = make_fastdiv(op.heads / op.groups);
   a.stream = (int64_t)s.count * op.heads * op.key_dim * op.value_dim * 4 >= kStreamStateBytes;
-  return op.dtype == CT_DT_BF16 ? decay_step<bf16_t>(a, (hipStream_t)stream) : decay_step<float>(a, (hipStream_t)stream);
+  hipStream_t st = (hipStream_t)stream;
+  if (p.step) return op.dtype == CT_DT_BF16 ? decay_step<bf16_t>(a, st) : decay_step<float>(a, st);
+  const int64_t units = p.piece ? p.pieces : s.count;
+  a.piece = p.piece;
+  a.per = p.piece ? seq_tiles(s, p.piece).per : 0;
+  a.frames = decay_shape(op.key_dim, op.value_dim).frames;
+  a.ends = (f32x4*)v.ws;
+  a.decays = v.ws + (p.piece ? p.pieces * op.heads * a.frames * 4 : 0);
+  return op.dtype == CT_DT_BF16 ? decay_prompt<bf16_t>(a, units, st) : decay_prompt<float>(a, units, st);
 }
 
 }  // namespace ct

@@ -206,7 +206,7 @@ int ct_decay_attention_run(const ct_decay_attention_op* op, const ct_sequences* 
     if (const int rc = check_workspace(me, ws, ws_bytes, p.ws_floats)) return rc;
     if (const int rc = require_init()) return rc;
     const DecayArrays arrays = {q, k, v, delta, dt_bias, a, state_in, state_out, o, (float*)ws};
-    return launched(me, launch_decay(*op, p, view_of(*seqs), arrays, seqs->max_len, stream));
+    return launched(me, launch_decay(*op, p, view_of(*seqs), arrays, stream));
   });
 }
 

@@ -86,6 +86,7 @@ int launch_mx_linear(const ct_mx_linear_op& op, const MxLinearPlan& p, const MxL
 
 // ---- ct_decay_attention ----
 struct DecayPlan {
+  bool step;          // token by token
   int piece;          // tokens of a piece (0: every sequence in one)
   int64_t pieces;     // pieces in all, an upper bound
   int64_t ws_floats;
@@ -99,6 +100,6 @@ struct DecayArrays {
   float* ws;
 };
 int launch_decay(const ct_decay_attention_op& op, const DecayPlan& p, const SeqView& s, const DecayArrays& v,
-                 int max_len, void* stream);
+                 void* stream);
 
 }  // namespace ct
