@@ -207,12 +207,16 @@ struct Mat<float> {
 template <int TERMS>
 __device__ __forceinline__ void split8(float (&v)[8], bf16x8 (&f)[TERMS]) {
 #pragma unroll
-  for (int t = 0; t < TERMS; ++t)
+  for (int t = 0; t < TERMS; ++t) {
+    unsigned w[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      f[t][i] = (__bf16)v[i];
-      v[i] -= (float)f[t][i];
+    for (int i = 0; i < 4; ++i) {
+      w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+      v[2 * i] -= unpack<bf16_t>(w[i], 0);
+      v[2 * i + 1] -= unpack<bf16_t>(w[i], 1);
     }
+    f[t] = __builtin_bit_cast(bf16x8, (u32x4){w[0], w[1], w[2], w[3]});
+  }
 }
 
 // A tile in LDS: rows of BYTES, their 16-byte groups permuted by the row's number so that eight
@@ -222,32 +226,36 @@ __device__ __forceinline__ int tile_at(int row, int group) {
   const int key = ((row & 3) << 1 | (row >> 2 & 1)) & (BYTES / 16 - 1);
   return row * BYTES + (group ^ key) * 16;
 }
-// Row r0 + lane % 16, steps of number k.
+// The permutation is an exclusive or on the group's bits of an address, so that a lane's address of
+// another group is its own one with that group's bits turned over, and that of a row a multiple of 8
+// further on its own one and the rows between.
+// Row r0 + lane % 16 (r0 a multiple of 8), steps of number k.
 template <typename T, int BYTES>
 __device__ __forceinline__ typename Mat<T>::Frag read_rows(const char* tile, int r0, int k) {
   const int lane = (int)threadIdx.x & 63;
-  return *(const typename Mat<T>::Frag*)(tile + tile_at<BYTES>(r0 + (lane & 15), k * 4 + (lane >> 4)));
+  return *(const typename Mat<T>::Frag*)(tile + r0 * BYTES + (tile_at<BYTES>(lane & 15, lane >> 4) ^ k * 64));
 }
-// Column of lane % 16, steps (rows) of number k: fp32 column c0 + lane % 16, bf16 the lane's of four
-// runs of four columns, `run` columns apart.
-template <typename T, int BYTES>
-__device__ __forceinline__ typename Mat<T>::Frag read_cols(const char* tile, int k, int c0, int run) {
+// Column of lane % 16, steps (rows) of number k. In bf16 the lane's of four runs of four columns that
+// lie RUN (4 or 8) columns apart, from column c0 on (a multiple of 16, or of 32 and 4 more); in fp32
+// column c0 + lane % 16.
+template <typename T, int BYTES, int RUN>
+__device__ __forceinline__ typename Mat<T>::Frag read_cols(const char* tile, int k, int c0) {
   const int lane = (int)threadIdx.x & 63, g = lane >> 4, l = lane & 15;
   if constexpr (sizeof(T) == 2) {
     typedef i16x4 __attribute__((address_space(3))) * lds_i16x4;
     i16x4 part[2];
-    const int col = c0 + (l & 3) * run;  // this lane's run for the transposed read, of row l / 4
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const char* p = tile + tile_at<BYTES>(k * 32 + g * 8 + h * 4 + (l >> 2), col / 8) + (col & 4) * 2;
+    for (int h = 0; h < 2; ++h) {  // this lane's run for the transposed read, of row l / 4
+      const int at = tile_at<BYTES>(g * 8 + h * 4 + (l >> 2), (l & 3) * RUN / 8) ^ c0 / 8 * 16;
+      const char* p = tile + k * 32 * BYTES + (c0 & 4) * 2 + at + ((l & 3) * RUN & 4) * 2;
       part[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4)(__attribute__((address_space(3))) char*)p);
     }
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
   } else {
-    const int col = c0 + l;
     f32x4 f;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) f[e] = *(const float*)(tile + tile_at<BYTES>(k * 16 + g * 4 + e, col / 4) + (col & 3) * 4);
+    for (int e = 0; e < 4; ++e)
+      f[e] = *(const float*)(tile + k * 16 * BYTES + (tile_at<BYTES>(g * 4 + e, l / 4) ^ c0 * 4) + (l & 3) * 4);
     return f;
   }
 }
@@ -292,34 +300,46 @@ __device__ __forceinline__ void fill_tile(char* tile, const T* base, int64_t ld,
   }
 }
 
-// What the tokens of a chunk carry: G in two parts, e^G, the weights of the state's sum and the
-// steps (1 where they do not scale the input).
+// What the tokens of a chunk carry: G in two parts, e^G and the steps (1 where they do not scale the
+// input), both times the scale of o, and the weights of the state's sum.
 template <int C>
 struct Steps {
   float hi[C], lo[C], grown[C], weight[C], dt[C];
-  float end;  // e^{G_C}
+  float end;   // e^{G_C}
+  double sum;  // G_C / ln 2
 };
 
 // Whether one of a lane's values is infinite or NaN.
-template <typename F, int N>
-__device__ __forceinline__ bool any_wild(const F& f) {
+__device__ __forceinline__ bool any_wild(bf16x8 f) {
+  typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+  const u32x4 q = __builtin_bit_cast(u32x4, f);
+  u16x2 m = {};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const unsigned w = q[i] & 0x7FFF7FFFu;
+    m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w));
+  }
+  return max(m.x, m.y) >= 0x7F80;
+}
+__device__ __forceinline__ bool any_wild(f32x4 f) {
   bool any = false;
 #pragma unroll
-  for (int e = 0; e < N; ++e) any |= !(__builtin_fabsf((float)f[e]) < __builtin_inff());
+  for (int e = 0; e < 4; ++e) any |= !(__builtin_fabsf(f[e]) < __builtin_inff());
   return any;
 }
 
 template <typename T, int DK, int NC, bool OUT, bool ALIGNED>
-__global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 ? 1 : 2) decay_tile_kernel(DecayArgs a) {
+__global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED && DK * NC == 256) ? 1 : 2) decay_tile_kernel(DecayArgs a) {
   typedef Mat<T> M;
   typedef typename M::Frag Frag;
   constexpr int C = M::CHUNK, KS = M::KS, IT = C / 16, DT = DK / 16, DKS = DK / KS, CKS = C / KS;
   constexpr int DV = 64 * NC, KB = DK * (int)sizeof(T), VB = DV * (int)sizeof(T), PB = C * (int)sizeof(T);
-  constexpr int AT_K = OUT ? C * KB : 0, AT_V = AT_K + C * KB, AT_P = AT_V + C * VB;
+  // OUT: q, k, v and the weights; else k and v, twice
+  constexpr int AT_K = OUT ? C * KB : 0, AT_V = AT_K + C * KB, AT_P = AT_V + C * VB, TWICE = OUT ? 0 : AT_P;
   extern __shared__ __align__(16) char lds[];
-  __shared__ Steps<C> steps[2];
+  __shared__ Steps<C> steps[8];  // four chunks ahead, a wave to each, and the four at work
   const int lane = (int)threadIdx.x & 63, wave = wave_id(), g = lane >> 4, l16 = lane & 15;
-  char *tq = lds, *tk = lds + AT_K, *tv = lds + AT_V, *tp = lds + AT_P;
+  char *tq = lds, *tp = lds + AT_P;
 
   const int unit = fdiv((int)blockIdx.x, a.dheads), head = (int)blockIdx.x - unit * a.heads;
   int begin, end;
@@ -343,17 +363,13 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 ? 1 : 2) decay_
   const T* k = (const T*)a.k + (int64_t)group * a.key;
   const T* v = (const T*)a.v + (int64_t)head * a.value + c0;
 
-  const auto fill_q = [&](int t) __attribute__((always_inline)) {
-    fill_tile<T, KB, C, ALIGNED>(tq, q + t * a.ldq, a.ldq, min(end - t, C), a.key);
+  const auto fill = [&](int t, int half) __attribute__((always_inline)) {
+    const int rows = min(end - t, C);
+    if constexpr (OUT) fill_tile<T, KB, C, ALIGNED>(tq, q + t * a.ldq, a.ldq, rows, a.key);
+    fill_tile<T, KB, C, ALIGNED>(lds + AT_K + half * TWICE, k + t * a.ldk, a.ldk, rows, a.key);
+    fill_tile<T, VB, C, ALIGNED>(lds + AT_V + half * TWICE, v + t * a.ldv, a.ldv, rows, cols);
   };
-  const auto fill_kv = [&](int t) __attribute__((always_inline)) {
-    fill_tile<T, KB, C, ALIGNED>(tk, k + t * a.ldk, a.ldk, min(end - t, C), a.key);
-    fill_tile<T, VB, C, ALIGNED>(tv, v + t * a.ldv, a.ldv, min(end - t, C), cols);
-  };
-  if (begin < end) {
-    if constexpr (OUT) fill_q(begin);
-    fill_kv(begin);
-  }
+  if (begin < end) fill(begin, 0);
 
   // The state: element e of S[t][c] is row row0 + row_of(t) + e, column cw + 16 c + l16, of a buffer
   // that ends with its last row; columns past the last have an offset past it.
@@ -385,12 +401,11 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 ? 1 : 2) decay_
           S[t][c][e] = load_elem<float>(rs, state_off[c] == kOobGroup ? kOobGroup : state_off[c] + (unsigned)((row_of(t) + e) * a.value) * 4, 0);
   }
 
-  double total = 0;
-  // Wave 0: what `delta` holds for the chunk at t, a token to a lane, and the chunk's steps from it
-  const auto ask = [&](int t) { return lane < C && t + lane < end ? delta_of(a, t + lane, head) : 0.f; };
-  const auto make_steps = [&](int t, float delta, Steps<C>& to) __attribute__((always_inline)) {
-    const Step s = step_of(a, delta, bias, rate);
-    double G = lane < C && t + lane < end ? (double)s.l * 1.4426950408889634 : 0.;
+  // The steps of the chunk at t, a token to a lane
+  const auto make_steps = [&](int t, Steps<C>& to) __attribute__((always_inline)) {
+    const bool mine = lane < C && t < end && t + lane < end;
+    const Step s = step_of(a, mine ? delta_of(a, t + lane, head) : 0.f, bias, rate);
+    double G = mine ? (double)s.l * 1.4426950408889634 : 0.;
 #pragma unroll
     for (int o = 1; o < C; o <<= 1) {
       const double up = __shfl_up(G, o);
@@ -398,27 +413,34 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 ? 1 : 2) decay_
     }
     const double all = __shfl(G, C - 1);
     if (lane < C) {
-      const float dt = a.step_input && t + lane < end ? s.dt : 1.f;
+      const float dt = a.step_input && mine ? s.dt : 1.f;
       to.hi[lane] = (float)G;
       to.lo[lane] = (float)(G - (double)(float)G);
-      to.grown[lane] = __builtin_amdgcn_exp2f((float)G);
+      to.grown[lane] = __builtin_amdgcn_exp2f((float)G) * a.scale;
       to.weight[lane] = __builtin_amdgcn_exp2f((float)(all - G)) * dt;
-      to.dt[lane] = dt;
-      if (lane == 0) to.end = __builtin_amdgcn_exp2f((float)all);
+      to.dt[lane] = dt * a.scale;
+      if (lane == 0) {
+        to.end = __builtin_amdgcn_exp2f((float)all);
+        to.sum = all;
+      }
     }
-    total += all;
   };
-  if (wave == 0 && begin < end) make_steps(begin, ask(begin), steps[0]);
 
+  double total = 0;
   int turn = 0;
 #pragma unroll 1
-  for (int t = begin; t < end; turn ^= 1) {
+  for (int t = begin; t < end; turn = (turn + 1) & 7) {
     const Steps<C>& st = steps[turn];
     const int next = tile_end(t, end, C);
+    if (turn % 4 == 0) make_steps(tile_end(t, end, wave * C), steps[turn + wave]);
     wait_copies();
     __syncthreads();
-    float delta = 0;
-    if (wave == 0 && next < end) delta = ask(next);
+    const int half = OUT ? 0 : turn & 1;
+    const char *tk = lds + AT_K + half * TWICE, *tv = lds + AT_V + half * TWICE;
+    if constexpr (!OUT) {
+      total += st.sum;
+      if (next < end) fill(next, half ^ 1);  // whose last chunk everybody has read
+    }
 
     f32x4 O[IT][NC];
     if constexpr (OUT) {
@@ -465,7 +487,9 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 ? 1 : 2) decay_
         for (int c = 0; c < NC; ++c) O[i][c] = f32x4{};
 #pragma unroll
       for (int s = 0; s < DKS; ++s) {
-        Frag fs[NC][M::STATE_TERMS];
+        Frag fs[NC][M::STATE_TERMS], fq[IT];
+#pragma unroll
+        for (int i = 0; i < IT; ++i) fq[i] = read_rows<T, KB>(tq, i * 16, s);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           if constexpr (sizeof(T) == 2) {
@@ -478,13 +502,11 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 ? 1 : 2) decay_
           }
         }
 #pragma unroll
-        for (int i = 0; i < IT; ++i) {
-          const Frag fq = read_rows<T, KB>(tq, i * 16, s);
+        for (int n = 0; n < M::STATE_TERMS; ++n)
 #pragma unroll
-          for (int c = 0; c < NC; ++c)
+          for (int i = 0; i < IT; ++i)
 #pragma unroll
-            for (int n = 0; n < M::STATE_TERMS; ++n) O[i][c] = M::mma(fs[c][n], fq, O[i][c]);
-        }
+            for (int c = 0; c < NC; ++c) O[i][c] = M::mma(fs[c][n], fq[i], O[i][c]);
         asm volatile("" ::: "memory");  // one step's operands at a time
       }
 #pragma unroll
@@ -496,13 +518,8 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 ? 1 : 2) decay_
           for (int e = 0; e < 4; ++e) O[i][c][e] *= grown;
       }
     }
-    if (wave == 0 && next < end) make_steps(next, delta, steps[turn ^ 1]);
-    if constexpr (OUT) {
-      __syncthreads();
-      if (next < end) fill_q(next);  // q has been read
-    }
 
-    // Tokens of the chunk: to the outputs behind them, and to the state
+    // The chunk's tokens to the state; their v stays in registers
     const float decay = st.end;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -510,92 +527,110 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 ? 1 : 2) decay_
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e) S[d][c][e] *= decay;
-    bool odd = false;
+    Frag fv[CKS][NC];
 #pragma unroll
     for (int s = 0; s < CKS; ++s) {
       constexpr int E = KS / 4;
-      Frag fv[NC], fw[NC][M::V_TERMS];
+      Frag fw[NC][M::V_TERMS];
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        fv[c] = read_cols<T, VB>(tv, s, wave * 16 * NC + 16 * c, 4);
+        fv[s][c] = read_cols<T, VB, 4>(tv, s, wave * 16 * NC + 16 * c);
         float x[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = (float)fv[c][e] * st.weight[s * KS + g * E + e];
+        for (int e = 0; e < E; ++e) x[e] = (float)fv[s][c][e] * st.weight[s * KS + g * E + e];
         if constexpr (sizeof(T) == 2) split8(x, fw[c]);
         else fw[c][0] = (f32x4){x[0], x[1], x[2], x[3]};
-        // What is infinite or NaN is added by itself, to the tokens from its own on: a product with
-        // the weight 0 of an earlier one would be NaN
-        if (OUT && __ballot(any_wild<Frag, E>(fv[c]))) {
-          odd = true;
-#pragma unroll
-          for (int e = 0; e < E; ++e)
-            if (!(__builtin_fabsf((float)fv[c][e]) < __builtin_inff())) fv[c][e] = 0;
-        }
       }
-      if constexpr (OUT) {
 #pragma unroll
-        for (int i = s * KS / 16; i < IT; ++i) {
+      for (int d = 0; d < DT; d += 2) {
+        Frag fk[2];
 #pragma unroll
-          for (int n = 0; n < M::P_TERMS; ++n) {
-            const Frag fp = read_rows<T, PB>(tp + n * C * PB, i * 16, s);
+        for (int h = 0; h < 2; ++h) fk[h] = read_cols<T, KB, 8>(tk, s, sizeof(T) == 2 ? d / 2 * 32 + h * 4 : (d + h) * 16);
 #pragma unroll
-            for (int c = 0; c < NC; ++c) O[i][c] = M::mma(fv[c], fp, O[i][c]);
-          }
-        }
+        for (int n = 0; n < M::V_TERMS; ++n)
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) S[d + h][c] = M::mma(fk[h], fw[c][n], S[d + h][c]);
         asm volatile("" ::: "memory");
-      }
-#pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        const Frag fk = sizeof(T) == 2 ? read_cols<T, KB>(tk, s, d / 2 * 32 + (d & 1) * 4, 8) : read_cols<T, KB>(tk, s, d * 16, 4);
-#pragma unroll
-        for (int c = 0; c < NC; ++c)
-#pragma unroll
-          for (int n = 0; n < M::V_TERMS; ++n) S[d][c] = M::mma(fk, fw[c][n], S[d][c]);
-        if (d % 2) asm volatile("" ::: "memory");
       }
     }
     if constexpr (OUT) {
+      // What is infinite or NaN is added by itself, to the tokens from its own on: a product with the
+      // weight 0 of an earlier one would be NaN
+      bool odd = false;
+#pragma unroll
+      for (int s = 0; s < CKS; ++s)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) odd |= any_wild(fv[s][c]);
+      odd = __ballot(odd) != 0;
+      if (odd) {
+#pragma unroll
+        for (int s = 0; s < CKS; ++s)
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int e = 0; e < KS / 4; ++e)
+              if (!(__builtin_fabsf((float)fv[s][c][e]) < __builtin_inff())) fv[s][c][e] = 0;
+      }
+      __syncthreads();  // the weights are there, and q, k and v have been read
+      if (next < end) fill(next, 0);
+
+      // The tokens of the chunk to the outputs behind them
+#pragma unroll
+      for (int s = 0; s < CKS; ++s)
+#pragma unroll
+        for (int n = 0; n < M::P_TERMS; ++n)
+#pragma unroll
+          for (int i = s * KS / 16; i < IT; ++i) {
+            const Frag fp = read_rows<T, PB>(tp + n * C * PB, i * 16, s);
+#pragma unroll
+            for (int c = 0; c < NC; ++c) O[i][c] = M::mma(fv[s][c], fp, O[i][c]);
+          }
       if (odd) {
 #pragma unroll
         for (int i = 0; i < IT; ++i)
 #pragma unroll
           for (int c = 0; c < NC; ++c)
 #pragma unroll 1
-            for (int j = 0; j <= i * 16 + l16; ++j) {
-              const int row = i * 16 + l16;
+            for (int j = 0; j <= i * 16 + l16 && t + j < end; ++j) {
+              const int row = i * 16 + l16, col = (wave * NC + c) * 16 + g * 4;
               float p = 0;
 #pragma unroll
               for (int n = 0; n < M::P_TERMS; ++n)
                 p += (float)*(const T*)(tp + n * C * PB + tile_at<PB>(row, j * (int)sizeof(T) / 16) + j * (int)sizeof(T) % 16);
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                const int col = (wave * NC + c) * 16 + g * 4 + e;
-                const float x = (float)*(const T*)(tv + tile_at<VB>(j, col * (int)sizeof(T) / 16) + col * (int)sizeof(T) % 16);
+                if (col + e >= cols) break;
+                const float x = (float)v[(t + j) * a.ldv + col + e];
                 if (!(__builtin_fabsf(x) < __builtin_inff())) O[i][c][e] += p * x;
               }
             }
       }
+      // Rows and columns past the last have an offset past the buffer
+      const __amdgpu_buffer_rsrc_t ro = make_rsrc((T*)a.o + t * a.ldo + (int64_t)head * a.value,
+                                                  ((min(end - t, C) - 1) * a.ldo + a.value) * (int64_t)sizeof(T));
 #pragma unroll
-      for (int i = 0; i < IT; ++i) {
-        const int row = t + i * 16 + l16;
-        if (row >= end) continue;
+      for (int i = 0; i < IT; ++i)
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           const int col = cw + 16 * c + g * 4;
-          T* p = (T*)a.o + row * a.ldo + (int64_t)head * a.value + col;
-          float x[4];
+          const unsigned off = (unsigned)((i * 16 + l16) * (int)a.ldo + col) * (unsigned)sizeof(T);
+          const bool row = t + i * 16 + l16 < end;
+          if constexpr (ALIGNED) {
+            const unsigned at = row && col < a.value ? off : kOobGroup;
+            if constexpr (sizeof(T) == 2)
+              __builtin_amdgcn_raw_buffer_store_b64((u32x2){pack_bf16(O[i][c][0], O[i][c][1]), pack_bf16(O[i][c][2], O[i][c][3])},
+                                                    ro, (int)at, 0, 0);
+            else
+              __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, O[i][c]), ro, (int)at, 0, 0);
+          } else {
 #pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = O[i][c][e] * a.scale;
-          if (col + 4 <= a.value) store_quad4(p, x, false);
-          else
-#pragma unroll
-            for (int e = 0; e < 3; ++e)
-              if (col + e < a.value) p[e] = from_f32<T>(x[e]);
+            for (int e = 0; e < 4; ++e)
+              store_elem<T>(ro, row && col + e < a.value ? off + e * (unsigned)sizeof(T) : kOobGroup, 0, O[i][c][e]);
+          }
         }
-      }
     }
-    __syncthreads();
-    if (next < end) fill_kv(next);  // k and v have been read
     t = next;
   }
 
@@ -638,10 +673,10 @@ __global__ void __launch_bounds__(256) decay_join_kernel(DecayArgs a) {
   }
 }
 
-// Whether operands' rows can be read 16 bytes at a time.
+// Whether rows can be read and written 16 bytes at a time.
 static bool decay_aligned(const DecayArgs& a, int e) {
-  const int64_t on = (int64_t)((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v) | a.ldq * e | a.ldk * e | a.ldv * e |
-                     (int64_t)a.key * e | (int64_t)a.value * e;
+  const int64_t on = (int64_t)((uintptr_t)a.q | (uintptr_t)a.k | (uintptr_t)a.v | (uintptr_t)a.o) | a.ldq * e | a.ldk * e |
+                     a.ldv * e | a.ldo * e | (int64_t)a.key * e | (int64_t)a.value * e;
   return on % 16 == 0;
 }
 struct DecayShape {
@@ -655,7 +690,7 @@ static DecayShape decay_shape(int key, int value) {
 template <typename T, int DK, int NC, bool OUT>
 static int decay_tiles(const DecayArgs& a, dim3 blocks, hipStream_t st) {
   constexpr int C = Mat<T>::CHUNK, e = (int)sizeof(T);
-  constexpr size_t lds = C * ((OUT ? 2 : 1) * DK * e + 64 * NC * e + (OUT ? Mat<T>::P_TERMS * C * e : 0));
+  constexpr size_t lds = OUT ? C * (2 * DK * e + 64 * NC * e + Mat<T>::P_TERMS * C * e) : 2 * C * (DK * e + 64 * NC * e);
   return decay_aligned(a, e) ? launch(decay_tile_kernel<T, DK, NC, OUT, true>, blocks, 256, lds, st, a)
                              : launch(decay_tile_kernel<T, DK, NC, OUT, false>, blocks, 256, lds, st, a);
 }
