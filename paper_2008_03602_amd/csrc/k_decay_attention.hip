@@ -401,10 +401,12 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
           S[t][c][e] = load_elem<float>(rs, state_off[c] == kOobGroup ? kOobGroup : state_off[c] + (unsigned)((row_of(t) + e) * a.value) * 4, 0);
   }
 
-  // The steps of the chunk at t, a token to a lane
-  const auto make_steps = [&](int t, Steps<C>& to) __attribute__((always_inline)) {
-    const bool mine = lane < C && t < end && t + lane < end;
-    const Step s = step_of(a, mine ? delta_of(a, t + lane, head) : 0.f, bias, rate);
+  // The steps of the chunk at t, a token to a lane, from what was asked for before
+  const auto has = [&](int t) { return lane < C && t < end && t + lane < end; };
+  const auto ask = [&](int t) { return has(t) ? delta_of(a, t + lane, head) : 0.f; };
+  const auto make_steps = [&](int t, float delta, Steps<C>& to) __attribute__((always_inline)) {
+    const bool mine = has(t);
+    const Step s = step_of(a, delta, bias, rate);
     double G = mine ? (double)s.l * 1.4426950408889634 : 0.;
 #pragma unroll
     for (int o = 1; o < C; o <<= 1) {
@@ -427,14 +429,16 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
   };
 
   double total = 0;
+  float delta = ask(tile_end(begin, end, wave * C));
   int turn = 0;
 #pragma unroll 1
   for (int t = begin; t < end; turn = (turn + 1) & 7) {
     const Steps<C>& st = steps[turn];
     const int next = tile_end(t, end, C);
-    if (turn % 4 == 0) make_steps(tile_end(t, end, wave * C), steps[turn + wave]);
+    if (turn % 4 == 0) make_steps(tile_end(t, end, wave * C), delta, steps[turn + wave]);
     wait_copies();
     __syncthreads();
+    if (turn % 4 == 3) delta = ask(tile_end(next, end, wave * C));
     const int half = OUT ? 0 : turn & 1;
     const char *tk = lds + AT_K + half * TWICE, *tv = lds + AT_V + half * TWICE;
     if constexpr (!OUT) {
@@ -447,16 +451,26 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
       // Weights of tokens i = 16 wave + l16 (a wave to 16 of them), j = 16 jt + 4 g + e
       if (wave < IT) {
         f32x4 p[IT] = {};
+        Frag fq = read_rows<T, KB>(tq, wave * 16, 0), fk[IT];
+#pragma unroll
+        for (int jt = 0; jt < IT; ++jt) fk[jt] = read_rows<T, KB>(tk, jt * 16, 0);
 #pragma unroll
         for (int s = 0; s < DKS; ++s) {
-          const Frag fq = read_rows<T, KB>(tq, wave * 16, s);
+          const Frag nq = read_rows<T, KB>(tq, wave * 16, s + 1 < DKS ? s + 1 : s);
 #pragma unroll
-          for (int jt = 0; jt < IT; ++jt) p[jt] = M::mma(read_rows<T, KB>(tk, jt * 16, s), fq, p[jt]);
+          for (int jt = 0; jt < IT; ++jt) {
+            const Frag now = fk[jt];
+            if (s + 1 < DKS) fk[jt] = read_rows<T, KB>(tk, jt * 16, s + 1);
+            if (jt <= wave) p[jt] = M::mma(now, fq, p[jt]);
+          }
+          fq = nq;
+          __builtin_amdgcn_sched_barrier(0);
         }
         const int i = wave * 16 + l16;
         const float hi = st.hi[i], lo = st.lo[i];
 #pragma unroll
         for (int jt = 0; jt < IT; ++jt) {
+          if (jt > (sizeof(T) == 2 ? wave | 1 : wave)) continue;  // a step of the product with v that no token of the wave's has
           const f32x4 hj = *(const f32x4*)&st.hi[jt * 16 + g * 4], lj = *(const f32x4*)&st.lo[jt * 16 + g * 4];
           const f32x4 dj = *(const f32x4*)&st.dt[jt * 16 + g * 4];
           float x[4];
@@ -485,11 +499,18 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
       for (int i = 0; i < IT; ++i)
 #pragma unroll
         for (int c = 0; c < NC; ++c) O[i][c] = f32x4{};
+      Frag nq[IT];
+#pragma unroll
+      for (int i = 0; i < IT; ++i) nq[i] = read_rows<T, KB>(tq, i * 16, 0);
 #pragma unroll
       for (int s = 0; s < DKS; ++s) {
         Frag fs[NC][M::STATE_TERMS], fq[IT];
 #pragma unroll
-        for (int i = 0; i < IT; ++i) fq[i] = read_rows<T, KB>(tq, i * 16, s);
+        for (int i = 0; i < IT; ++i) {
+          fq[i] = nq[i];
+          if (s + 1 < DKS) nq[i] = read_rows<T, KB>(tq, i * 16, s + 1);
+        }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
           if constexpr (sizeof(T) == 2) {
@@ -507,7 +528,7 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
           for (int i = 0; i < IT; ++i)
 #pragma unroll
             for (int c = 0; c < NC; ++c) O[i][c] = M::mma(fs[c][n], fq[i], O[i][c]);
-        asm volatile("" ::: "memory");  // one step's operands at a time
+        __builtin_amdgcn_sched_barrier(0);  // one step's operands ahead
       }
 #pragma unroll
       for (int i = 0; i < IT; ++i) {
@@ -527,14 +548,22 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
       for (int c = 0; c < NC; ++c)
 #pragma unroll
         for (int e = 0; e < 4; ++e) S[d][c][e] *= decay;
-    Frag fv[CKS][NC];
+    Frag fv[CKS][NC], nk[2];
+    const auto read_k = [&](int s, int d) __attribute__((always_inline)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) nk[h] = read_cols<T, KB, 8>(tk, s, sizeof(T) == 2 ? d / 2 * 32 + h * 4 : (d + h) * 16);
+    };
+    read_k(0, 0);
+#pragma unroll
+    for (int s = 0; s < CKS; ++s)
+#pragma unroll
+      for (int c = 0; c < NC; ++c) fv[s][c] = read_cols<T, VB, 4>(tv, s, wave * 16 * NC + 16 * c);
 #pragma unroll
     for (int s = 0; s < CKS; ++s) {
       constexpr int E = KS / 4;
       Frag fw[NC][M::V_TERMS];
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        fv[s][c] = read_cols<T, VB, 4>(tv, s, wave * 16 * NC + 16 * c);
         float x[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) x[e] = (float)fv[s][c][e] * st.weight[s * KS + g * E + e];
@@ -543,16 +572,17 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
       }
 #pragma unroll
       for (int d = 0; d < DT; d += 2) {
-        Frag fk[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) fk[h] = read_cols<T, KB, 8>(tk, s, sizeof(T) == 2 ? d / 2 * 32 + h * 4 : (d + h) * 16);
+        const Frag fk[2] = {nk[0], nk[1]};
+        if (d + 2 < DT) read_k(s, d + 2);
+        else if (s + 1 < CKS) read_k(s + 1, 0);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int n = 0; n < M::V_TERMS; ++n)
 #pragma unroll
           for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int c = 0; c < NC; ++c) S[d + h][c] = M::mma(fk[h], fw[c][n], S[d + h][c]);
-        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     if constexpr (OUT) {
@@ -664,12 +694,24 @@ __global__ void __launch_bounds__(256) decay_join_kernel(DecayArgs a) {
   if (at >= a.frames || pieces < 2) return;
   const int64_t step = (int64_t)a.heads * a.frames;
   f32x4* p = a.ends + (unit * a.heads + head) * a.frames + at;
-  f32x4 run = *p, held = pieces > 2 ? p[step] : f32x4{};
-  for (int i = 1; i < pieces; ++i) {
-    const f32x4 end = held;
-    if (i + 2 < pieces) held = p[(i + 1) * step];
-    p[i * step] = run;
-    if (i + 1 < pieces) run = end + run * a.decays[(unit + i) * a.heads + head];
+  const float* decay = a.decays + unit * a.heads + head;
+  constexpr int AHEAD = 8;
+  f32x4 run = *p;
+  for (int i = 1; i < pieces; i += AHEAD) {  // pieces i to i + 7: their ends all on their way, the last one's not needed
+    f32x4 end[AHEAD];
+    float d[AHEAD];
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) {
+      const int from = min(i + n, pieces - 2);
+      end[n] = p[from * step];
+      d[n] = decay[(int64_t)from * a.heads];
+    }
+#pragma unroll
+    for (int n = 0; n < AHEAD; ++n) {
+      if (i + n >= pieces) break;
+      p[(i + n) * step] = run;
+      run = end[n] + run * d[n];
+    }
   }
 }
 
