@@ -103,7 +103,6 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) mx_linear_kernel(MxLinearAr
   constexpr int AT_X = BN * RBW, AT_SW = AT_X + BM * RBX, AT_SX = AT_SW + BN * 4, TEAM = AT_SX + BM * 4;
   constexpr int STAGE = WK * TEAM;
   static_assert(BN % (RPCW * WAVES) == 0 && BM % (RPCX * WAVES) == 0 && SW <= 64 && SX <= 64, "every wave copies as many rows");
-  static_assert((RPCW * WAVES >> 1) % (RBW / 16) == 0 && (RPCX * WAVES >> 1) % (RBX / 16) == 0, "one permutation for every copy");
   extern __shared__ __align__(16) char lds[];
 
   const TileAt tile = tile_of_block(a, (int)blockIdx.x);
@@ -118,23 +117,24 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) mx_linear_kernel(MxLinearAr
   const __amdgpu_buffer_rsrc_t rw = make_rsrc(vw.base, vw.bytes), rx = make_rsrc(vx.base, vx.bytes);
   const __amdgpu_buffer_rsrc_t rsw = make_rsrc(vsw.base, vsw.bytes), rsx = make_rsrc(vsx.base, vsx.bytes);
 
-  // Byte of a row that a lane copies in each step: whole rows to a copy, lane by lane in LDS, so
-  // that the permutation of a row's groups is one of the addresses that its lanes read.
-  const auto first = [&](int rb) {
-    const int lpr = rb / 16, row = wave * (64 / lpr) + lane / lpr;
-    return ((lane % lpr) ^ ((row >> 1) & (lpr - 1))) * 16;
+  // The row of copy i that a lane copies 16 bytes of in each step, and which: whole rows to a copy,
+  // lane by lane in LDS, so that the permutation of a row's groups is one of the addresses that its
+  // lanes read (the same for every copy, but for a single wave's of 8-bit rows).
+  const auto row_of = [&](int rb, int i) { return (i * WAVES + wave) * (1024 / rb) + lane / (rb / 16); };
+  const auto first = [&](int rb, int i) {
+    const bool same = WAVES * (1024 / rb) % (rb / 8) == 0;
+    return ((lane % (rb / 16)) ^ ((row_of(rb, same ? 0 : i) >> 1) & (rb / 16 - 1))) * 16;
   };
-  const int first_w = first(RBW), first_x = first(RBX);
   unsigned off_w[NCW], off_x[NCX];
 #pragma unroll
   for (int i = 0; i < NCW; ++i) {
-    const int r = (i * WAVES + wave) * RPCW + lane / (RBW / 16);
-    off_w[i] = n0 + r < a.n ? (unsigned)(r * (int)a.ldw + first_w) : kOobGroup;
+    const int r = row_of(RBW, i);
+    off_w[i] = n0 + r < a.n ? (unsigned)(r * (int)a.ldw + first(RBW, i)) : kOobGroup;
   }
 #pragma unroll
   for (int i = 0; i < NCX; ++i) {
-    const int r = (i * WAVES + wave) * RPCX + lane / (RBX / 16);
-    off_x[i] = m0 + r < a.m ? (unsigned)(r * (int)a.ldx + first_x) : kOobGroup;
+    const int r = row_of(RBX, i);
+    off_x[i] = m0 + r < a.m ? (unsigned)(r * (int)a.ldx + first(RBX, i)) : kOobGroup;
   }
   const unsigned off_sw = n0 + wave * SW + lane < a.n ? (unsigned)((wave * SW + lane) * (int)a.ldws) : kOobGroup;
   const unsigned off_sx = m0 + wave * SX + lane < a.m ? (unsigned)((wave * SX + lane) * (int)a.ldxs) : kOobGroup;
@@ -149,13 +149,16 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) mx_linear_kernel(MxLinearAr
         return tail.value ? uniform_part(k, bytes) : (int)k;
       };
       const int kw = at(RBW, vw.bytes), kx = at(RBX, vx.bytes), ksw = at(4, vsw.bytes), ksx = at(4, vsx.bytes);
-      const bool out_w = none || (tail.value && step * RBW + first_w >= row_w);
-      const bool out_x = none || (tail.value && step * RBX + first_x >= row_x);
 #pragma unroll
-      for (int i = 0; i < NCW; ++i) copy_lds<16>(rw, dst + (i * WAVES + wave) * 1024, out_w ? kOobGroup : off_w[i], kw);
+      for (int i = 0; i < NCW; ++i) {
+        const bool out = none || (tail.value && step * RBW + first(RBW, i) >= row_w);
+        copy_lds<16>(rw, dst + (i * WAVES + wave) * 1024, out ? kOobGroup : off_w[i], kw);
+      }
 #pragma unroll
-      for (int i = 0; i < NCX; ++i)
-        copy_lds<16>(rx, dst + AT_X + (i * WAVES + wave) * 1024, out_x ? kOobGroup : off_x[i], kx);
+      for (int i = 0; i < NCX; ++i) {
+        const bool out = none || (tail.value && step * RBX + first(RBX, i) >= row_x);
+        copy_lds<16>(rx, dst + AT_X + (i * WAVES + wave) * 1024, out ? kOobGroup : off_x[i], kx);
+      }
       // some lane of every wave copies, so that the copies on their way are as many in each
       if (lane < SW) copy_lds<4>(rsw, dst + AT_SW + wave * SW * 4, none ? kOobGroup : off_sw, ksw);
       if (lane < SX) copy_lds<4>(rsx, dst + AT_SX + wave * SX * 4, none ? kOobGroup : off_sx, ksx);
@@ -248,11 +251,11 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) mx_linear_kernel(MxLinearAr
 }
 
 // ------------------------------------------------------------------ plans and launches
-enum { MXL_32, MXL_64, MXL_128X64, MXL_128, MXL_256, MXL_KINDS };
+enum { MXL_32X16, MXL_32, MXL_64, MXL_128X64, MXL_128, MXL_256, MXL_KINDS };
 struct MxShape {
   int bm, bn, wm, wn, wk, stages;
 };
-constexpr MxShape kMxTiles[MXL_KINDS] = {{32, 32, 1, 2, 4, 3}, {64, 64, 2, 2, 2, 3}, {128, 64, 2, 2, 1, 3},
+constexpr MxShape kMxTiles[MXL_KINDS] = {{32, 16, 1, 1, 8, 3}, {32, 32, 1, 2, 4, 3}, {64, 64, 2, 2, 2, 3}, {128, 64, 2, 2, 1, 3},
                                          {128, 128, 2, 2, 1, 2}, {256, 256, 4, 2, 1, 2}};
 
 static int64_t tiles_of(const ct_mx_linear_op& op, int kind) {
@@ -275,6 +278,7 @@ MxLinearPlan plan_mx_linear(const ct_mx_linear_op& op) {
       p.kind = kind;
     }
   if (op.m <= 32 || (p.kind == MXL_64 && tiles_of(op, MXL_64) < kPlanCus * 3 / 4)) p.kind = MXL_32;
+  if (p.kind == MXL_32 && op.m <= 32 && tiles_of(op, MXL_32) < kPlanCus * 3 / 4) p.kind = MXL_32X16;
   // A long reduction over few tiles: slices of it, of 32 steps at least, so that they save more
   // than the second kernel takes
   const int64_t blocks = tiles_of(op, p.kind);
@@ -291,13 +295,15 @@ template <int FW, int FX, bool EXACT, int KIND>
 static int mxl_launch(MxLinearArgs a, hipStream_t st) {
   constexpr MxShape t = kMxTiles[KIND];
   constexpr int stage = t.wk * (t.bn * (mx_step_bytes(FW) + 4) + t.bm * (mx_step_bytes(FX) + 4));
+  constexpr int stages = 3 * stage <= 160 * 1024 ? 3 : 2;
   if (!set_tiles(a, t.bm, t.bn, 64 * t.wm * t.wn * t.wk)) return refuse_size("ct_mx_linear_run");
-  return launch(mx_linear_kernel<FW, FX, EXACT, t.bm, t.bn, t.wm, t.wn, t.wk, t.stages>,
-                dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)a.split), 64 * t.wm * t.wn * t.wk, t.stages * stage, st, a);
+  return launch(mx_linear_kernel<FW, FX, EXACT, t.bm, t.bn, t.wm, t.wn, t.wk, stages>,
+                dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)a.split), 64 * t.wm * t.wn * t.wk, stages * stage, st, a);
 }
 template <int FW, int FX, bool EXACT>
 static int mxl_pick(const MxLinearArgs& a, int kind, hipStream_t st) {
   switch (kind) {
+    case MXL_32X16: return mxl_launch<FW, FX, EXACT, MXL_32X16>(a, st);
     case MXL_32: return mxl_launch<FW, FX, EXACT, MXL_32>(a, st);
     case MXL_64: return mxl_launch<FW, FX, EXACT, MXL_64>(a, st);
     case MXL_128X64: return mxl_launch<FW, FX, EXACT, MXL_128X64>(a, st);
