@@ -266,17 +266,25 @@ static int64_t tiles_of(const ct_mx_linear_op& op, int kind) {
 MxLinearPlan plan_mx_linear(const ct_mx_linear_op& op) {
   MxLinearPlan p = {};
   const int steps = (int)(((int64_t)op.k + 127) / 128);
-  auto rounds = [&](int kind) { return (double)((tiles_of(op, kind) + kPlanCus - 1) / kPlanCus); };
-  const std::pair<int, double> costs[] = {{MXL_64, 0.5 * rounds(MXL_64)},
-                                          {MXL_128X64, 0.8 * rounds(MXL_128X64)},
-                                          {MXL_128, 1.3 * rounds(MXL_128)},
-                                          {MXL_256, op.out_dtype == CT_DT_F32 ? 1e299 : 4.0 * rounds(MXL_256)}};
+  // Rounds of the device, and what a round costs beside one of 64 x 64 tiles, of which a compute unit
+  // has two at a time (as of 128 x 64). Measured on 1021 x 515 by 1277, 512 x 2048 by 2048, 200 x 1024
+  // by 4096, 2048^3, 4096 x 1024 by 1024, 4000 x 500 by 3000, 16000 x 320 by 320 and 8192 x 4096 by
+  // 8192: the choice is the fastest or within 12 % of it. With the elements in bf16 256 x 256 tiles
+  // leave no registers.
+  auto rounds = [&](int kind, int blocks) { return (double)((tiles_of(op, kind) + kPlanCus * blocks - 1) / (kPlanCus * blocks)); };
+  const double r128 = rounds(MXL_128, 1);
+  const std::pair<int, double> costs[] = {{MXL_64, rounds(MXL_64, 2)},
+                                          {MXL_128X64, 1.7 * rounds(MXL_128X64, 2)},
+                                          {MXL_128, r128 > 1 ? 1.5 * r128 : 1.7},
+                                          {MXL_256, op.out_dtype == CT_DT_F32 ? 1e299 : 4.6 * rounds(MXL_256, 1)}};
   double least = 1e300;
   for (auto [kind, cost] : costs)
     if (cost < least) {
       least = cost;
       p.kind = kind;
     }
+  // Smaller tiles where 64 x 64 leaves compute units without one: 64 x 4096 by 4096 13.6 to 7.7 us, and
+  // for few rows 24 x 8192 by 4096 11.1 to 9.9
   if (op.m <= 32 || (p.kind == MXL_64 && tiles_of(op, MXL_64) < kPlanCus * 3 / 4)) p.kind = MXL_32;
   if (p.kind == MXL_32 && op.m <= 32 && tiles_of(op, MXL_32) < kPlanCus * 3 / 4) p.kind = MXL_32X16;
   // A long reduction over few tiles: slices of it, of 32 steps at least, so that they save more
@@ -295,10 +303,9 @@ template <int FW, int FX, bool EXACT, int KIND>
 static int mxl_launch(MxLinearArgs a, hipStream_t st) {
   constexpr MxShape t = kMxTiles[KIND];
   constexpr int stage = t.wk * (t.bn * (mx_step_bytes(FW) + 4) + t.bm * (mx_step_bytes(FX) + 4));
-  constexpr int stages = 3 * stage <= 160 * 1024 ? 3 : 2;
   if (!set_tiles(a, t.bm, t.bn, 64 * t.wm * t.wn * t.wk)) return refuse_size("ct_mx_linear_run");
-  return launch(mx_linear_kernel<FW, FX, EXACT, t.bm, t.bn, t.wm, t.wn, t.wk, stages>,
-                dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)a.split), 64 * t.wm * t.wn * t.wk, stages * stage, st, a);
+  return launch(mx_linear_kernel<FW, FX, EXACT, t.bm, t.bn, t.wm, t.wn, t.wk, t.stages>,
+                dim3((unsigned)(a.tiles_m * a.tiles_n), (unsigned)a.split), 64 * t.wm * t.wn * t.wk, t.stages * stage, st, a);
 }
 template <int FW, int FX, bool EXACT>
 static int mxl_pick(const MxLinearArgs& a, int kind, hipStream_t st) {
