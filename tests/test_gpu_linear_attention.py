@@ -342,24 +342,31 @@ def check_norm(rows, cols, dtype, out, groups=1, residual=True, gate=True, weigh
         if pitch > cols:
             assert (y.as_strided((rows, pitch - cols), (pitch, 1), y.storage_offset() + cols) == 7.0).all()
         return
-    q, s = y.cpu(), s.cpu()
-    blocks, row = (cols + 31) // 32, L.mx_row_bytes(cols, out)
-    assert (q[:, row:] == 0xA5).all() and (s[:, L.mx_scale_bytes(cols):] == 0xA5).all()
+    row = L.mx_row_bytes(cols, out)
+    assert (y[:, row:] == 0xA5).all() and (s[:, L.mx_scale_bytes(cols):] == 0xA5).all()
+    check_rows(y, s, ref, bound, out, what)
+
+
+def check_rows(q, s, ref, bound, fmt, what):
+    """Stored rows against what rounding allows of values `bound` around ref."""
+    q, s = q.cpu(), s.cpu()
+    rows, cols = ref.shape
+    blocks = (cols + 31) // 32
     assert (s[:, blocks:L.mx_scale_bytes(cols)] == 0).all()
-    assert (codes_of(q, cols, out)[:, cols:] == 0).all()
+    assert (codes_of(q, cols, fmt)[:, cols:] == 0).all()
     full, fb = torch.zeros(rows, blocks * 32, dtype=D), torch.zeros(rows, blocks * 32, dtype=D)
     full[:, :cols], fb[:, :cols] = ref, bound
     m, i = full.abs().reshape(rows, blocks, 32).max(2)
     mb = fb.reshape(rows, blocks, 32).amax(2)
     e = s[:, :blocks].double() - 127
-    lo, hi = ((exponent((m + k * mb).clamp(min=1e-300)) - TOP_E[out]).clamp(min=-127) for k in (-1, 1))
+    lo, hi = ((exponent((m + k * mb).clamp(min=1e-300)) - TOP_E[fmt]).clamp(min=-127) for k in (-1, 1))
     assert ((e >= lo) & (e <= hi)).all(), what + ": scales"
     t, scale = full, two_to(e).repeat_interleave(32, 1)
-    got = values_of(q, s, blocks * 32, out)
+    got = values_of(q, s, blocks * 32, fmt)
     reach = (t.abs() + fb) / scale
-    step = two_to(exponent(reach.clamp(min=1e-300)).clamp(min=LOW_E[out]) - BITS[out])
+    step = two_to(exponent(reach.clamp(min=1e-300)).clamp(min=LOW_E[fmt]) - BITS[fmt])
     near = (got - t).abs() <= (step / 2 * scale + fb) * (1 + 1e-12)
-    full_scale = (reach >= TOP[out]) & (got == torch.sign(t) * TOP[out] * scale)
+    full_scale = (reach >= TOP[fmt]) & (got == torch.sign(t) * TOP[fmt] * scale)
     assert (near | full_scale).all(), what + ": elements"
 
 
