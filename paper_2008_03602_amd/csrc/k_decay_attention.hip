@@ -764,12 +764,15 @@ DecayPlan plan_decay(const ct_decay_attention_op& op, const ct_sequences& s) {
   p.step = longest <= kDecayStepTokens;
   if (p.step) return p;
   const DecayShape shape = decay_shape(op.key_dim, op.value_dim);
-  // Pieces, so that two blocks are at work on every compute unit, of 256 tokens at least: a piece's
-  // state is as many bytes as some 64 of its tokens
-  const int64_t rows = (int64_t)s.tokens * op.heads * shape.slices;
-  const int64_t piece = (rows / (2 * kPlanCus) + 63) / 64 * 64;
-  p.piece = (int)(piece < 256 ? 256 : piece);
-  if (longest <= p.piece + p.piece / 2) p.piece = 0;
+  // Pieces run every token twice, and a chunk takes two blocks on a compute unit 1.3 times one's
+  // time. So whole sequences up to 1.5 times a unit's share of the rows: 16 heads of 128 x 128, 16
+  // sequences of 512 tokens 70 us, in pieces of 256 92 us; 8 of 1024 111 and 92; one of 192 22 and 21,
+  // of 256 27 and 22. Then pieces that give each unit one block up to 128 tokens, and two above (one
+  // sequence of 1024 tokens in pieces of 64 31 us, of 256 47; of 2048 in 64 47, in 128 42, in 256 50;
+  // of 4096 in 128 61, in 256 63; of 16384 in 512 148).
+  const int64_t share = ((int64_t)s.tokens * op.heads * shape.slices / kPlanCus + 63) / 64 * 64;
+  const int64_t one = share < 64 ? 64 : share < 128 ? share : 128, two = (share / 2 + 63) / 64 * 64;
+  if (longest > 3 * (share < 128 ? 128 : share) / 2) p.piece = (int)(one > two ? one : two);
   if (!p.piece) return p;
   const SeqView v = {s.offsets, s.slots, s.tokens, s.count, s.num_slots, !s.offsets && s.count ? s.tokens / s.count : 0};
   p.pieces = seq_tiles(v, p.piece).total;
