@@ -24,11 +24,20 @@ struct NormArgs {
 
 enum { NORM_F32 = CT_DT_F32, NORM_BF16 = CT_DT_BF16, NORM_MX8 = CT_MX_E4M3, NORM_MX4 = CT_MX_E2M1 };
 
+template <int CTRL>
+__device__ __forceinline__ float lane_perm(float v) {
+  return __builtin_bit_cast(float, quad_perm<CTRL>(__builtin_bit_cast(unsigned, v)));
+}
 // The sum over the TEAM lanes (a power of two up to 64), or over a block of four waves.
 template <int TEAM>
 __device__ __forceinline__ float team_sum(float v) {
-#pragma unroll
-  for (int o = 1; o < (TEAM < 64 ? TEAM : 64); o <<= 1) v += __shfl_xor(v, o);
+  // the other lane of a pair, of four, of eight (mirrored), of sixteen: both sides add the same two numbers
+  v += lane_perm<0xB1>(v);
+  v += lane_perm<0x4E>(v);
+  v += lane_perm<0x141>(v);
+  if constexpr (TEAM > 8) v += lane_perm<0x140>(v);
+  if constexpr (TEAM > 16) v += __shfl_xor(v, 16);
+  if constexpr (TEAM > 32) v += __shfl_xor(v, 32);
   if constexpr (TEAM > 64) {
     __shared__ float part[TEAM / 64];
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
@@ -42,7 +51,7 @@ __device__ __forceinline__ float team_sum(float v) {
 
 // A team of TEAM lanes to a part, STEPS octs a lane in registers; STEPS = 0: as many as it takes,
 // read again for the outputs.
-template <typename T, int OUT, int TEAM, int STEPS>
+template <typename T, int OUT, int TEAM, int STEPS, bool EVEN>
 __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
   constexpr int TEAMS = 256 / TEAM, S = STEPS ? STEPS : 1;
   const int unit = (int)blockIdx.x * TEAMS + (int)threadIdx.x / TEAM;  // below 2^31: units are, in whole blocks
@@ -56,30 +65,51 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
   const float* w = a.w + first;
   const auto col = [&](int s) { return (s * TEAM + lane) * 8; };
 
+  const auto load = [](auto& q, const auto* p, int left) __attribute__((always_inline)) {
+    if constexpr (EVEN) q.load(p);
+    else load_oct(q, p, left);
+  };
+  const auto store = [](auto* p, const float* v, int left) __attribute__((always_inline)) {
+    store_oct(p, v, EVEN ? 8 : left);
+  };
+
   float h[S][8];
   RawOct<T> gate[S];
+  RawOct<float> weight[S];
+  const auto values = [&](const RawOct<T>& q, const RawOct<T>& r, float* v) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = q.at(i);
+    if (a.res) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += r.at(i);
+    }
+  };
   const auto read = [&](int c, float* v) __attribute__((always_inline)) {
     RawOct<T> q = {}, r = {};
-    if (c < part) {
-      load_oct<T>(q, x + c, part - c);
-      if (a.res) load_oct<T>(r, res + c, part - c);
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = a.res ? q.at(i) + r.at(i) : q.at(i);
+    if (c < part) load(q, x + c, part - c);
+    if (a.res && c < part) load(r, res + c, part - c);
+    values(q, r, v);
   };
   float ss = 0;
   if constexpr (STEPS > 0) {
-#pragma unroll
-    for (int s = 0; s < S; ++s) read(col(s), h[s]);
+    // everything is asked for before the first value is looked at: one latency, not three
+    RawOct<T> q[S], r[S];
 #pragma unroll
     for (int s = 0; s < S; ++s) {
-      gate[s] = {};
-      if (a.z && col(s) < part) load_oct<T>(gate[s], z + col(s), part - col(s));
+      q[s] = {}; r[s] = {}; gate[s] = {}; weight[s] = {};
+      if (col(s) < part) {
+        if (S <= 2 && a.w) load(weight[s], w + col(s), part - col(s));
+        load(q[s], x + col(s), part - col(s));
+        if (a.res) load(r[s], res + col(s), part - col(s));
+        if (a.z) load(gate[s], z + col(s), part - col(s));
+      }
     }
 #pragma unroll
-    for (int s = 0; s < S; ++s)
+    for (int s = 0; s < S; ++s) {
+      values(q[s], r[s], h[s]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) ss = fmaf(h[s][i], h[s][i], ss);
+    }
   } else {
     for (int s = 0; col(s) < part; ++s) {
       read(col(s), h[0]);
@@ -91,25 +121,28 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
   // sqrt and the division are rounded to nearest: one call a part's lanes
   const float scale = 1.f / __builtin_sqrtf(fmaf(ss, a.inv, a.eps));
 
-  const auto write = [&](int c, const float* v, const RawOct<T>& g) __attribute__((always_inline)) {
+  const auto write = [&](int c, const float* v, const RawOct<T>& g, RawOct<float>& wq) __attribute__((always_inline)) {
     const int left = part - c;
-    if (a.sum && left > 0) store_oct<T>(sum + c, v, left);
-    RawOct<float> wq = {};
-    if (a.w && left > 0) load_oct<float>(wq, w + c, left);
+    if (a.sum && left > 0) store(sum + c, v, left);
     float y[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      y[i] = v[i] * scale;
-      if (a.w) y[i] *= wq.at(i);
-      if (a.z) y[i] *= silu_f32(g.at(i));
+    for (int i = 0; i < 8; ++i) y[i] = v[i] * scale;
+    if (a.w) {
+      if ((STEPS == 0 || S > 2) && left > 0) load(wq, w + c, left);  // more steps: no registers to keep them in
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] *= wq.at(i);
+    }
+    if (a.z) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] *= silu_f32(g.at(i));
     }
     if constexpr (OUT == NORM_F32) {
-      if (left > 0) store_oct<float>((float*)a.y + row * a.ldy + first + c, y, left);
+      if (left > 0) store((float*)a.y + row * a.ldy + first + c, y, left);
     } else if constexpr (OUT == NORM_BF16) {
-      if (left > 0) store_oct<bf16_t>((bf16_t*)a.y + row * a.ldy + first + c, y, left);
+      if (left > 0) store((bf16_t*)a.y + row * a.ldy + first + c, y, left);
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = i < left ? y[i] : 0.f;  // also where 0 met an infinite scale
+      for (int i = 0; i < 8; ++i) y[i] = i < (EVEN ? 8 * (left > 0) : left) ? y[i] : 0.f;  // also where 0 met an infinite scale
       // lanes behind the part have nothing to write: behind the row's last block, or of the next part
       mx_store<OUT>(y, (char*)a.y + row * a.ldy, a.scales + row * a.lds,
                     c < (part + kMxBlock - 1) / kMxBlock * kMxBlock ? first + c : kNoColumn, a.cols);
@@ -117,13 +150,14 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
   };
   if constexpr (STEPS > 0) {
 #pragma unroll
-    for (int s = 0; s < S; ++s) write(col(s), h[s], gate[s]);
+    for (int s = 0; s < S; ++s) write(col(s), h[s], gate[s], weight[s]);
   } else {
     for (int s = 0; s * TEAM * 8 < part; ++s) {  // every lane, for the blocks' sake
       read(col(s), h[0]);
       gate[0] = {};
-      if (a.z && col(s) < part) load_oct<T>(gate[0], z + col(s), part - col(s));
-      write(col(s), h[0], gate[0]);
+      if (a.z && col(s) < part) load(gate[0], z + col(s), part - col(s));
+      weight[0] = {};
+      write(col(s), h[0], gate[0], weight[0]);
     }
   }
 }
@@ -132,7 +166,8 @@ template <typename T, int OUT, int TEAM, int STEPS>
 static int norm_go(const NormArgs& a, hipStream_t st) {
   const int64_t blocks = ((int64_t)a.units + 256 / TEAM - 1) / (256 / TEAM);
   if (!fits_launch(blocks, 256)) return refuse_size("ct_norm_run");
-  return launch(norm_kernel<T, OUT, TEAM, STEPS>, dim3((unsigned)blocks), 256, 0, st, a);
+  return a.part % 8 ? launch(norm_kernel<T, OUT, TEAM, STEPS, false>, dim3((unsigned)blocks), 256, 0, st, a)
+                    : launch(norm_kernel<T, OUT, TEAM, STEPS, true>, dim3((unsigned)blocks), 256, 0, st, a);
 }
 template <typename T, int OUT>
 static int norm_pick(const NormArgs& a, hipStream_t st) {
