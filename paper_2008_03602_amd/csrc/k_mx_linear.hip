@@ -229,7 +229,8 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) mx_linear_kernel(MxLinearAr
   };
 
   // Steps past the end read 0, so that STAGES - 1 of them are in flight at every wait. The
-  // barrier also says that every wave has read the stage that is filled next.
+  // barrier also says that every wave has read the stage that is filled next; a team of one wave has
+  // copied and read its stages itself, and does not wait for the others.
   static_assert((NCW + NCX + 2) * (STAGES - 2) <= 63, "the counter of loads on their way has six bits");
   if (rounds > 0) {
 #pragma unroll
@@ -237,7 +238,7 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) mx_linear_kernel(MxLinearAr
     int stage = 0;
     for (int c = 0; c < rounds; ++c) {
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NCW + NCX + 2) * (STAGES - 2)) : "memory");
-      __builtin_amdgcn_s_barrier();
+      if constexpr (WAVES > 1) __builtin_amdgcn_s_barrier();
       asm volatile("" ::: "memory");
       fetch(c + STAGES - 1, stage ? stage - 1 : STAGES - 1);
       multiply(c, stage);
