@@ -383,9 +383,12 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
     const int col = cw + 16 * c + l16;
     state_off[c] = col < a.value ? (unsigned)(row0 * a.value + col) * 4 : kOobGroup;
   }
-  f32x4* frames = a.ends + ((int64_t)unit * a.heads + head) * a.frames + (((int)blockIdx.y * 4 + wave) * NC * DT) * 64 + lane;
+  const auto frame_of = [&](int u) {
+    return a.ends + ((int64_t)u * a.heads + head) * a.frames + (((int)blockIdx.y * 4 + wave) * NC * DT) * 64 + lane;
+  };
+  f32x4* frames = frame_of(unit);
   f32x4 S[DT][NC];
-  if (OUT && !first) {
+  if (OUT && !(first && last)) {
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -399,6 +402,15 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
 #pragma unroll
         for (int e = 0; e < 4; ++e)
           S[t][c][e] = load_elem<float>(rs, state_off[c] == kOobGroup ? kOobGroup : state_off[c] + (unsigned)((row_of(t) + e) * a.value) * 4, 0);
+    // The join hands the sequence's state on to its first piece too: state_out may be state_in, and
+    // the last piece's block may write it before the first one's starts.
+    if (!OUT && first) {
+      f32x4* keep = frame_of(unit + tiles_in(r.end - begin, a.piece) - 1);
+#pragma unroll
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) keep[(t * NC + c) * 64] = S[t][c];
+    }
   }
 
   // The steps of the chunk at t, a token to a lane, from what was asked for before
@@ -684,7 +696,8 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
 }
 
 // Every piece's state at its end, from zeros (a sequence's first: from its own state), to the state
-// before each piece but the first.
+// before each piece. The place of the last one, whose end nobody needs, holds the sequence's own state
+// until then.
 __global__ void __launch_bounds__(256) decay_join_kernel(DecayArgs a) {
   const int s = fdiv((int)blockIdx.x, a.dheads), head = (int)blockIdx.x - s * a.heads;
   const int at = (int)blockIdx.y * 256 + (int)threadIdx.x;
@@ -697,6 +710,7 @@ __global__ void __launch_bounds__(256) decay_join_kernel(DecayArgs a) {
   const float* decay = a.decays + unit * a.heads + head;
   constexpr int AHEAD = 8;
   f32x4 run = *p;
+  *p = p[(pieces - 1) * step];
   for (int i = 1; i < pieces; i += AHEAD) {  // pieces i to i + 7: their ends all on their way, the last one's not needed
     f32x4 end[AHEAD];
     float d[AHEAD];

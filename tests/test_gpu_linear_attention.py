@@ -612,6 +612,21 @@ def test_attention_of_one_long_prompt(dtype):
     check_attention([1200, 1300], 1, 1, 128, 40, dtype, delta=False, seed=3, hint=0)
 
 
+@pytest.mark.parametrize("dtype", [B, F])
+def test_attention_of_pieces_with_states_in_place(dtype):
+    """The state that the first piece of a sequence reads is the one that its last piece writes."""
+    check_attention([4000], 16, 16, 16, 16, dtype, in_place=True, seed=11)
+    check_attention([900, 3, 0, 260, 64, 1], 8, 2, 128, 130, dtype, in_place=True, seed=12, unused=(4,), lead=3, tail=2)
+    check_attention([520] * 3, 4, 4, 40, 72, dtype, in_place=True, uniform=True, seed=13)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+def test_attention_around_the_lengths_of_pieces(dtype):
+    for n in (127, 128, 192, 193, 256, 257, 320):
+        check_attention([n], 2, 1, 64, 40, dtype, seed=n)
+        check_attention([n, 1, n - 64, 64], 1, 1, 24, 65, dtype, seed=n, in_place=True)
+
+
 def run_plain(s, lens, heads, groups, key, value, dtype, state=None, hint=None):
     off = torch.tensor([sum(lens[:i]) for i in range(len(lens) + 1)], dtype=torch.int32).cuda()
     op = L.make_decay_attention(heads, groups, key, value, CODE[dtype], L.DT_F32, scale=1.0)
