@@ -373,6 +373,13 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
   const T* k = (const T*)a.k + (int64_t)group * a.key;
   const T* v = (const T*)a.v + (int64_t)head * a.value + c0;
 
+  // What delta holds for the chunk at t, a token to a lane, as it lies there: no wait until its steps are made
+  const auto ask = [&](int t) __attribute__((always_inline)) {
+    if (!a.delta || t >= end) return 0u;
+    const int64_t at = min((int64_t)t + lane, (int64_t)end - 1) * a.lddelta + head;
+    return a.delta_bf16 ? (unsigned)((const uint16_t*)a.delta)[at] : ((const unsigned*)a.delta)[at];
+  };
+  unsigned delta = ask(tile_end(begin, end, wave * C));  // first: loads come back in their order
   const auto fill = [&](int t, int half) __attribute__((always_inline)) {
     const int rows = min(end - t, C);
     if constexpr (OUT) fill_tile<T, KB, C, ALIGNED>(tq, q + t * a.ldq, a.ldq, rows, a.key);
@@ -404,14 +411,20 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
 #pragma unroll
       for (int c = 0; c < NC; ++c) S[t][c] = frames[(t * NC + c) * 64];
   } else {
-    const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.state_in + state_at, first && slot >= 0 && a.state_in ? state_bytes : 0);
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
-      for (int c = 0; c < NC; ++c)
+      for (int c = 0; c < NC; ++c) S[t][c] = f32x4{};
+    if (first && slot >= 0 && a.state_in) {
+      const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.state_in + state_at, state_bytes);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          S[t][c][e] = load_elem<float>(rs, state_off[c] == kOobGroup ? kOobGroup : state_off[c] + (unsigned)((row_of(t) + e) * a.value) * 4, 0);
+      for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            S[t][c][e] = load_elem<float>(rs, state_off[c] == kOobGroup ? kOobGroup : state_off[c] + (unsigned)((row_of(t) + e) * a.value) * 4, 0);
+    }
     // The join hands the sequence's state on to its first piece too: state_out may be state_in, and
     // the last piece's block may write it before the first one's starts.
     if (!OUT && first) {
@@ -423,12 +436,10 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
     }
   }
 
-  // The steps of the chunk at t, a token to a lane, from what was asked for before
-  const auto has = [&](int t) { return lane < C && t < end && t + lane < end; };
-  const auto ask = [&](int t) { return has(t) ? delta_of(a, t + lane, head) : 0.f; };
-  const auto make_steps = [&](int t, float delta, Steps<C>& to) __attribute__((always_inline)) {
-    const bool mine = has(t);
-    const Step s = step_of(a, delta, bias, rate);
+  // The steps of the chunk at t from what was asked for before
+  const auto make_steps = [&](int t, unsigned delta, Steps<C>& to) __attribute__((always_inline)) {
+    const bool mine = lane < C && t < end && t + lane < end;
+    const Step s = step_of(a, __builtin_bit_cast(float, a.delta_bf16 ? delta << 16 : delta), bias, rate);
     double G = mine ? (double)s.l * 1.4426950408889634 : 0.;
 #pragma unroll
     for (int o = 1; o < C; o <<= 1) {
@@ -451,7 +462,6 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
   };
 
   double total = 0;
-  float delta = ask(tile_end(begin, end, wave * C));
   int turn = 0;
 #pragma unroll 1
   for (int t = begin; t < end; turn = (turn + 1) & 7) {
