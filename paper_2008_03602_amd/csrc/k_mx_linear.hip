@@ -292,6 +292,21 @@ MxLinearPlan plan_mx_linear(const ct_mx_linear_op& op) {
       least = cost;
       p.kind = kind;
     }
+  // Up to 64 rows or columns past whole 256 x 256 tiles would take the device another round; they go
+  // apart where that is less: 8192 x 2048 by 8208 186 to 177 us, 4096 x 4096 by 8224 203 to 158,
+  // 4100 x 4096 by 8200 206 to 164, 8192 x 4096 by 2064 116 to 87, 4096 x 512 by 4100 24.5 to 26.2
+  if (op.out_dtype == CT_DT_BF16)
+    for (int tails = 1; tails < 4; ++tails) {
+      const int tm = tails & 1 ? op.m % 256 : 0, tn = tails & 2 ? op.n % 256 : 0;
+      if (tm > 64 || tn > 64 || (tails & 1 && !tm) || (tails & 2 && !tn)) continue;
+      const int64_t tiles = (((int64_t)op.m - tm + 255) / 256) * (((int64_t)op.n - tn + 255) / 256);
+      const double cost = 4.6 * (double)((tiles + kPlanCus - 1) / kPlanCus) + (tm != 0) + (tn != 0);
+      if (!tiles || cost >= least) continue;
+      least = cost;
+      p.kind = MXL_256;
+      p.tail_m = tm;
+      p.tail_n = tn;
+    }
   // Smaller tiles where 64 x 64 leaves compute units without one: 64 x 4096 by 4096 13.6 to 7.7 us, and
   // for few rows 24 x 8192 by 4096 11.1 to 9.5
   if (op.m <= 32 || (p.kind == MXL_64 && tiles_of(op, MXL_64) < kPlanCus * 3 / 4)) p.kind = MXL_32;
@@ -335,6 +350,28 @@ static int mxl_sums(const MxLinearArgs& a, int kind, hipStream_t st) {
 }
 
 int launch_mx_linear(const ct_mx_linear_op& op, const MxLinearPlan& p, const MxLinearArrays& v, void* stream) {
+  if (p.tail_m || p.tail_n) {
+    const int64_t o = elem_bytes(op.out_dtype);
+    const auto part = [&](int m0, int m, int n0, int n, bool whole) {
+      ct_mx_linear_op sub = op;
+      sub.m = m;
+      sub.n = n;
+      MxLinearPlan q = p;
+      q.tail_m = q.tail_n = 0;
+      if (!whole) q.kind = plan_mx_linear(sub).kind;
+      const int64_t at = m0 * op.ldy + n0, rat = m0 * op.ldr + n0;
+      const MxLinearArrays a = {(const char*)v.x + m0 * op.ldx, (const char*)v.xs + m0 * op.ldxs,
+                                (const char*)v.w + n0 * op.ldw, (const char*)v.ws + n0 * op.ldws,
+                                v.bias ? v.bias + n0 : nullptr, op.res ? (const char*)v.res + rat * o : nullptr,
+                                (char*)v.y + at * o, nullptr};
+      return launch_mx_linear(sub, q, a, stream);
+    };
+    const int m = op.m - p.tail_m, n = op.n - p.tail_n;
+    int rc = part(0, m, 0, n, true);
+    if (!rc && p.tail_n) rc = part(0, op.m, n, p.tail_n, false);
+    if (!rc && p.tail_m) rc = part(m, p.tail_m, 0, n, false);
+    return rc;
+  }
   MxLinearArgs a = {};
   a.x = (const char*)v.x; a.xs = (const unsigned char*)v.xs;
   a.w = (const char*)v.w; a.wsc = (const unsigned char*)v.ws;

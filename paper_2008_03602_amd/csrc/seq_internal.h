@@ -72,6 +72,7 @@ struct MxLinearPlan {
   int kind;           // the kernel (k_mx_linear.hip)
   int split;          // slices of the reduction, each with partial sums of its own
   int per_split;      // steps of 128 elements in a slice
+  int tail_m, tail_n; // last rows and columns of y that a launch of their own computes
   int64_t ws_floats;  // split * m * n where the reduction is split
 };
 MxLinearPlan plan_mx_linear(const ct_mx_linear_op& op);

@@ -274,6 +274,11 @@ def test_product_of_split_reductions():
             check_product(20, 24, 16500, fx, fw, out, act=2, res=2, seed=5)
 
 
+def test_product_of_rows_and_columns_past_large_tiles():
+    for m, n, res, in_place in ((4096, 4099, 1, True), (4100, 4096, 2, False), (4104, 4136, 1, False)):
+        check_product(m, n, 160, L.MX_E4M3, L.MX_E2M1, B, act=3, res=res, seed=m, yp=n + 5, sp=12, in_place=in_place)
+
+
 def test_product_without_a_reduction_is_its_epilogue():
     for out in (B, F):
         b, r = normal(gen(1), 40), normal(gen(2), 9, 40, dtype=out)
