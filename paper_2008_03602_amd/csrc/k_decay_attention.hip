@@ -271,8 +271,9 @@ __device__ __forceinline__ typename Mat<T>::Frag read_cols(const char* tile, int
 }
 
 // ROWS rows of a tile of BYTES each from memory, 16 bytes a lane straight into LDS where the rows
-// lie on 16 bytes (wait_copies() and a barrier before they are read), else element by element
-// through registers. Elements past `cols` and rows past `rows` read 0.
+// lie on 16 bytes (wait_copies() and a barrier before they are read), else through registers; rows
+// shorter than that element by element (8192 tokens of 8 heads of 250 x 130: 425 us with all of them so,
+// 238 in groups of 16 bytes at any address). Elements past `cols` and rows past `rows` read 0.
 template <typename T, int BYTES, int ROWS, bool ALIGNED>
 __device__ __forceinline__ void fill_tile(char* tile, const T* base, int64_t ld, int rows, int cols) {
   constexpr int GROUPS = BYTES / 16, N = ROWS * GROUPS / 256, E = 16 / (int)sizeof(T);
@@ -292,6 +293,31 @@ __device__ __forceinline__ void fill_tile(char* tile, const T* base, int64_t ld,
       int col;
       const unsigned off = offset(i, &col);
       __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)(mine + i * 4096), 16, (int)(col < cols ? off : kOobGroup), 0, 0, 0);
+    }
+  } else if (cols >= E) {
+    // A row's last group comes from the 16 bytes that end with the row, turned down; lanes without a
+    // group read the tile's first
+    const int bits = (E - cols % E) % E * 8 * (int)sizeof(T);
+    u32x4 w[N];
+    int left[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int col;
+      offset(i, &col);
+      left[i] = cols - col;
+      const int row = left[i] > 0 ? (i * 256 + (int)threadIdx.x) / GROUPS : 0;
+      w[i] = *(const u32x4_any*)(base + row * ld + (left[i] > 0 ? min(col, cols - E) : 0));
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      if (left[i] < E) {
+        typedef uint64_t u64x2 __attribute__((ext_vector_type(2)));
+        u64x2 q = __builtin_bit_cast(u64x2, w[i]);
+        if (bits >= 64) q = (u64x2){q.y >> (bits - 64), 0};
+        else if (bits) q = (u64x2){q.x >> bits | q.y << (64 - bits), q.y >> bits};
+        w[i] = left[i] > 0 ? __builtin_bit_cast(u32x4, q) : u32x4{};
+      }
+      *(u32x4*)(tile + (i * 256 + (int)threadIdx.x) * 16) = w[i];
     }
   } else {
 #pragma unroll 1
@@ -686,6 +712,8 @@ __global__ void __launch_bounds__(256, DK * (int)sizeof(T) > 512 || (!ALIGNED &&
                                                     ro, (int)at, 0, 0);
             else
               __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, O[i][c]), ro, (int)at, 0, 0);
+          } else if (row && col + 4 <= a.value) {
+            store_quad4((T*)a.o + (t + i * 16 + l16) * a.ldo + (int64_t)head * a.value + col, (const float*)&O[i][c], false);
           } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)

@@ -14,7 +14,6 @@ constexpr int mx_scales(int cols) { return (mx_blocks(cols) + 3) / 4 * 4; }
 struct Oct {
   float v[8];
 };
-typedef u32x4 u32x4_any __attribute__((aligned(2)));
 // Eight elements as they lie in memory, at any element's address: asked for early, looked at late.
 template <typename T>
 struct RawOct {

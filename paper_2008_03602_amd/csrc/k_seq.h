@@ -63,6 +63,7 @@ struct Quad {
 // Four elements of a row that all exist, in one access wherever the row lies.
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 typedef u32x2 u32x2_any __attribute__((aligned(2)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
 template <typename O>
 __device__ __forceinline__ Quad load_quad4(const O* p) {
   if constexpr (sizeof(O) == 2) {
