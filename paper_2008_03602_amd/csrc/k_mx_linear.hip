@@ -295,7 +295,7 @@ MxLinearPlan plan_mx_linear(const ct_mx_linear_op& op) {
   // Up to 64 rows or columns past whole 256 x 256 tiles would take the device another round; they go
   // apart where that is less: 8192 x 2048 by 8208 186 to 177 us, 4096 x 4096 by 8224 203 to 158,
   // 4100 x 4096 by 8200 206 to 164, 8192 x 4096 by 2064 116 to 87, 4096 x 512 by 4100 24.5 to 26.2
-  if (op.out_dtype == CT_DT_BF16)
+  if (op.out_dtype == CT_DT_BF16 && op.m > 32)
     for (int tails = 1; tails < 4; ++tails) {
       const int tm = tails & 1 ? op.m % 256 : 0, tn = tails & 2 ? op.n % 256 : 0;
       if (tm > 64 || tn > 64 || (tails & 1 && !tm) || (tails & 2 && !tn)) continue;
