@@ -692,9 +692,11 @@ int ct_mx_linear_run(const ct_mx_linear_op *op, const void *x, const void *x_sca
  * x, res and z (rows x cols) in `dtype`, w (cols) fp32; res, w and z may be NULL.
  * sum (optional) takes h, rounded to `dtype`; y is of type `out`, a CT_DT_* or
  * microscaled rows (CT_MX_*, ldy then in bytes; parts are whole blocks of 32
- * where there are several), and comes from h before it is rounded. h^2 is summed
- * in fp32, and a part whose sum is past its range counts as infinite. An output
- * may be an input itself where type and pitch are the same. */
+ * where there are several), and comes from h before it is rounded to `dtype`: from
+ * x + res in fp32, whose squares are summed in fp64. Elements and scales of
+ * microscaled rows are those of the formula's own values, also where these lie
+ * beside the border of a rounding. An output may be an input itself where type
+ * and pitch are the same. */
 typedef struct ct_norm_op {
     int32_t rows, cols, groups;
     int32_t dtype;  /* CT_DT_*             */

@@ -75,17 +75,20 @@ template <int CTRL>
 __device__ __forceinline__ unsigned quad_perm(unsigned v) {
   return (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
 }
-// The block's scale byte from each lane's eight values. Magnitudes are compared as their bits, in
-// whose order infinities and NaN come last and the exponent is on top: floor(log2 m) + 127 of a
-// normal m, 0 of the others, whose scale is the least one anyway.
-template <int FORMAT>
-__device__ __forceinline__ unsigned mx_scale(const float* v) {
+// The block's largest magnitude from each lane's eight values, as its bits, in whose order infinities
+// and NaN come last and the exponent is on top.
+__device__ __forceinline__ unsigned mx_largest(const float* v) {
   unsigned m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, __builtin_bit_cast(unsigned, v[i]) & 0x7FFFFFFFu);
   m = max(m, quad_perm<0xB1>(m));  // lanes 1 0 3 2
-  m = max(m, quad_perm<0x4E>(m));  // lanes 2 3 0 1
-  const int e = (int)(m >> 23);
+  return max(m, quad_perm<0x4E>(m));  // lanes 2 3 0 1
+}
+// The scale byte of a block by its largest magnitude: the exponent's bits are floor(log2 m) + 127 of a
+// normal m, 0 of the others, whose scale is the least one anyway.
+template <int FORMAT>
+__device__ __forceinline__ unsigned mx_scale(unsigned largest) {
+  const int e = (int)(largest >> 23);
   return e == 255 ? 255u : (unsigned)max(e - (FORMAT == CT_MX_E4M3 ? 8 : 2), 0);
 }
 // 1 / 2^(s - 127), a normal number for every s that mx_scale gives (246 at most); of s = 255
@@ -95,12 +98,11 @@ __device__ __forceinline__ float mx_inverse(unsigned s) { return __builtin_bit_c
 __device__ __forceinline__ float mx_scale_value(unsigned s) {
   return __builtin_bit_cast(float, s == 255 ? 0x7FC00000u : s == 0 ? 0x00400000u : s << 23);
 }
-// Eight elements of a lane: two words of e4m3, or one of e2m1. Values over the scale, which is
-// exact; the conversion rounds to nearest even. It saturates e2m1, and e4m3 past 464 would be
-// NaN, so those are held at 448 before it.
+// Eight elements of a lane: two words of e4m3, or one of e2m1. Values over the scale (times `inv`, of
+// mx_inverse), which is exact; the conversion rounds to nearest even. It saturates e2m1, and e4m3 past
+// 464 would be NaN, so those are held at 448 before it.
 template <int FORMAT>
-__device__ __forceinline__ u32x2 mx_elements(const float* v, unsigned scale) {
-  const float inv = mx_inverse(scale);
+__device__ __forceinline__ u32x2 mx_elements(const float* v, float inv) {
   float t[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) t[i] = v[i] * inv;
@@ -126,23 +128,17 @@ __device__ __forceinline__ u32x2 mx_elements(const float* v, unsigned scale) {
     return (u32x2){w, 0};
   }
 }
-// A column behind every row's blocks, for lanes with nothing to write.
-constexpr int kNoColumn = 0x7FFFFFE0;
-// Eight values (0 past the row's end) of column `col` on (a multiple of 8) of a row of `cols`, to
-// the row's elements and scales. The four lanes of a block call this together, those with
-// nothing to write too (col past the last block).
+// A lane's elements from column `col` on (a multiple of 8) of a row of `cols`, and their block's scale,
+// to the row.
 template <int FORMAT>
-__device__ __forceinline__ void mx_store(const float* v, char* q, unsigned char* scales, int col, int cols) {
-  const unsigned s = mx_scale<FORMAT>(v);
-  const u32x2 w = mx_elements<FORMAT>(v, s);
-  const int block = col / kMxBlock, blocks = mx_blocks(cols);
-  if (block >= blocks) return;
+__device__ __forceinline__ void mx_write(u32x2 w, unsigned scale, char* q, unsigned char* scales, unsigned col, int cols) {
   if constexpr (FORMAT == CT_MX_E4M3) *(u32x2*)(q + col) = w;
   else *(unsigned*)(q + col / 2) = w.x;
   if (col % kMxBlock == 0) {
-    scales[block] = (unsigned char)s;
+    const unsigned block = col / kMxBlock, blocks = (unsigned)mx_blocks(cols);
+    scales[block] = (unsigned char)scale;
     if (block == blocks - 1)
-      for (int b = blocks; b < mx_scales(cols); ++b) scales[b] = 0;
+      for (int b = (int)blocks; b < mx_scales(cols); ++b) scales[b] = 0;
   }
 }
 

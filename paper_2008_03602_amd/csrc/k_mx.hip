@@ -40,7 +40,9 @@ __global__ void __launch_bounds__(kMxThreads) mx_quantise_kernel(MxArgs a) {
   float v[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = r.at(i);
-  mx_store<FORMAT>(v, a.q + row * a.ldq, a.scales + row * a.lds, col, a.cols);
+  const unsigned scale = mx_scale<FORMAT>(mx_largest(v));  // the four lanes of a block together
+  mx_write<FORMAT>(mx_elements<FORMAT>(v, mx_inverse(scale)), scale, a.q + row * a.ldq, a.scales + row * a.lds,
+                   (unsigned)col, a.cols);
 }
 
 template <typename T, int FORMAT>
