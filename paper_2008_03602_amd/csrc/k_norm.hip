@@ -190,6 +190,18 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
   ss = team_sum<TEAM>(ss);
   const double scale64 = rsqrt_f64(fma(ss, a.inv, (double)a.eps));
   const float scale = (float)scale64;
+  const auto scaled = [&](const float* v, float* y) __attribute__((always_inline)) {
+    if (a.eps == 0.f) {  // a part of tiny values may have a scale past fp32: it is lifted first, exactly
+      asm volatile("");
+      const bool tiny = scale64 > 0x1p100;
+      const float lift = tiny ? 0x1p100f : 1.f, rest = tiny ? (float)(scale64 * 0x1p-100) : scale;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = v[i] * lift * rest;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i] = v[i] * scale;
+    }
+  };
 
   // Eight outputs of 8 or 4 bits with their block's scale. Lanes behind the part have nothing to write:
   // behind the row's last block, or of the next part.
@@ -207,8 +219,7 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
   const auto write = [&](int c, const float* v, const RawOct<T>& g, RawOct<float>& wq) __attribute__((always_inline)) {
     const int left = part - c;
     float y[8], z[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = v[i] * scale;
+    scaled(v, y);
     if (a.w) {
       asm volatile("");
       if (STEPS == 0 || S > 2) load(wq, w, c);  // more steps: no registers to keep them in

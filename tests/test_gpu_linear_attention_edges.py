@@ -6,7 +6,7 @@ import torch
 
 from paper_2008_03602_amd import _lib as L
 from gpu_util import device_ready, note
-from test_gpu_linear_attention import B, CODE, D, F, FORMATS, codes_of, mx_buffers, quantise64
+from test_gpu_linear_attention import B, CODE, D, F, FORMATS, check_norm, codes_of, mx_buffers, quantise64
 from test_gpu_sequence import gen, normal, stream
 
 pytestmark = pytest.mark.gpu
@@ -47,3 +47,21 @@ def test_norm_rounds_as_the_formula_beside_the_borders(rows, cols, groups, resid
     assert torch.equal(s.cpu().long(), scale), "%d scales" % int((s.cpu().long() != scale).sum())
     got = codes_of(q.cpu(), cols, fmt)
     assert torch.equal(got, code), "%d elements" % int((got != code).sum())
+
+
+@pytest.mark.parametrize("out", [B, F, *FORMATS])
+@pytest.mark.parametrize("dtype", [B, F])
+def test_norm_of_tiny_values_without_eps(dtype, out):
+    """Values whose squares are below fp32, and some whose reciprocal root mean square is above it."""
+    for std in (1e-21, 1e-25, 1e-36, 1e-38, *((1e-42,) if dtype == F else ())):
+        for rows, cols, groups in ((5, 96, 3), (3, 515, 1), (2, 4100, 1), (2, 20000, 1)):
+            if groups == 1 or out in (B, F) or cols // groups % 32 == 0:
+                check_norm(rows, cols, dtype, out, groups, std=std, eps=0.0, seed=cols)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+def test_norm_of_huge_values(dtype):
+    """Values whose squares are past fp32 and whose norm is not."""
+    for std in (1e21, 1e36):
+        check_norm(3, 200, dtype, F, std=std, residual=False, seed=2)
+        check_norm(3, 200, dtype, L.MX_E4M3, std=std, residual=False, seed=2)
