@@ -11,7 +11,10 @@
 // largest (measured: 2^-13 of it survives beside it and 2^-14 does not, across eights all 23 bits
 // do), 1.5e-5 of the result for two operands of normal values in e4m3, which an output of bf16
 // (2^-9) does not show. For fp32 outputs the elements are turned into bf16, which holds each with
-// its scale exactly, and multiplied by the 16-bit instruction: products exact, sums in fp32.
+// its scale exactly while both are of normal size, and multiplied by the 16-bit instruction: products
+// exact, sums in fp32. A wave that meets a block whose scale would leave bf16 (bytes below 10 or above 246
+// of e4m3, 2 and 252 of e2m1, in a block that is not all 0) sums its part of the tile again, of elements
+// without their scales, and scales each block's sum: the other operand's scale may bring it back.
 //
 // Measured, 8-bit x by 4-bit w: 8192 x 4096 by 8192 with SiLU 236-250 us (2.2-2.3 PFLOP/s; 227
 // without the epilogue), bound by the card's power; 24 x 8192 by 4096 9.5 us, 1.9 TB/s, bound by the
@@ -44,25 +47,22 @@ template <int FORMAT>
 struct MxFrag {
   u32x4 lo, hi;  // e2m1: hi is not used
 };
-// Four words of eight bf16 each from 32 elements with their scale.
+// Eight elements, of one word (e2m1) or two, with their scale in bf16.
 template <int FORMAT>
-__device__ __forceinline__ bf16x8 mx_bf16(const MxFrag<FORMAT>& f, int c, unsigned scale) {
+__device__ __forceinline__ bf16x8 mx_eight(unsigned w0, unsigned w1, unsigned scale) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   const float s = __builtin_bit_cast(float, scale << 23);  // the conversion takes the exponent's bits as they are
   bf16x2 p[4];
   if constexpr (FORMAT == CT_MX_E4M3) {
-    const u32x4 q = c < 2 ? f.lo : f.hi;
-    const unsigned w0 = q[c % 2 * 2], w1 = q[c % 2 * 2 + 1];
     p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s, false);
     p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, s, true);
     p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, false);
     p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, s, true);
   } else {
-    const unsigned w = f.lo[c];
-    p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0);
-    p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1);
-    p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2);
-    p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3);
+    p[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w0, s, 0);
+    p[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w0, s, 1);
+    p[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w0, s, 2);
+    p[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w0, s, 3);
   }
   bf16x8 r;
 #pragma unroll
@@ -72,12 +72,46 @@ __device__ __forceinline__ bf16x8 mx_bf16(const MxFrag<FORMAT>& f, int c, unsign
   }
   return r;
 }
+// Eight of a lane's 32 elements, number c of them, with their scale.
+template <int FORMAT>
+__device__ __forceinline__ bf16x8 mx_bf16(const MxFrag<FORMAT>& f, int c, unsigned scale) {
+  if constexpr (FORMAT == CT_MX_E4M3) {
+    const u32x4 q = c < 2 ? f.lo : f.hi;
+    return mx_eight<FORMAT>(q[c % 2 * 2], q[c % 2 * 2 + 1], scale);
+  } else {
+    return mx_eight<FORMAT>(f.lo[c], 0, scale);
+  }
+}
+// Eight elements as they lie at byte `off` of rows.
+template <int FORMAT>
+__device__ __forceinline__ u32x2 mx_raw(__amdgpu_buffer_rsrc_t rows, unsigned off) {
+  if constexpr (FORMAT == CT_MX_E4M3)
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rows, (int)off, 0, 0));
+  else
+    return (u32x2){(unsigned)__builtin_amdgcn_raw_buffer_load_b32(rows, (int)off, 0, 0), 0};
+}
+__device__ __forceinline__ unsigned mx_word(__amdgpu_buffer_rsrc_t rows, unsigned off) {
+  return (unsigned)__builtin_amdgcn_raw_buffer_load_b32(rows, (int)off, 0, 0);
+}
 template <int FORMAT>
 __device__ __forceinline__ i32x8 mx_operand(const MxFrag<FORMAT>& f) {
   if constexpr (FORMAT == CT_MX_E4M3)
     return __builtin_bit_cast(i32x8, __builtin_shufflevector(f.lo, f.hi, 0, 1, 2, 3, 4, 5, 6, 7));
   else
     return __builtin_bit_cast(i32x8, __builtin_shufflevector(f.lo, f.lo, 0, 1, 2, 3, -1, -1, -1, -1));
+}
+// Whether bf16 does not hold every element of a block with this scale as a normal number; 255 is NaN.
+template <int FORMAT>
+__device__ __forceinline__ bool mx_far(int scale) {
+  constexpr int LOW = FORMAT == CT_MX_E4M3 ? 10 : 2, HIGH = FORMAT == CT_MX_E4M3 ? 246 : 252;
+  return (unsigned)(scale - LOW) > (unsigned)(HIGH - LOW);
+}
+// Whether that matters for a block: not where every element is 0.
+template <int FORMAT>
+__device__ __forceinline__ bool mx_counts(const MxFrag<FORMAT>& f, int scale) {
+  unsigned bits = f.lo.x | f.lo.y | f.lo.z | f.lo.w;
+  if constexpr (FORMAT == CT_MX_E4M3) bits |= f.hi.x | f.hi.y | f.hi.z | f.hi.w;
+  return mx_far<FORMAT>(scale) && (scale == 255 || (bits & (FORMAT == CT_MX_E4M3 ? 0x7F7F7F7Fu : 0x77777777u)) != 0);
 }
 constexpr int mx_code(int format) { return format == CT_MX_E4M3 ? 0 : 4; }  // of the instruction
 
@@ -101,8 +135,11 @@ __device__ __forceinline__ MxRows mx_rows(const void* p, int64_t ld, int r0, int
 // the 16 rows of a fragment lie in distinct banks. Every address is in bounds: rows are a buffer
 // that ends with the last of the tile's, and rows, groups and scales past the end have an offset
 // past it, and read 0.
+// Waves of a SIMD that the registers leave room for: three blocks of 128 x 128 fit LDS.
+constexpr int mx_waves(bool exact, int tile) { return exact && tile == 128 * 128 ? 3 : 1; }
+
 template <int FW, int FX, bool EXACT, int BM, int BN, int WM, int WN, int WK, int STAGES>
-__global__ void __launch_bounds__(64 * WM * WN * WK) mx_linear_kernel(MxLinearArgs a) {
+__global__ void __launch_bounds__(64 * WM * WN * WK, mx_waves(EXACT, BM * BN)) mx_linear_kernel(MxLinearArgs a) {
   constexpr int WAVES = WM * WN, RBW = mx_step_bytes(FW), RBX = mx_step_bytes(FX);
   constexpr int RPCW = 1024 / RBW, RPCX = 1024 / RBX;  // rows of one copy
   constexpr int NCW = BN / RPCW / WAVES, NCX = BM / RPCX / WAVES;  // copies of a wave
@@ -144,8 +181,9 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) mx_linear_kernel(MxLinearAr
     const int r = row_of(RBX, i);
     off_x[i] = m0 + r < a.m ? (unsigned)(r * (int)a.ldx + first(RBX, i)) : kOobGroup;
   }
-  const unsigned off_sw = n0 + wave * SW + lane < a.n ? (unsigned)((wave * SW + lane) * (int)a.ldws) : kOobGroup;
-  const unsigned off_sx = m0 + wave * SX + lane < a.m ? (unsigned)((wave * SX + lane) * (int)a.ldxs) : kOobGroup;
+  // Rows past the last have its scales: their elements are 0, and no scale is there that the operands do not have.
+  const unsigned off_sw = (unsigned)(min(wave * SW + lane, a.n - 1 - n0) * (int)a.ldws);
+  const unsigned off_sx = (unsigned)(min(wave * SX + lane, a.m - 1 - m0) * (int)a.ldxs);
 
   auto fetch = [&](int c, int stage) __attribute__((always_inline)) {
     const int step = begin + c * WK + team;
@@ -184,26 +222,37 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) mx_linear_kernel(MxLinearAr
   };
   const int pw0 = place(RBW, 0), pw1 = place(RBW, 1), px0 = place(RBX, 0), px1 = place(RBX, 1);
   f32x4 acc[TN][TM] = {};
+  bool again = false;  // exact sums: bf16 does not hold all elements of the wave's rows
   auto multiply = [&](int c, int stage) __attribute__((always_inline)) {
     const char* base = lds + stage * STAGE + team * TEAM;
     const char *sw = base + wn * RBW, *sx = base + AT_X + wm * RBX;
     const unsigned char *cw = (const unsigned char*)base + AT_SW + (wn + lrow) * 4 + kg,
                         *cx = (const unsigned char*)base + AT_SX + (wm + lrow) * 4 + kg;
-    // scales behind a row's last block are not read as such: their elements are 0
-    const bool real = (begin + c * WK + team) * 4 + kg < a.blocks;
+    // scales behind a row's last block, or the slice's, are not read as such: their elements are 0
+    const bool real = (begin + c * WK + team) * 4 + kg < min(a.blocks, end * 4);
+    const auto read_w = [&](int i) __attribute__((always_inline)) {
+      MxFrag<FW> f;
+      f.lo = *(const u32x4*)(sw + i * 16 * RBW + pw0);
+      if constexpr (FW == CT_MX_E4M3) f.hi = *(const u32x4*)(sw + i * 16 * RBW + pw1);
+      return f;
+    };
+    const auto read_x = [&](int j) __attribute__((always_inline)) {
+      MxFrag<FX> f;
+      f.lo = *(const u32x4*)(sx + j * 16 * RBX + px0);
+      if constexpr (FX == CT_MX_E4M3) f.hi = *(const u32x4*)(sx + j * 16 * RBX + px1);
+      return f;
+    };
     MxFrag<FW> fw[TN];
     MxFrag<FX> fx[TM];
     int ew[TN], ex[TM];
 #pragma unroll
     for (int i = 0; i < TN; ++i) {
-      fw[i].lo = *(const u32x4*)(sw + i * 16 * RBW + pw0);
-      if constexpr (FW == CT_MX_E4M3) fw[i].hi = *(const u32x4*)(sw + i * 16 * RBW + pw1);
+      fw[i] = read_w(i);
       ew[i] = cw[i * 64];
     }
 #pragma unroll
     for (int j = 0; j < TM; ++j) {
-      fx[j].lo = *(const u32x4*)(sx + j * 16 * RBX + px0);
-      if constexpr (FX == CT_MX_E4M3) fx[j].hi = *(const u32x4*)(sx + j * 16 * RBX + px1);
+      fx[j] = read_x(j);
       ex[j] = cx[j * 64];
     }
     if (!real) {
@@ -224,6 +273,26 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) mx_linear_kernel(MxLinearAr
 #pragma unroll
           for (int i = 0; i < TN; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bw[i], bx, acc[i][j], 0, 0, 0);
         }
+      }
+      int low_w = ew[0], high_w = ew[0], low_x = ex[0], high_x = ex[0];
+#pragma unroll
+      for (int i = 1; i < TN; ++i) {
+        low_w = min(low_w, ew[i]);
+        high_w = max(high_w, ew[i]);
+      }
+#pragma unroll
+      for (int j = 1; j < TM; ++j) {
+        low_x = min(low_x, ex[j]);
+        high_x = max(high_x, ex[j]);
+      }
+      if (__ballot(mx_far<FW>(low_w) || mx_far<FW>(high_w) || mx_far<FX>(low_x) || mx_far<FX>(high_x))) {
+        asm volatile("" ::: "memory");  // the elements are read again, or they would stay in registers until here
+        bool counts = false;
+#pragma unroll
+        for (int i = 0; i < TN; ++i) counts |= mx_counts<FW>(read_w(i), ew[i]);
+#pragma unroll
+        for (int j = 0; j < TM; ++j) counts |= mx_counts<FX>(read_x(j), ex[j]);
+        again |= __ballot(counts) != 0;
       }
     } else {
       constexpr int CW = mx_code(FW), CX = mx_code(FX);
@@ -251,6 +320,48 @@ __global__ void __launch_bounds__(64 * WM * WN * WK) mx_linear_kernel(MxLinearAr
       fetch(c + STAGES - 1, stage ? stage - 1 : STAGES - 1);
       multiply(c, stage);
       stage = stage == STAGES - 1 ? 0 : stage + 1;
+    }
+  }
+  if constexpr (EXACT) {
+    if (again) {
+      // The wave's sums once more, a tile at a time and a block, 32 elements, with each instruction: the tiles
+      // that are done wait where the sums of every wave are, and nothing else needs registers that others do not.
+      const auto at = [&](int row, int64_t ld, int block, int bytes) { return (unsigned)(row * (int)ld + block * bytes * 4 + kg * bytes); };
+#pragma unroll
+      for (int i = 0; i < TN; ++i)
+#pragma unroll
+        for (int j = 0; j < TM; ++j) {
+          const int of_w = wn + i * 16 + lrow, of_x = wm + j * 16 + lrow, to = wn + i * 16 + kg * 4;
+          const bool has_w = n0 + of_w < a.n, has_x = m0 + of_x < a.m;
+          f32x4 total = {};
+#pragma unroll 1
+          for (int step = begin + team; step < end; step += WK) {
+            u32x2 w[4], x[4];
+            unsigned e_w[4], e_x;  // of four blocks each: bytes behind the last block are not read as scales
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+              const bool real = step * 4 + b < a.blocks;
+              w[b] = mx_raw<FW>(rw, has_w && real ? at(of_w, a.ldw, step * 4 + b, RBW / 16) : kOobGroup);
+              x[b] = mx_raw<FX>(rx, has_x && real ? at(of_x, a.ldx, step * 4 + b, RBX / 16) : kOobGroup);
+            }
+            e_x = mx_word(rsx, has_x ? (unsigned)(of_x * (int)a.ldxs + step * 4) : kOobGroup);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) e_w[e] = mx_word(rsw, n0 + to + e < a.n ? (unsigned)((to + e) * (int)a.ldws + step * 4) : kOobGroup);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+              if (step * 4 + b >= a.blocks) break;
+              const f32x4 none = {};
+              const f32x4 sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mx_eight<FW>(w[b].x, w[b].y, 127), mx_eight<FX>(x[b].x, x[b].y, 127), none, 0, 0, 0);
+              const int sx = e_x >> 8 * b & 255;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const int sw = e_w[e] >> 8 * b & 255;
+                total[e] += sw == 255 || sx == 255 ? __builtin_nanf("") : __builtin_amdgcn_ldexpf(sum[e], sw + sx - 254);
+              }
+            }
+          }
+          acc[i][j] = total;
+        }
     }
   }
   // The compiler counts the waits behind this instruction's results by the passes of 4-bit

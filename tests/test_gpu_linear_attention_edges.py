@@ -6,8 +6,9 @@ import torch
 
 from paper_2008_03602_amd import _lib as L
 from gpu_util import device_ready, note
-from test_gpu_linear_attention import B, CODE, D, F, FORMATS, check_norm, codes_of, mx_buffers, quantise64
-from test_gpu_sequence import gen, normal, stream
+from test_gpu_linear_attention import (B, CODE, D, F, FORMATS, NAN, PAIRS, ROUND, U, check_norm, codes_of, dropped, mx_buffers,
+                                       quantise64, random_rows, values_of)
+from test_gpu_sequence import gen, normal, stream, within
 
 pytestmark = pytest.mark.gpu
 
@@ -65,3 +66,65 @@ def test_norm_of_huge_values(dtype):
     for std in (1e21, 1e36):
         check_norm(3, 200, dtype, F, std=std, residual=False, seed=2)
         check_norm(3, 200, dtype, L.MX_E4M3, std=std, residual=False, seed=2)
+
+
+# ------------------------------------------------------------------ product
+def far_rows(g, m, n, k, fx, fw):
+    """Rows of x and w whose blocks' scales lie anywhere, such that those of a block of both make up for each
+    other: products of normal size."""
+    xq, xs, _ = random_rows(g, m, k, fx)
+    wq, wsc, _ = random_rows(g, n, k, fw)
+    blocks = (k + 31) // 32
+    ends = torch.tensor([0, 1, 2, 3, 5, 8, 9, 10, 60, 127, 200, 245, 246, 247, 249, 252, 253, 254])
+    s = ends[torch.randint(0, len(ends), (blocks,), generator=g)]
+    for scales, centre in ((xs, s), (wsc, 254 - s)):
+        near = centre + torch.randint(-2, 3, (scales.shape[0], blocks), generator=g)
+        scales[:, :blocks] = near.clamp(0, 254).to(torch.uint8).cuda()
+    return xq, xs, values_of(xq.cpu(), xs.cpu(), k, fx), wq, wsc, values_of(wq.cpu(), wsc.cpu(), k, fw)
+
+
+def check_far(m, n, k, fx, fw, out, nan=True):
+    note("mx product of far scales m%d n%d k%d formats %d %d -> %s" % (m, n, k, fx, fw, out))
+    xq, xs, x, wq, wsc, w = far_rows(gen(m + n + k), m, n, k, fx, fw)
+    want, mag = x @ w.t(), x.abs() @ w.abs().t()
+    assert 1e-3 < float(mag.median()) < 1e12
+    if nan:  # a block without an element that is not 0 is NaN all the same
+        row = L.mx_row_bytes(32, fx)
+        xq[m // 2, :row] = 0
+        xs[m // 2, 0] = 255
+        wsc[n // 3, (k + 31) // 32 - 1] = 255
+        want[m // 2], want[:, n // 3] = NAN, NAN
+    op = L.make_mx_linear(m, n, k, fx, fw, CODE[out])
+    ws = torch.full((max(16, L.ct_mx_linear_workspace(op)),), 255, dtype=torch.uint8, device="cuda")
+    y = torch.full((m, n), NAN, dtype=out, device="cuda")
+    L.ct_mx_linear_run(op, xq, xs, wq, wsc, None, None, y, ws, stream())
+    torch.cuda.synchronize()
+    # exact products, k sums in fp32; what the matrix cores drop for bf16
+    bound = (k + 4) * U * mag + (dropped(x, w) if out == B else 0.0)
+    within(y, want, bound + ROUND[out] * (want.abs() + bound), "far scales m%d n%d k%d %d %d %s" % (m, n, k, fx, fw, out))
+
+
+@pytest.mark.parametrize("out", [B, F])
+@pytest.mark.parametrize("fx,fw", PAIRS)
+@pytest.mark.parametrize("m,n,k", [(1, 16, 32), (5, 33, 129), (20, 40, 96), (33, 48, 1000), (130, 70, 515), (200, 260, 4000),
+                                   (20, 24, 9000)])
+def test_product_of_scales_that_make_up_for_each_other(m, n, k, fx, fw, out):
+    check_far(m, n, k, fx, fw, out)
+
+
+@pytest.mark.parametrize("fx,fw", PAIRS)
+def test_product_of_blocks_of_zeros_with_any_scale(fx, fw):
+    """Scales of blocks that are all 0 change nothing, to the bit."""
+    g = gen(8)
+    xq, xs, x = random_rows(g, 70, 256, fx)
+    wq, wsc, w = random_rows(g, 66, 256, fw)
+    row = L.mx_row_bytes(32, fx)
+    xq[:, 2 * row:3 * row], xq[5] = 0, 0
+    y, z = (torch.empty(70, 66, device="cuda") for _ in range(2))
+    op = L.make_mx_linear(70, 66, 256, fx, fw, L.DT_F32)
+    for scale, to in ((127, y), (0, z), (254, z)):
+        xs[:, 2], xs[5] = scale, scale
+        L.ct_mx_linear_run(op, xq, xs, wq, wsc, None, None, to, None, stream())
+        torch.cuda.synchronize()
+        assert to is y or torch.equal(y, z)
+    assert (y[5] == 0).all()
