@@ -26,6 +26,7 @@
 
 #include "k_linear.h"
 #include "k_mx.h"
+#include "mx_linear_plan.h"
 
 namespace ct {
 
@@ -371,68 +372,7 @@ __global__ void __launch_bounds__(64 * WM * WN * WK, mx_waves(EXACT, BM * BN)) m
 }
 
 // ------------------------------------------------------------------ plans and launches
-enum { MXL_32X16, MXL_32, MXL_64, MXL_128X64, MXL_128, MXL_256, MXL_KINDS };
-struct MxShape {
-  int bm, bn, wm, wn, wk, stages;
-};
-constexpr MxShape kMxTiles[MXL_KINDS] = {{32, 16, 1, 1, 8, 3}, {32, 32, 1, 2, 4, 3}, {64, 64, 2, 2, 2, 3}, {128, 64, 2, 2, 1, 3},
-                                         {128, 128, 2, 2, 1, 2}, {256, 256, 4, 2, 1, 2}};
-
-static int64_t tiles_of(const ct_mx_linear_op& op, int kind) {
-  const MxShape t = kMxTiles[kind];
-  return (((int64_t)op.m + t.bm - 1) / t.bm) * (((int64_t)op.n + t.bn - 1) / t.bn);
-}
-
-MxLinearPlan plan_mx_linear(const ct_mx_linear_op& op) {
-  MxLinearPlan p = {};
-  const int steps = (int)(((int64_t)op.k + 127) / 128);
-  // Rounds of the device, and what a round costs beside one of 64 x 64 tiles, of which a compute unit
-  // has two at a time (as of 128 x 64). Measured on 1021 x 515 by 1277, 512 x 2048 by 2048, 200 x 1024
-  // by 4096, 2048^3, 4096 x 1024 by 1024, 4000 x 500 by 3000, 16000 x 320 by 320 and 8192 x 4096 by
-  // 8192: the choice is the fastest or within 12 % of it. With the elements in bf16 256 x 256 tiles
-  // leave no registers.
-  auto rounds = [&](int kind, int blocks) { return (double)((tiles_of(op, kind) + kPlanCus * blocks - 1) / (kPlanCus * blocks)); };
-  const double r128 = rounds(MXL_128, 1);
-  const std::pair<int, double> costs[] = {{MXL_64, rounds(MXL_64, 2)},
-                                          {MXL_128X64, 1.7 * rounds(MXL_128X64, 2)},
-                                          {MXL_128, r128 > 1 ? 1.5 * r128 : 1.7},
-                                          {MXL_256, op.out_dtype == CT_DT_F32 ? 1e299 : 4.6 * rounds(MXL_256, 1)}};
-  double least = 1e300;
-  for (auto [kind, cost] : costs)
-    if (cost < least) {
-      least = cost;
-      p.kind = kind;
-    }
-  // Up to 64 rows or columns past whole 256 x 256 tiles would take the device another round; they go
-  // apart where that is less: 8192 x 2048 by 8208 186 to 177 us, 4096 x 4096 by 8224 203 to 158,
-  // 4100 x 4096 by 8200 206 to 164, 8192 x 4096 by 2064 116 to 87, 4096 x 512 by 4100 24.5 to 26.2
-  if (op.out_dtype == CT_DT_BF16 && op.m > 32)
-    for (int tails = 1; tails < 4; ++tails) {
-      const int tm = tails & 1 ? op.m % 256 : 0, tn = tails & 2 ? op.n % 256 : 0;
-      if (tm > 64 || tn > 64 || (tails & 1 && !tm) || (tails & 2 && !tn)) continue;
-      const int64_t tiles = (((int64_t)op.m - tm + 255) / 256) * (((int64_t)op.n - tn + 255) / 256);
-      const double cost = 4.6 * (double)((tiles + kPlanCus - 1) / kPlanCus) + (tm != 0) + (tn != 0);
-      if (!tiles || cost >= least) continue;
-      least = cost;
-      p.kind = MXL_256;
-      p.tail_m = tm;
-      p.tail_n = tn;
-    }
-  // Smaller tiles where 64 x 64 leaves compute units without one: 64 x 4096 by 4096 13.6 to 7.7 us, and
-  // for few rows 24 x 8192 by 4096 11.1 to 9.5
-  if (op.m <= 32 || (p.kind == MXL_64 && tiles_of(op, MXL_64) < kPlanCus * 3 / 4)) p.kind = MXL_32;
-  if (p.kind == MXL_32 && op.m <= 32 && tiles_of(op, MXL_32) < kPlanCus * 3 / 4) p.kind = MXL_32X16;
-  // A long reduction over few tiles: slices of it, of 32 steps at least, so that they save more
-  // than the second kernel takes
-  const int64_t blocks = tiles_of(op, p.kind);
-  int split = 1;
-  if (blocks <= kPlanCus / 4 && steps >= 64) split = (int)(kPlanCus / blocks < steps / 32 ? kPlanCus / blocks : steps / 32);
-  const int per = steps ? (steps + split - 1) / split : 1;
-  p.split = steps ? (steps + per - 1) / per : 1;
-  p.per_split = per;
-  p.ws_floats = p.split > 1 ? (int64_t)p.split * op.m * ((op.n + 3) / 4 * 4) : 0;
-  return p;
-}
+MxLinearPlan plan_mx_linear(const ct_mx_linear_op& op) { return mx_linear_plan(op); }
 
 template <int FW, int FX, bool EXACT, int KIND>
 static int mxl_launch(MxLinearArgs a, hipStream_t st) {
@@ -452,7 +392,8 @@ static int mxl_pick(const MxLinearArgs& a, int kind, hipStream_t st) {
     case MXL_128: return mxl_launch<FW, FX, EXACT, MXL_128>(a, st);
     default:
       if constexpr (!EXACT) return mxl_launch<FW, FX, EXACT, MXL_256>(a, st);
-      return mxl_launch<FW, FX, EXACT, MXL_128>(a, st);  // with the elements in bf16 it leaves no registers
+      set_error("ct_mx_linear_run: no 256 x 256 tiles of exact sums");  // mx_linear_plan takes none
+      return -2;
   }
 }
 template <int FW, int FX>
