@@ -5,10 +5,12 @@ import pytest
 import torch
 
 from paper_2008_03602_amd import _lib as L
+import test_gpu_linear_attention as block
 from gpu_util import device_ready, note
 from test_gpu_linear_attention import (B, CODE, D, F, FORMATS, NAN, PAIRS, ROUND, U, check_norm, codes_of, dropped, mx_buffers,
                                        quantise64, random_rows, values_of)
 from test_gpu_sequence import gen, normal, stream, within
+from test_host_linear_attention_plans import TILES
 
 pytestmark = pytest.mark.gpu
 
@@ -128,3 +130,30 @@ def test_product_of_blocks_of_zeros_with_any_scale(fx, fw):
         torch.cuda.synchronize()
         assert to is y or torch.equal(y, z)
     assert (y[5] == 0).all()
+
+
+def dropped_there(x, w):
+    """What `dropped` gives, worked out on the device: large products take the CPU minutes."""
+    m, k = x.shape
+    xa, wa = (torch.nn.functional.pad(t.abs(), (0, -k % 8)).reshape(t.shape[0], -1, 8).cuda() for t in (x, w))
+    out = torch.empty(m, w.shape[0], dtype=D, device="cuda")
+    for i in range(m):
+        out[i] = (xa[i][None] * wa).amax(2).sum(1)
+    return 7 * 2.0 ** -13 * out.cpu()
+
+
+@pytest.mark.parametrize("fx,fw", PAIRS)
+@pytest.mark.parametrize("m,n,k,out", [t[:4] for t in TILES])
+def test_product_on_every_tile(m, n, k, out, fx, fw, monkeypatch):
+    """Every kernel, whole and ragged tiles, the reduction in one and in slices, rows and columns apart; which
+    sizes reach which is checked where they are listed."""
+    monkeypatch.setattr(block, "dropped", dropped_there)
+    yp = n + (5 if m < 3000 else 0)
+    block.check_product(m, n, k, fx, fw, B if out == "bf16" else F, act=(m + k) % 5, res=1 + n % 2, seed=m + n, yp=yp,
+                        sp=L.mx_scale_bytes(k) + 4, in_place=m % 2 == 1)
+
+
+@pytest.mark.parametrize("fx,fw", PAIRS)
+@pytest.mark.parametrize("m,n,k", [t[:3] for t in TILES if t[3] == "f32"])
+def test_product_of_far_scales_on_every_exact_tile(m, n, k, fx, fw):
+    check_far(m, n, k, fx, fw, F)
