@@ -7,8 +7,8 @@ import torch
 from paper_2008_03602_amd import _lib as L
 import test_gpu_linear_attention as block
 from gpu_util import device_ready, note
-from test_gpu_linear_attention import (B, CODE, D, F, FORMATS, NAN, PAIRS, ROUND, U, check_norm, codes_of, dropped, mx_buffers,
-                                       quantise64, random_rows, values_of)
+from test_gpu_linear_attention import (B, CODE, D, F, FORMATS, INF, NAN, PAIRS, ROUND, U, attention_inputs, check_attention,
+                                       check_norm, codes_of, dropped, mx_buffers, quantise64, random_rows, run_plain, values_of)
 from test_gpu_sequence import gen, normal, stream, within
 from test_host_linear_attention_plans import TILES
 
@@ -157,3 +157,63 @@ def test_product_on_every_tile(m, n, k, out, fx, fw, monkeypatch):
 @pytest.mark.parametrize("m,n,k", [t[:3] for t in TILES if t[3] == "f32"])
 def test_product_of_far_scales_on_every_exact_tile(m, n, k, fx, fw):
     check_far(m, n, k, fx, fw, F)
+
+
+# ------------------------------------------------------------------ attention
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("key,value", [(64, 64), (64, 128), (128, 64), (128, 128), (256, 64), (256, 128), (250, 130), (256, 256)])
+def test_attention_in_pieces_of_every_shape(key, value, dtype):
+    """Each kernel of the pieces' ends, rows on 16 bytes and off them, the state written where it is read."""
+    for pad in (0, 3):
+        assert check_attention([600], 2, 1, key, value, dtype, in_place=True, pad=pad, seed=key + value) > 0
+    assert check_attention([330, 0, 5, 260], 2, 2, key, value, dtype, in_place=True, step_input=True, seed=key, lead=2) > 0
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+@pytest.mark.parametrize("name,bad", [("v", NAN), ("v", INF), ("k", NAN), ("k", -INF), ("q", NAN), ("delta", NAN), ("state", NAN),
+                                      ("state", INF)])
+def test_attention_in_pieces_keeps_infinities_and_nan_behind_their_token(name, bad, dtype):
+    """What a token's value reaches crosses the pieces behind it and nothing else: a sequence of nine pieces, the
+    value at the first and last row of one, inside one, at the sequence's ends, or in its state."""
+    heads, key, value, lens = 3, 32, 40, [40, 520, 90]
+    op = L.make_decay_attention(heads, heads, key, value, CODE[dtype], L.DT_F32)
+    seqs = L.make_sequences(sum(lens), 3, 3, 520, torch.zeros(4, dtype=torch.int32, device="cuda"))
+    assert L.ct_decay_attention_workspace(op, seqs) // (heads * (key * 2 * value * 4 + 4)) >= 9
+    s = attention_inputs(gen(4), sum(lens), heads, heads, key, value, 3, dtype, F)
+    clean, cs = run_plain(s, lens, heads, heads, key, value, dtype, s["state"])
+    for t in (40, 40 + 192, 40 + 255, 40 + 300, 559) if name != "state" else (40,):
+        note("attention in pieces: %s %s at token %d %s" % (name, bad, t, dtype))
+        d = {k: v.clone() if v is not None else None for k, v in s.items()}
+        reached = torch.zeros(sum(lens), heads, value, dtype=torch.bool)
+        rstate = torch.zeros(3, heads, key, value, dtype=torch.bool)
+        if name == "state":
+            d["state"][1, 1, 5, 7] = bad
+            reached[t:560, 1, 7] = rstate[1, 1, 5, 7] = True
+        else:
+            d[name][t, {"v": value + 7, "delta": 1}.get(name, key + 5)] = bad  # of the second head
+            if name == "q":
+                reached[t, 1] = True
+            elif name == "v":
+                reached[t:560, 1, 7] = rstate[1, 1, :, 7] = True
+            else:
+                reached[t:560, 1] = True
+                rstate[1, 1, 5 if name == "k" else slice(None)] = True
+        got, gs = run_plain(d, lens, heads, heads, key, value, dtype, d["state"])
+        flat = reached.reshape(sum(lens), -1)
+        assert torch.equal(got[~flat], clean[~flat]) and torch.equal(gs[~rstate], cs[~rstate]), (name, bad, t)
+        assert not torch.isfinite(got[flat]).any() and not torch.isfinite(gs[rstate]).any(), (name, bad, t)
+
+
+@pytest.mark.parametrize("dtype", [B, F])
+def test_attention_in_pieces_forgets_behind_an_infinite_rate(dtype):
+    """A decay of 0 inside a piece, at its first row and its last: what was before leaves nothing."""
+    heads, key, value, lens = 2, 32, 32, [600]
+    s = attention_inputs(gen(6), 600, heads, heads, key, value, 1, dtype, F)
+    for rows in ([100], [128], [191], [0, 64, 599]):
+        d = dict(s, delta=s["delta"].clone())
+        d["delta"][rows, 1] = INF
+        o, st = run_plain(d, lens, heads, heads, key, value, dtype, s["state"])
+        ref, bound, new, nbound = block.attention64({**d, "delta": d["delta"].clamp(max=1e4)}, torch.tensor([0, 600]), torch.tensor([0]),
+                                                    1.0, False, True, dtype)
+        within(o, ref, bound, "forgetting at %s" % rows)
+        within(st, new, nbound, "forgetting at %s: state" % rows)
