@@ -751,7 +751,7 @@ __global__ void __launch_bounds__(256) decay_join_kernel(DecayArgs a) {
   const int at = (int)blockIdx.y * 256 + (int)threadIdx.x;
   const SeqRange r = seq_range(a.seqs, s);
   const int pieces = tiles_in(r.end - r.begin, a.piece);
-  const int64_t unit = a.seqs.offsets ? r.begin / a.piece + (int64_t)s : (int64_t)s * a.per;
+  const int64_t unit = a.seqs.offsets ? first_tile(r.begin, a.piece, s) : (int64_t)s * a.per;
   if (at >= a.frames || pieces < 2) return;
   const int64_t step = (int64_t)a.heads * a.frames;
   f32x4* p = a.ends + (unit * a.heads + head) * a.frames + at;

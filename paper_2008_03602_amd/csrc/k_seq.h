@@ -186,10 +186,15 @@ __device__ __forceinline__ float activate(float v, int act) {
 struct SeqRange {
   int s, begin, end;  // rows begin..end-1 of sequence s
 };
+// The row an offset says, kept inside least..tokens.
+constexpr int seq_row(int offset, int least, int tokens) {
+  const int row = offset > least ? offset : least;
+  return row < tokens ? row : tokens;
+}
 // The rows of sequence s, kept inside 0..tokens whatever the offsets hold.
 __device__ __forceinline__ SeqRange seq_range(const SeqView& v, int s) {
   if (!v.offsets) return {s, s * v.len, s * v.len + v.len};
-  const int b = min(max(v.offsets[s], 0), v.tokens), e = min(max(v.offsets[s + 1], b), v.tokens);
+  const int b = seq_row(v.offsets[s], 0, v.tokens), e = seq_row(v.offsets[s + 1], b, v.tokens);
   return {s, b, e};
 }
 // State slot of sequence s, -1 for none.
@@ -207,11 +212,13 @@ struct SeqTiles {
   int64_t total;
   int per;  // tiles of each sequence where the lengths are equal
 };
-inline SeqTiles seq_tiles(const SeqView& v, int step) {
+constexpr SeqTiles seq_tiles(const SeqView& v, int step) {
   if (v.offsets) return {(int64_t)v.tokens / step + v.count, 0};
   const int per = v.len > step ? tiles_in(v.len, step) : 1;
   return {(int64_t)per * v.count, per};
 }
+// The number of a sequence's first tile, where lengths are not equal.
+constexpr int first_tile(int begin, int step, int s) { return begin / step + s; }
 // The end of a tile that starts at row t0 of a sequence: 2^31 rows may be less than a tile away.
 constexpr int tile_end(int t0, int end, int step) { return end - t0 > step ? t0 + step : end; }
 // The row that tile k of a sequence starts at: its end at most, -1 for a number past that (and
@@ -234,7 +241,7 @@ __device__ __forceinline__ SeqRange find_tile(const SeqView& v, int per, int ste
   while (true) {
     const int stride = (n + 63) / 64, i = lane * stride;
     const bool at_or_before =
-        i < n && min(max(v.offsets[lo + min(i, n - 1)], 0), v.tokens) / step + lo + i <= id;
+        i < n && first_tile(seq_row(v.offsets[lo + min(i, n - 1)], 0, v.tokens), step, lo + i) <= id;
     const uint64_t below = __ballot(!at_or_before);  // the first lane past the tile
     const int k = below ? __builtin_ctzll(below) : 64;
     if (k == 0) return {-1, 0, 0};
@@ -244,7 +251,7 @@ __device__ __forceinline__ SeqRange find_tile(const SeqView& v, int per, int ste
   }
   lo = __builtin_amdgcn_readfirstlane(lo);
   const SeqRange r = seq_range(v, lo);
-  *first = tile_start(r.begin, r.end, step, id - (r.begin / step + lo));
+  *first = tile_start(r.begin, r.end, step, id - first_tile(r.begin, step, lo));
   return *first < 0 ? SeqRange{-1, 0, 0} : r;
 }
 

@@ -22,9 +22,9 @@ TILES = [
 ]
 
 
-def holds(tmp_path, unit):
+def holds(tmp_path, unit, header="mx_linear_plan.h"):
     src = tmp_path / "unit.hip"
-    src.write_text('#include "mx_linear_plan.h"\n' + unit)
+    src.write_text('#include "%s"\n' % header + unit)
     cmd = [B._hipcc()] + B.HIP_FLAGS + ["--offload-host-only", "-fsyntax-only", "-fconstexpr-steps=100000000", str(src)]
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
     assert r.returncode == 0, r.stdout[-3000:]
@@ -84,3 +84,79 @@ static_assert(sound(), "");
 def test_workspaces_are_as_the_plans_say(m, n, k, out, kind, split, tm, tn):
     op = L.make_mx_linear(m, n, k, L.MX_E4M3, L.MX_E2M1, L.DT_BF16 if out == "bf16" else L.DT_F32)
     assert (L.ct_mx_linear_workspace(op) > 0) == bool(split)
+
+
+def test_pieces_of_bad_offsets_have_places_of_their_own(tmp_path):
+    """A sequence's pieces are numbered from first_tile on. Whatever the offsets hold, the places of its pieces,
+    the last one's too, are below the total that workspaces are sized by; where the offsets ascend no two
+    sequences have one in common, and every row lies in one piece."""
+    holds(tmp_path, r"""
+constexpr unsigned next(unsigned& seed) { return seed = seed * 1664525u + 1013904223u, seed >> 8; }
+constexpr bool inside() {
+  unsigned seed = 3;
+  for (int round = 0; round < 3000; ++round) {
+    const int count = 1 + next(seed) % 7, step = 64 * (1 + next(seed) % 4), tokens = next(seed) % 3000;
+    const bool ascend = next(seed) % 2;
+    int offsets[8] = {}, last = 0;
+    for (int i = 0; i <= count; ++i) {
+      const unsigned kind = next(seed) % 6;
+      if (ascend) offsets[i] = last = last + (kind ? (int)(next(seed) % (tokens - last + 1)) / 2 : 0);
+      else offsets[i] = kind == 0 ? -2147483647 - 1 : kind == 1 ? 2147483647 : (int)(next(seed) % (tokens + 200)) - 100;
+    }
+    const ct::SeqView view = {offsets, nullptr, tokens, count, count, 0};
+    const int64_t total = ct::seq_tiles(view, step).total;
+    int64_t behind = 0;  // the first number that no sequence so far has
+    for (int s = 0; s < count; ++s) {
+      const int begin = ct::seq_row(offsets[s], 0, tokens), end = ct::seq_row(offsets[s + 1], begin, tokens);
+      if (begin < 0 || begin > end || end > tokens) return false;
+      const int first = ct::first_tile(begin, step, s), tiles = ct::tiles_in(end - begin, step), owned = tiles ? tiles : 1;
+      if (first < 0 || first + owned > total || (ascend && first < behind)) return false;
+      behind = first + owned;
+      int row = begin;
+      for (int k = 0; k < tiles; ++k) {
+        const int at = ct::tile_start(begin, end, step, k);
+        if (at != row || at >= end) return false;
+        row = ct::tile_end(at, end, step);
+      }
+      if (row != end || ct::tile_start(begin, end, step, tiles + 1) >= 0) return false;
+    }
+  }
+  return true;
+}
+static_assert(inside(), "");
+constexpr bool equal_lengths() {
+  for (int len : {0, 1, 63, 64, 65, 1000, 1 << 29})
+    for (int step : {64, 256})
+      for (int count : {0, 1, 3}) {
+        const ct::SeqView view = {nullptr, nullptr, len * count, count, count, len};
+        const ct::SeqTiles t = ct::seq_tiles(view, step);
+        if (t.per < 1 || t.total != (int64_t)t.per * count || (int64_t)t.per * step < len) return false;
+      }
+  return true;
+}
+static_assert(equal_lengths(), "");
+""", "k_seq.h")
+
+
+def test_workspaces_of_attention_hold_every_piece():
+    """The library's own answer: a state and a decay for each head and piece, for as many pieces as it takes."""
+    for tokens, count, heads, key, value in ((65536, 1, 2, 128, 128), (600, 1, 2, 250, 130), (4096, 3, 4, 64, 64), (70000, 1000, 1, 8, 8)):
+        op = L.make_decay_attention(heads, heads, key, value, L.DT_BF16)
+        need = L.ct_decay_attention_workspace(op, L.make_sequences(tokens, count, count, tokens, 0x1000))
+        dk = 64 if key <= 64 else 128 if key <= 128 else 256
+        columns = -(-value // 64) * 64 if value <= 64 or dk == 256 else -(-value // 128) * 128
+        each = 4 * heads * (dk * columns + 1)
+        assert need > 0 and need % each == 0
+        pieces = need // each - count  # tokens / piece
+        assert 1 <= pieces <= tokens // 64
+
+
+def test_attention_refuses_a_workspace_that_is_too_small():
+    ok = 0x1000
+    op, seqs = L.make_decay_attention(2, 2, 128, 128, L.DT_BF16), L.make_sequences(65536, 1, 1)
+    need = L.ct_decay_attention_workspace(op, seqs)
+    assert need > 0
+    for ws, have, what in ((None, 0, "workspace"), (ok, need - 1, "workspace"), (ok + 8, need, "16-byte")):
+        with pytest.raises(L.CtError) as e:
+            L.ct_decay_attention_run(op, seqs, ok, ok, ok, ok, ok, ok, ok, ok, ok, ws=ws, ws_bytes=have)
+        assert e.value.code == L.CT_E_ARG and what in str(e.value)
