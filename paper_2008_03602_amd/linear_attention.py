@@ -110,7 +110,7 @@ class LinearAttentionBlock:
     def run(self, plan: dict, x: torch.Tensor, y: torch.Tensor) -> torch.Tensor:
         """One pass over x (rows x model) into y on the current stream; the slots move on. The
         calls follow each other on one stream, so they share a workspace. Rows of no sequence
-        come out as they went in."""
+        come out as they went in, those with an infinity or NaN as NaN."""
         for t in (x, y):
             if t.dtype != self.dtype or not t.is_cuda or t.shape != (plan["seqs"].tokens, self.model) or \
                     not t.is_contiguous():

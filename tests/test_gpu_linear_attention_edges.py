@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2008_03602_amd import _lib as L
+from paper_2008_03602_amd.linear_attention import LinearAttentionBlock
 import test_gpu_linear_attention as block
 from gpu_util import device_ready, note
 from test_gpu_linear_attention import (B, CODE, D, F, FORMATS, INF, NAN, PAIRS, ROUND, U, attention_inputs, check_attention,
@@ -217,3 +218,30 @@ def test_attention_in_pieces_forgets_behind_an_infinite_rate(dtype):
                                                     1.0, False, True, dtype)
         within(o, ref, bound, "forgetting at %s" % rows)
         within(st, new, nbound, "forgetting at %s: state" % rows)
+
+
+# ------------------------------------------------------------------ the block
+def test_rows_of_nobody_may_hold_anything():
+    """Infinities and NaN in rows of no sequence leave every other row, of a sequence or not, and the states as
+    they are without them; the rows themselves come out NaN."""
+    net = LinearAttentionBlock(256, 4, 2, 32, 64, slots=4, max_rows=300)
+    off = torch.tensor([5, 75, 75, 200, 233], dtype=torch.int32, device="cuda")
+    plan = net.plan(net.sequences(240, 4, 125, off))
+    x = normal(gen(3), 240, 256, dtype=B)
+    wild = x.clone()
+    wild[2, 7], wild[234, 0], wild[236] = INF, -INF, NAN
+    note("a block with infinities and NaN in rows of nobody")
+    outs = []
+    for t in (x, wild, x):
+        net.reset()
+        y = torch.empty(240, 256, dtype=B, device="cuda")
+        net.run(plan, t.cuda(), y)
+        outs.append((y.cpu(), net.state.cpu()))
+    others = torch.ones(240, dtype=torch.bool)
+    others[[2, 234, 236]] = False
+    assert torch.equal(outs[0][0], outs[2][0]) and torch.equal(outs[0][1], outs[2][1])
+    assert torch.equal(outs[1][0][others], outs[0][0][others]) and torch.equal(outs[1][1], outs[0][1])
+    assert torch.isnan(outs[1][0][~others]).all()
+    inside = torch.zeros(240, dtype=torch.bool)
+    inside[5:233] = True
+    assert torch.equal(outs[0][0][~inside], x[~inside]) and torch.isfinite(outs[0][0].float()).all()
