@@ -14,7 +14,8 @@
 // its scale exactly while both are of normal size, and multiplied by the 16-bit instruction: products
 // exact, sums in fp32. A wave that meets a block whose scale would leave bf16 (bytes below 10 or above 246
 // of e4m3, 2 and 252 of e2m1, in a block that is not all 0) sums its part of the tile again, of elements
-// without their scales, and scales each block's sum: the other operand's scale may bring it back.
+// without their scales, and scales each block's sum: the other operand's scale may bring it back. Rows
+// without such a block keep the sums that they had.
 //
 // Measured, 8-bit x by 4-bit w: 8192 x 4096 by 8192 with SiLU 236-275 us by the card (2.0-2.3 PFLOP/s). Its
 // matrix cores are busy 52 % of its clocks, at 1.9 GHz: 65 % of a step's, and 23 thousand clocks of each
@@ -109,12 +110,16 @@ __device__ __forceinline__ bool mx_far(int scale) {
   constexpr int LOW = FORMAT == CT_MX_E4M3 ? 10 : 2, HIGH = FORMAT == CT_MX_E4M3 ? 246 : 252;
   return (unsigned)(scale - LOW) > (unsigned)(HIGH - LOW);
 }
-// Whether that matters for a block: not where every element is 0.
+// Whether that matters for elements of a block: not where all of them are 0.
+template <int FORMAT>
+__device__ __forceinline__ bool mx_counts(u32x2 bits, int scale) {
+  return mx_far<FORMAT>(scale) && (scale == 255 || ((bits.x | bits.y) & (FORMAT == CT_MX_E4M3 ? 0x7F7F7F7Fu : 0x77777777u)) != 0);
+}
 template <int FORMAT>
 __device__ __forceinline__ bool mx_counts(const MxFrag<FORMAT>& f, int scale) {
-  unsigned bits = f.lo.x | f.lo.y | f.lo.z | f.lo.w;
-  if constexpr (FORMAT == CT_MX_E4M3) bits |= f.hi.x | f.hi.y | f.hi.z | f.hi.w;
-  return mx_far<FORMAT>(scale) && (scale == 255 || (bits & (FORMAT == CT_MX_E4M3 ? 0x7F7F7F7Fu : 0x77777777u)) != 0);
+  u32x2 bits = {f.lo.x | f.lo.y, f.lo.z | f.lo.w};
+  if constexpr (FORMAT == CT_MX_E4M3) bits |= (u32x2){f.hi.x | f.hi.y, f.hi.z | f.hi.w};
+  return mx_counts<FORMAT>(bits, scale);
 }
 constexpr int mx_code(int format) { return format == CT_MX_E4M3 ? 0 : 4; }  // of the instruction
 
@@ -329,6 +334,7 @@ __global__ void __launch_bounds__(64 * WM * WN * WK, mx_waves(EXACT, BM * BN)) m
     if (again) {
       // The wave's sums once more, a tile at a time and a block, 32 elements, with each instruction: the tiles
       // that are done wait where the sums of every wave are, and nothing else needs registers that others do not.
+      // Outputs of rows without such a block keep theirs: their bits are no matter of other rows.
       const auto at = [&](int row, int64_t ld, int block, int bytes) { return (unsigned)(row * (int)ld + block * bytes * 4 + kg * bytes); };
 #pragma unroll
       for (int i = 0; i < TN; ++i)
@@ -337,16 +343,18 @@ __global__ void __launch_bounds__(64 * WM * WN * WK, mx_waves(EXACT, BM * BN)) m
           const int of_w = wn + i * 16 + lrow, of_x = wm + j * 16 + lrow, to = wn + i * 16 + kg * 4;
           const bool has_w = n0 + of_w < a.n, has_x = m0 + of_x < a.m;
           f32x4 total = {};
+          int bad_w = 0, bad_x = 0;  // of the rows whose elements the lane reads
 #pragma unroll 1
           for (int step = begin + team; step < end; step += WK) {
             u32x2 w[4], x[4];
-            unsigned e_w[4], e_x;  // of four blocks each: bytes behind the last block are not read as scales
+            unsigned e_w[4], e_x, own_w;  // of four blocks each: bytes behind the last block are not read as scales
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
               const bool real = step * 4 + b < a.blocks;
               w[b] = mx_raw<FW>(rw, has_w && real ? at(of_w, a.ldw, step * 4 + b, RBW / 16) : kOobGroup);
               x[b] = mx_raw<FX>(rx, has_x && real ? at(of_x, a.ldx, step * 4 + b, RBX / 16) : kOobGroup);
             }
+            own_w = mx_word(rsw, has_w ? (unsigned)(of_w * (int)a.ldws + step * 4) : kOobGroup);
             e_x = mx_word(rsx, has_x ? (unsigned)(of_x * (int)a.ldxs + step * 4) : kOobGroup);
 #pragma unroll
             for (int e = 0; e < 4; ++e) e_w[e] = mx_word(rsw, n0 + to + e < a.n ? (unsigned)((to + e) * (int)a.ldws + step * 4) : kOobGroup);
@@ -356,6 +364,8 @@ __global__ void __launch_bounds__(64 * WM * WN * WK, mx_waves(EXACT, BM * BN)) m
               const f32x4 none = {};
               const f32x4 sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mx_eight<FW>(w[b].x, w[b].y, 127), mx_eight<FX>(x[b].x, x[b].y, 127), none, 0, 0, 0);
               const int sx = e_x >> 8 * b & 255;
+              bad_w |= mx_counts<FW>(w[b], own_w >> 8 * b & 255);
+              bad_x |= mx_counts<FX>(x[b], sx);
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
                 const int sw = e_w[e] >> 8 * b & 255;
@@ -363,7 +373,14 @@ __global__ void __launch_bounds__(64 * WM * WN * WK, mx_waves(EXACT, BM * BN)) m
               }
             }
           }
-          acc[i][j] = total;
+          const auto whole = [](int bad) {  // of the row, from its four lanes
+            bad |= __shfl_xor(bad, 16);
+            return bad | __shfl_xor(bad, 32);
+          };
+          bad_w = whole(bad_w);
+          bad_x = whole(bad_x);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = __shfl(bad_w, kg * 4 + e) | bad_x ? total[e] : acc[i][j][e];
         }
     }
   }

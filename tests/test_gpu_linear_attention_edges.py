@@ -133,6 +133,28 @@ def test_product_of_blocks_of_zeros_with_any_scale(fx, fw):
     assert (y[5] == 0).all()
 
 
+@pytest.mark.parametrize("fx,fw", PAIRS)
+@pytest.mark.parametrize("m,n,k", [(20, 24, 600), (70, 66, 1000), (40, 70, 9000), (2000, 2010, 200), (2900, 2200, 168)])
+def test_product_of_far_scales_leaves_the_bits_of_other_rows(m, n, k, fx, fw):
+    g = gen(m + k)
+    xq, xs, _ = random_rows(g, m, k, fx)
+    wq, wsc, _ = random_rows(g, n, k, fw)
+    op = L.make_mx_linear(m, n, k, fx, fw, L.DT_F32)
+    ws = torch.full((max(16, L.ct_mx_linear_workspace(op)),), 255, dtype=torch.uint8, device="cuda")
+    ys = []
+    for far in (False, True):
+        if far:
+            xs[m // 2, 0], xs[1, 3], xs[3, (k + 31) // 32 - 1], xs[5, 1], wsc[n // 2, 2] = 1, 255, 254, 0, 250
+        y = torch.empty(m, n, device="cuda")
+        L.ct_mx_linear_run(op, xq, xs, wq, wsc, None, None, y, ws, stream())
+        torch.cuda.synchronize()
+        ys.append(y.cpu())
+    same = torch.ones(m, n, dtype=torch.bool)
+    same[[m // 2, 1, 3, 5]], same[:, n // 2] = False, False
+    assert torch.equal(ys[0][same], ys[1][same])
+    assert torch.isnan(ys[1][1]).all() and torch.isfinite(ys[1][same]).all()
+
+
 def dropped_there(x, w):
     """What `dropped` gives, worked out on the device: large products take the CPU minutes."""
     m, k = x.shape
