@@ -106,16 +106,21 @@ __device__ __forceinline__ double logistic_f64(double z, const double* terms) {
 template <typename T, int OUT, int TEAM, int STEPS, bool EVEN>
 __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
   constexpr int TEAMS = 256 / TEAM, S = STEPS ? STEPS : 1;
-  const int unit = (int)blockIdx.x * TEAMS + (int)threadIdx.x / TEAM;  // below 2^31: units are, in whole blocks
+  // a wave's lanes are of one team where teams are waves and more: their row's arithmetic is the scalar ALU's
+  const int team = TEAM < 64 ? (int)threadIdx.x / TEAM : __builtin_amdgcn_readfirstlane((int)threadIdx.x / TEAM);
+  const int unit = (int)blockIdx.x * TEAMS + team;  // below 2^31: units are, in whole blocks
   const bool mine = unit < a.units;
-  const int row = mine ? fdiv(unit, a.groups) : 0, first = mine ? (unit - row * a.groups.d) * a.part : 0;
+  int row = mine ? unit : 0, first = 0;
+  if (a.groups.d > 1) {
+    row = fdiv(row, a.groups);
+    first = mine ? (unit - row * a.groups.d) * a.part : 0;
+  }
   const int lane = (int)threadIdx.x % TEAM, part = mine ? a.part : 0;
-  // pitches are at most 2^31: one product of 32 by 32 bits a row's start, not three
+  // Where the part starts in an array; pitches are at most 2^31: one product of 32 by 32 bits, not three
   const auto at = [&](int64_t ld) { return (int64_t)((uint64_t)(unsigned)row * (unsigned)ld); };
   const T* x = (const T*)a.x + at(a.ldx) + first;
-  const T* res = (const T*)a.res + at(a.ldres) + first;
-  const T* z = (const T*)a.z + at(a.ldz) + first;
-  T* sum = (T*)a.sum + at(a.ldsum) + first;
+  const auto res = [&] { return (const T*)a.res + at(a.ldres) + first; };
+  const auto z_row = [&] { return (const T*)a.z + at(a.ldz) + first; };
   const float* w = a.w + first;
   const auto col = [&](int s) { return (s * TEAM + lane) * 8; };
 
@@ -156,7 +161,7 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
   const auto read = [&](int c, float* v) __attribute__((always_inline)) {
     RawOct<T> q, r;
     load(q, x, c);
-    if (a.res) load(r, res, c);
+    if (a.res) load(r, res(), c);
     values(c, q, r, v);
   };
   const auto squares = [](const float* v) __attribute__((always_inline)) {  // of four chains, not one
@@ -173,8 +178,8 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
     for (int s = 0; s < S; ++s) {
       if (S <= 2 && a.w) load(weight[s], w, col(s));
       load(q[s], x, col(s));
-      if (a.res) load(r[s], res, col(s));
-      if (a.z) load(gate[s], z, col(s));
+      if (a.res) load(r[s], res(), col(s));
+      if (a.z) load(gate[s], z_row(), col(s));
     }
 #pragma unroll
     for (int s = 0; s < S; ++s) {
@@ -243,12 +248,11 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
       cut(c, y);
       const float error = norm_error(z, a.z), less = 1.f - error, more = 1.f + error;
       const unsigned largest = mx_largest(y), e = mx_scale<OUT>(largest);
-      const auto of = [&](float factor) {
-        return mx_scale<OUT>(__builtin_bit_cast(unsigned, __builtin_bit_cast(float, largest) * factor));
-      };
+      // the exponents of largest * less and of largest * more, as steps of its last bit, rounded up
+      const unsigned reach = (unsigned)fmaf(error, 16777216.f, 1.f), low = largest - min(reach, largest);
       const u32x2 q = mx_elements<OUT>(y, mx_inverse(e) * less), top = mx_elements<OUT>(y, mx_inverse(e) * more);
       put(c, q, e);
-      return __ballot(q.x != top.x || q.y != top.y || of(less) != of(more) || error > 0.5f) != 0;
+      return __ballot(q.x != top.x || q.y != top.y || (low ^ (largest + reach)) >> 23 || error > 0.5f) != 0;
     }
   };
   // The same in fp64 from what is in memory still, over what write() left.
@@ -258,7 +262,7 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
     RawOct<float> wq;
     read(c, v);
     if (a.w) load(wq, w, c);
-    if (a.z) load(g, z, c);
+    if (a.z) load(g, z_row(), c);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       double d = (double)v[i] * scale64;
@@ -273,7 +277,7 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
   };
   // after the outputs, which may need x and res again: sum may be one of them
   const auto keep = [&](int c, const float* v) __attribute__((always_inline)) {
-    if (a.sum && c < part) store(sum + c, v, part - c);
+    if (a.sum && c < part) store((T*)a.sum + at(a.ldsum) + first + c, v, part - c);
   };
   if constexpr (STEPS > 0) {
     unsigned near = 0;  // a bit a step
@@ -288,7 +292,7 @@ __global__ void __launch_bounds__(256) norm_kernel(NormArgs a) {
   } else {
     for (int s = 0; s * TEAM * 8 < part; ++s) {  // every lane, for the blocks' sake
       read(col(s), h[0]);
-      if (a.z) load(gate[0], z, col(s));
+      if (a.z) load(gate[0], z_row(), col(s));
       const bool near = write(col(s), h[0], gate[0], weight[0]);
       if constexpr (OUT == NORM_MX8 || OUT == NORM_MX4) {
         if (near) again(col(s));
